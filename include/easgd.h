@@ -356,6 +356,115 @@ int easgd_layer_product(int kind, int d_in, int d_out, int P, int b,
                         const float *A, const float *Wl, size_t ld, const float *dZ,
                         float *out, size_t out_ws, int relu, void *stream);
 
+/*
+ * ---- Rows of logits: what a network answers with -------------------------------------------------------------------
+ *
+ * The calls below work on the rows that a network's last layer puts out, before any softmax: those of the workers
+ * ([P][b][classes], rows = P*b) or of any larger model.
+ *
+ *   logits  DEVICE in  [rows][ld], row-major; a row's first V entries are its logits, entries [V, ld) are never read
+ *   dtype   EASGD_F32, EASGD_BF16 or EASGD_F16: the elements of logits (and of dlogits).  Arithmetic is fp32 or wider.
+ *   1 <= V <= 2^20, ld >= V, rows < 2^30; rows == 0 is a call that does nothing.
+ * Rows may start at any element's address; every alignment takes 128-bit accesses.
+ *
+ * The order of a row's logits, wherever one is meant: larger logits first, equal ones (0 and -0 among them) by
+ * ascending index.  A logit of -inf is a masked place.  Whole numbers that come back (indices, tokens) are exact.
+ * All results are the same bits from run to run.
+ *
+ * workspace: DEVICE scratch of at least the bytes that the call's _workspace_bytes function names for the same sizes (it
+ * may be 0: then workspace may be NULL), 256-byte aligned; contents undefined before and after.  Calls that may
+ * overlap in time (other streams, graphs that are replayed side by side) need workspaces of their own.
+ */
+typedef enum { EASGD_F32 = 0, EASGD_BF16 = 1, EASGD_F16 = 2 } easgd_dtype;
+#define EASGD_MAX_TOP 256
+
+/*
+ * The k first logits of every row's order and the row's log-sum-exp at a temperature: what a teacher hands on.
+ *
+ *   values   DEVICE out [rows][k] fp32    the k largest logits as they are, in the row's order
+ *   indices  DEVICE out [rows][k] int32   where they stand
+ *   lse      DEVICE out [rows] fp32, or NULL   log sum_j exp(logits[j] / temperature)
+ *   1 <= k <= EASGD_MAX_TOP; temperature in [1e-6, 1e6].
+ * A logit of -inf or NaN is never taken; places that are left over (k > V, masked rows) hold -inf and -1.
+ * lse is -inf for a row whose logits are all -inf, +inf where one is +inf, and otherwise NaN where one is NaN.
+ * Errors: EASGD_EINVAL, EASGD_ERANGE, EASGD_EWORKSPACE, EASGD_ELAUNCH.
+ */
+size_t easgd_top_logits_workspace_bytes(size_t rows, int V, int k);
+int easgd_top_logits(const void *logits, int dtype, size_t rows, int V, size_t ld, int k, float temperature,
+                     float *values, int32_t *indices, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Distillation: the loss of a student's logits z against a teacher's top logits a_i at places t_i, i < k, both at
+ * temperature T, mixed with the cross-entropy of a label y at temperature 1, and its gradient.  Per row:
+ *
+ *   q = softmax(z / T), S = {t_i};
+ *   teacher_lse == NULL:  p_i = exp(a_i/T) / sum_i exp(a_i/T)         the teacher's probabilities, renormalised over S
+ *   teacher_lse != NULL:  p_i = exp(a_i/T - teacher_lse)              the teacher's probabilities; what they leave over,
+ *                         r = max(0, 1 - sum_i p_i), R = sum of q outside S   is the probability of "any other place"
+ *   KL   = sum_i p_i (log p_i - log q[t_i])  (+ r (log r - log R); left out where r == 0 or no place outside S has mass)
+ *   loss = (1 - hard) T^2 KL + hard (log sum_j exp(z[j]) - z[y])
+ *   d loss / d z[j] = (1 - hard) T (c q[j] - sum of p_i with t_i == j - (j outside S: r q[j] / R)) + hard (softmax(z)[j] - (j == y))
+ *                     with c = sum_i p_i (+ r where its term counts)
+ *
+ *   indices      DEVICE in [rows][k] int32   t_i; an index outside [0, V) marks a slot that is not used (its value is ignored).  An
+ *                                            index that comes up twice counts with both probabilities.
+ *   values       DEVICE in [rows][k] fp32    a_i (-inf: probability 0), as easgd_top_logits writes them
+ *   teacher_lse  DEVICE in [rows] fp32, or NULL   at the same temperature, as easgd_top_logits writes it
+ *   labels       DEVICE in [rows] int32, or NULL (then hard == 0).  A row whose label is outside [0, V) is padding: its
+ *                                            logits are not read, its loss and gradient are 0.
+ *   loss         DEVICE out [rows] fp32
+ *   state        DEVICE out [rows][4] fp32   for the backward pass: m = max z, sum exp((z-m)/T), sum exp(z-m) (0 where
+ *                                            hard is 0), the first sum over the places outside S (0 without teacher_lse)
+ *   scale, dloss     the gradient is that of scale * sum over the rows of dloss[row] * loss[row]; dloss DEVICE in [rows] fp32, or
+ *                    NULL: all 1.  (Mean losses of b samples: scale = 1/b.)
+ *   dlogits      DEVICE out [rows][dld], element type of logits; entries [V, dld) of a row are not written; aligned like
+ *                                            logits, but need not share their alignment or stride
+ *   1 <= k <= EASGD_MAX_TOP; temperature in [1e-6, 1e6]; hard in [0, 1]; scale finite.
+ * A student's row whose logits are all -inf has loss and gradient 0, as has a row without a used slot as far as KL goes; a
+ * teacher's place where the student's logit is -inf gives an infinite loss and a finite gradient; a NaN or +inf among
+ * the row's logits gives NaN.
+ *
+ * easgd_distill_loss is the forward pass (state may be NULL), easgd_distill_grad the backward pass from what it left in
+ * state, easgd_distill both in one call.  Errors: EASGD_EINVAL, EASGD_ERANGE, EASGD_EWORKSPACE, EASGD_ELAUNCH.
+ */
+size_t easgd_distill_workspace_bytes(size_t rows, int V, int k);
+int easgd_distill_loss(const void *logits, int dtype, size_t rows, int V, size_t ld,
+                       const int32_t *indices, const float *values, const float *teacher_lse, int k, const int32_t *labels,
+                       float temperature, float hard, float *loss, float *state,
+                       void *workspace, size_t workspace_bytes, void *stream);
+int easgd_distill_grad(const void *logits, int dtype, size_t rows, int V, size_t ld,
+                       const int32_t *indices, const float *values, const float *teacher_lse, int k, const int32_t *labels,
+                       float temperature, float hard, const float *state, const float *dloss, float scale,
+                       void *dlogits, size_t dld, void *stream);
+int easgd_distill(const void *logits, int dtype, size_t rows, int V, size_t ld,
+                  const int32_t *indices, const float *values, const float *teacher_lse, int k, const int32_t *labels,
+                  float temperature, float hard, float scale, float *loss, void *dlogits, size_t dld,
+                  void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * One token of every row, drawn with a given random number.  With w[j] = exp((z[j] - max z) / temperature), the tokens
+ * that may be drawn are the shortest of three prefixes of the row's order (at least its first token):
+ *   top_k   its first top_k tokens;
+ *   top_p   the shortest prefix whose w sum up to at least top_p times the sum over the first top_k tokens;
+ *   min_p   the tokens with w >= min_p.
+ * The token is the first j in index order at which the running sum of w over these tokens exceeds u times their sum.
+ *
+ *   u            DEVICE in [rows] fp32 in [0, 1) (a NaN or a value below 0 counts as 0, one from 1 on as the largest below 1)
+ *   temperature  DEVICE in [rows] fp32, or NULL: 1.  0 (or less, or NaN): the first token of the order.
+ *   top_k        DEVICE in [rows] int32, or NULL; < 1: no limit
+ *   top_p        DEVICE in [rows] fp32, or NULL; >= 1 or NaN: no limit
+ *   min_p        DEVICE in [rows] fp32, or NULL; <= 0 or NaN: no limit
+ *   tokens       DEVICE out [rows] int32      -1 for a row without any logit above -inf
+ *   logprob      DEVICE out [rows] fp32, or NULL   log of w[token] over the sum of the tokens that may be drawn (NaN where tokens is -1)
+ * NaN logits count as masked.  Where logits are +inf, only those may be drawn, each with w = 1.
+ * Sums are whole numbers of units of 2^-51 (V <= 2048) up to 2^-42 (V = 2^20) of the largest w, so no order of addition changes them.
+ * Errors: EASGD_EINVAL, EASGD_ERANGE, EASGD_EWORKSPACE, EASGD_ELAUNCH.
+ */
+size_t easgd_sample_tokens_workspace_bytes(size_t rows, int V);
+int easgd_sample_tokens(const void *logits, int dtype, size_t rows, int V, size_t ld, const float *u,
+                        const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                        int32_t *tokens, float *logprob, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Number of parameters N of the packed layout for `dims`; 0 on invalid input. */
 size_t easgd_mlp_num_params(const int *dims, int n_layers);
 

@@ -78,6 +78,22 @@ def _load() -> ctypes.CDLL:
     lib.easgd_mlp_round_bf16v.restype = i
     lib.easgd_layer_product.argtypes = [i, i, i, i, i, vp, vp, sz, vp, vp, sz, i, vp]
     lib.easgd_layer_product.restype = i
+    lib.easgd_top_logits_workspace_bytes.argtypes = [sz, i, i]
+    lib.easgd_top_logits_workspace_bytes.restype = sz
+    lib.easgd_top_logits.argtypes = [vp, i, sz, i, sz, i, f, vp, vp, vp, vp, sz, vp]
+    lib.easgd_top_logits.restype = i
+    lib.easgd_distill_workspace_bytes.argtypes = [sz, i, i]
+    lib.easgd_distill_workspace_bytes.restype = sz
+    lib.easgd_distill_loss.argtypes = [vp, i, sz, i, sz, vp, vp, vp, i, vp, f, f, vp, vp, vp, sz, vp]
+    lib.easgd_distill_loss.restype = i
+    lib.easgd_distill_grad.argtypes = [vp, i, sz, i, sz, vp, vp, vp, i, vp, f, f, vp, vp, f, vp, sz, vp]
+    lib.easgd_distill_grad.restype = i
+    lib.easgd_distill.argtypes = [vp, i, sz, i, sz, vp, vp, vp, i, vp, f, f, f, vp, vp, sz, vp, sz, vp]
+    lib.easgd_distill.restype = i
+    lib.easgd_sample_tokens_workspace_bytes.argtypes = [sz, i]
+    lib.easgd_sample_tokens_workspace_bytes.restype = sz
+    lib.easgd_sample_tokens.argtypes = [vp, i, sz, i, sz, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.easgd_sample_tokens.restype = i
     lib.easgd_mlp_num_params.argtypes = [ip, i]
     lib.easgd_mlp_num_params.restype = sz
     lib.easgd_stream_copy.argtypes = [vp, vp, sz, vp]
@@ -366,6 +382,197 @@ def easgd_mlp_round(dims: Sequence[int], W, Wc, X, y, eta: float, rho: float, V=
                                 _dev("workspace", workspace, torch.uint8, nbytes), workspace.numel(),
                                 _stream(stream)))
     return workspace
+
+
+# ---- rows of logits ----------------------------------------------------------------------------------------------
+
+MAX_TOP = 256                       # EASGD_MAX_TOP of include/easgd.h
+_LOGIT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # easgd_dtype
+
+
+def _logit_rows(name: str, t: torch.Tensor):
+    """Address, element type, rows, row length and stride of a matrix of logits (rows may be strided, a row's elements not)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA/HIP tensor")
+    code = _LOGIT_TYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be torch.float32, torch.bfloat16 or torch.float16, got {t.dtype}")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be [rows][V]")
+    rows, V = t.shape
+    ld, step = t.stride()
+    if V > 1 and step != 1:
+        raise ValueError(f"{name}: a row's elements must follow one another")
+    if rows <= 1 or V == 0:
+        ld = max(V, 1)
+    elif ld < V:
+        raise ValueError(f"{name}: rows must not overlap (stride {ld}, length {V})")
+    return t.data_ptr(), code, rows, V, ld
+
+
+def _on_device_of(logits, **others) -> None:
+    """Everything a call touches is on the current device, where its kernels run."""
+    here = torch.cuda.current_device()
+    if logits.device.index != here:
+        raise ValueError(f"logits are on {logits.device}, the current device is cuda:{here}")
+    for name, t in others.items():
+        if t is not None and t.device != logits.device:
+            raise ValueError(f"{name} must be on {logits.device}, is on {t.device}")
+
+
+def _row_vector(name: str, t, dtype, rows: int):
+    """Address of an optional [rows] tensor."""
+    if t is None:
+        return None
+    if isinstance(t, torch.Tensor) and t.shape != (rows,):
+        raise ValueError(f"{name} must be [{rows}], got {list(t.shape)}")
+    return _dev(name, t, dtype, rows)
+
+
+def _teacher_slots(name: str, t, dtype, rows: int, k: int) -> int:
+    if isinstance(t, torch.Tensor) and t.shape != (rows, k):
+        raise ValueError(f"{name} must be [{rows}][{k}], got {list(t.shape)}")
+    return _dev(name, t, dtype, rows * k)
+
+
+def _new(shape, dtype, like, stream):
+    """A tensor for a result or for scratch; one that another stream than the current one works on is kept from reuse."""
+    t = torch.empty(shape, dtype=dtype, device=like.device)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
+def _scratch(nbytes: int, workspace, like, stream):
+    if workspace is None:
+        if nbytes == 0:
+            return None, None, 0
+        workspace = _new(nbytes, torch.uint8, like, stream)
+    elif workspace.device != like.device:
+        raise ValueError(f"workspace must be on {like.device}, is on {workspace.device}")
+    return workspace, _dev("workspace", workspace, torch.uint8, nbytes), workspace.numel()
+
+
+@functools.lru_cache(maxsize=256)
+def easgd_top_logits_workspace_bytes(rows: int, V: int, k: int) -> int:
+    return int(_lib.easgd_top_logits_workspace_bytes(rows, V, k))
+
+
+@functools.lru_cache(maxsize=256)
+def easgd_distill_workspace_bytes(rows: int, V: int, k: int) -> int:
+    return int(_lib.easgd_distill_workspace_bytes(rows, V, k))
+
+
+@functools.lru_cache(maxsize=256)
+def easgd_sample_tokens_workspace_bytes(rows: int, V: int) -> int:
+    return int(_lib.easgd_sample_tokens_workspace_bytes(rows, V))
+
+
+def easgd_top_logits(logits, k: int, temperature: float = 1.0, values=None, indices=None, lse=None, workspace=None, stream=None):
+    """The k first logits of every row's order and the row's log-sum-exp at `temperature`: what a teacher hands on.
+    logits [rows][V] (fp32, bf16 or fp16, rows may be strided) -> values [rows][k] fp32, indices [rows][k] int32,
+    lse [rows] fp32; places left over hold -inf and -1."""
+    ptr, code, rows, V, ld = _logit_rows("logits", logits)
+    _on_device_of(logits, values=values, indices=indices, lse=lse)
+    k = int(k)
+    if k < 1 or k > MAX_TOP:
+        raise ValueError(f"k must be in [1, {MAX_TOP}], got {k}")
+    if values is None:
+        values = _new((rows, k), torch.float32, logits, stream)
+    if indices is None:
+        indices = _new((rows, k), torch.int32, logits, stream)
+    if lse is None:
+        lse = _new((rows,), torch.float32, logits, stream)
+    _ws, ws, nbytes = _scratch(easgd_top_logits_workspace_bytes(rows, V, k), workspace, logits, stream)
+    _check(_lib.easgd_top_logits(ptr, code, rows, V, ld, k, temperature, _teacher_slots("values", values, torch.float32, rows, k),
+                                 _teacher_slots("indices", indices, torch.int32, rows, k), _row_vector("lse", lse, torch.float32, rows),
+                                 ws, nbytes, _stream(stream)))
+    return values, indices, lse
+
+
+def _distill_args(logits, indices, values, temperature, teacher_lse, labels, hard):
+    ptr, code, rows, V, ld = _logit_rows("logits", logits)
+    if not isinstance(indices, torch.Tensor) or indices.dim() != 2:
+        raise ValueError("indices must be [rows][k]")
+    k = indices.shape[1]
+    _on_device_of(logits, indices=indices, values=values, teacher_lse=teacher_lse, labels=labels)
+    return rows, V, k, (ptr, code, rows, V, ld, _teacher_slots("indices", indices, torch.int32, rows, k),
+                        _teacher_slots("values", values, torch.float32, rows, k), _row_vector("teacher_lse", teacher_lse, torch.float32, rows),
+                        k, _row_vector("labels", labels, torch.int32, rows), temperature, hard)
+
+
+def _gradient_rows(logits, dlogits, rows: int, V: int, stream):
+    if dlogits is None:
+        dlogits = _new((rows, V), logits.dtype, logits, stream)
+    ptr, code, drows, dV, dld = _logit_rows("dlogits", dlogits)
+    if dlogits.dtype != logits.dtype or (drows, dV) != (rows, V):
+        raise ValueError(f"dlogits must be [{rows}][{V}] {logits.dtype}, got {list(dlogits.shape)} {dlogits.dtype}")
+    _on_device_of(logits, dlogits=dlogits)
+    return dlogits, ptr, dld
+
+
+def easgd_distill_loss(logits, indices, values, temperature: float = 1.0, teacher_lse=None, labels=None, hard: float = 0.0,
+                       loss=None, state=None, workspace=None, stream=None):
+    """Forward pass of distillation: the loss of every row of student logits [rows][V] against the teacher's top logits
+    (indices, values [rows][k]; teacher_lse [rows] turns what they leave over into one more outcome), mixed with the
+    cross-entropy of labels [rows] by `hard`.  Returns loss [rows] and state [rows][4], which easgd_distill_grad takes."""
+    rows, V, k, args = _distill_args(logits, indices, values, temperature, teacher_lse, labels, hard)
+    if loss is None:
+        loss = _new((rows,), torch.float32, logits, stream)
+    if state is None:
+        state = _new((rows, 4), torch.float32, logits, stream)
+    _on_device_of(logits, loss=loss, state=state)
+    _ws, ws, nbytes = _scratch(easgd_distill_workspace_bytes(rows, V, k), workspace, logits, stream)
+    _check(_lib.easgd_distill_loss(*args, _row_vector("loss", loss, torch.float32, rows), _teacher_slots("state", state, torch.float32, rows, 4),
+                                   ws, nbytes, _stream(stream)))
+    return loss, state
+
+
+def easgd_distill_grad(logits, indices, values, state, temperature: float = 1.0, teacher_lse=None, labels=None, hard: float = 0.0,
+                       scale: float = 1.0, dloss=None, dlogits=None, stream=None):
+    """Backward pass of easgd_distill_loss: the gradient of scale * sum(dloss * loss) (dloss None: all ones) with respect to
+    the student's logits, in their type."""
+    rows, V, k, args = _distill_args(logits, indices, values, temperature, teacher_lse, labels, hard)
+    dlogits, dptr, dld = _gradient_rows(logits, dlogits, rows, V, stream)
+    _on_device_of(logits, state=state, dloss=dloss)
+    _check(_lib.easgd_distill_grad(*args, _teacher_slots("state", state, torch.float32, rows, 4), _row_vector("dloss", dloss, torch.float32, rows),
+                                   scale, dptr, dld, _stream(stream)))
+    return dlogits
+
+
+def easgd_distill(logits, indices, values, temperature: float = 1.0, teacher_lse=None, labels=None, hard: float = 0.0,
+                  scale: float = 1.0, loss=None, dlogits=None, workspace=None, stream=None):
+    """Loss and gradient of distillation in one call: easgd_distill_loss, and the gradient of scale * sum(loss)."""
+    rows, V, k, args = _distill_args(logits, indices, values, temperature, teacher_lse, labels, hard)
+    if loss is None:
+        loss = _new((rows,), torch.float32, logits, stream)
+    _on_device_of(logits, loss=loss)
+    dlogits, dptr, dld = _gradient_rows(logits, dlogits, rows, V, stream)
+    _ws, ws, nbytes = _scratch(easgd_distill_workspace_bytes(rows, V, k), workspace, logits, stream)
+    _check(_lib.easgd_distill(*args, scale, _row_vector("loss", loss, torch.float32, rows), dptr, dld, ws, nbytes, _stream(stream)))
+    return loss, dlogits
+
+
+def easgd_sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None, logprob=None,
+                        workspace=None, stream=None):
+    """One token of every row of logits [rows][V], drawn with the random numbers u [rows] in [0, 1); temperature, top_p,
+    min_p (fp32) and top_k (int32) are [rows] tensors on the GPU or None.  Returns tokens [rows] int32 (-1: every logit
+    masked) and the logarithm of the probability with which each was drawn."""
+    ptr, code, rows, V, ld = _logit_rows("logits", logits)
+    if u is None:
+        raise TypeError("u must be a CUDA/HIP tensor")
+    if tokens is None:
+        tokens = _new((rows,), torch.int32, logits, stream)
+    if logprob is None:
+        logprob = _new((rows,), torch.float32, logits, stream)
+    _on_device_of(logits, u=u, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, tokens=tokens, logprob=logprob)
+    _ws, ws, nbytes = _scratch(easgd_sample_tokens_workspace_bytes(rows, V), workspace, logits, stream)
+    _check(_lib.easgd_sample_tokens(ptr, code, rows, V, ld, _row_vector("u", u, torch.float32, rows),
+                                    _row_vector("temperature", temperature, torch.float32, rows), _row_vector("top_k", top_k, torch.int32, rows),
+                                    _row_vector("top_p", top_p, torch.float32, rows), _row_vector("min_p", min_p, torch.float32, rows),
+                                    _row_vector("tokens", tokens, torch.int32, rows), _row_vector("logprob", logprob, torch.float32, rows),
+                                    ws, nbytes, _stream(stream)))
+    return tokens, logprob
 
 
 def stream_copy(dst, src, stream=None) -> None:
