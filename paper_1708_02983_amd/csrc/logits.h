@@ -125,6 +125,11 @@ template <int DT> struct Row {
         if constexpr (VEC == 4) return make_uint4(e[0], e[1], e[2], e[3]);
         else return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4 % VEC] | e[5 % VEC] << 16, e[6 % VEC] | e[7 % VEC] << 16);
     }
+    __device__ static __forceinline__ uint4 empty()
+    {
+        constexpr unsigned two = VEC == 4 ? Type::NEG_INF : Type::NEG_INF << 16 | Type::NEG_INF;
+        return make_uint4(two, two, two, two);
+    }
     // index of the element at place i of slot s
     __device__ __forceinline__ int index(int s, int i) const { return s * VEC + i - shift; }
 };
@@ -169,13 +174,14 @@ __device__ __forceinline__ float wave_max(float v)
 template <int BLOCK, typename T> __device__ __forceinline__ T block_sum(T v, T *scratch)
 {
     constexpr int WAVES = BLOCK / 64;
+    static_assert((WAVES & (WAVES - 1)) == 0, "the wavefronts' values are joined in a tree");
     v = wave_sum(v);
     if constexpr (WAVES > 1) {
         if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
         __syncthreads();
-        v = scratch[0];
+        v = scratch[threadIdx.x & (WAVES - 1)];         // one load and a tree: registers are scarce where rows are held in them
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) v += scratch[w];
+        for (int o = WAVES / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
         __syncthreads();
     }
     return v;
@@ -187,9 +193,9 @@ template <int BLOCK> __device__ __forceinline__ float block_max(float v, float *
     if constexpr (WAVES > 1) {
         if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
         __syncthreads();
-        v = scratch[0];
+        v = scratch[threadIdx.x & (WAVES - 1)];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) v = fmaxf(v, scratch[w]);
+        for (int o = WAVES / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
         __syncthreads();
     }
     return v;
