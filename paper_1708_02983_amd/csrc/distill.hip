@@ -23,6 +23,7 @@ struct DistillArgs {
     float scale;
     void *dlogits;
     size_t dld;
+    size_t rows;
     float4 *partial;          // [rows][segments]: (m, ST, S1, SO) of a part of a row
     int segments, seg_slots;  // slots of a part of a row
 };
@@ -30,82 +31,105 @@ struct DistillArgs {
 enum { DISTILL_LOSS = 1, DISTILL_GRAD = 2, DISTILL_BOTH = 3 };
 
 // ---- exponentials of a row at both temperatures ------------------------------------------------------------------
-// h_j is a power of e_j where T is 1, 2 or 4: one or two multiplications in the place of an exponential.
-enum { HARD_NONE = 0, HARD_SAME = 1, HARD_SQUARE = 2, HARD_FOURTH = 3, HARD_EXP = 4 };
+// Where h_j comes from: nobody asks for it, or T is 1 and it is e_j; T is 2 and it is e_j^2 (a multiplication in the place of an
+// exponential); an exponential of its own.
+enum { HARD_PLAIN = 0, HARD_SQUARE = 1, HARD_EXP = 2 };
+
+__device__ __forceinline__ float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
 
 struct Scales {
     float c, c1;              // log2(e) / T, log2(e)
-    float margin;             // logits this far above the reference make exponentials of 2^24 at most
-    int hard;                 // where h_j comes from; HARD_NONE: nobody asks for it
-    __device__ __forceinline__ Scales(const DistillArgs &a)
-    {
-        c = (float)(LOG2E / (double)a.temperature);
-        c1 = (float)LOG2E;
-        margin = 24.f / fmaxf(c, c1);
-        hard = !(a.hard > 0.f) ? HARD_NONE : a.temperature == 1.f ? HARD_SAME : a.temperature == 2.f ? HARD_SQUARE :
-               a.temperature == 4.f ? HARD_FOURTH : HARD_EXP;
-    }
-    __device__ __forceinline__ float soft(float d) const { return exp2_fast(d * c); }
+    __device__ __forceinline__ Scales(const DistillArgs &a) : c((float)(LOG2E / (double)a.temperature)), c1((float)LOG2E) {}
 };
 
-// Running sums of a thread, relative to a reference near the maximum that its wavefront shares: it is moved only when
-// a logit exceeds it by 24 binary orders of magnitude (sums of 2^20 such terms are far from fp32's end), so that the
-// loop over a row has one comparison for it instead of a rescaling per 128 bits.
-template <int VEC, bool TAIL> struct RowSums {
-    float ref = -INFINITY, top = -INFINITY, st = 0.f, s1 = 0.f, so = 0.f;
+// Exponentials relative to a logit `ref`: 2^((x - ref) c) in one fused multiply-add and one exponential, as 2^(x c - rc) with
+// rc = ref * c rounded once for all; what that rounding takes from every exponent alike, `lost`, is known exactly and goes
+// into the row's factors.  Where ref is so large that ref * c might overflow (rows of fp32's lowest value), every
+// other logit is at least one unit of 2^-23 ref away and its exponential 0 or infinite at any scale: a power of two, exact, does.
+struct Reference {
+    float ref, c, c1, rc, rc1, lost, lost1;
+    __device__ __forceinline__ Reference(const Scales &q) : ref(-INFINITY), c(q.c), c1(q.c1), rc(0.f), rc1(0.f), lost(0.f), lost1(0.f) {}
+    __device__ __forceinline__ Reference(float r, const Scales &q) { set(r, q); }
+    __device__ __forceinline__ void set(float r, const Scales &q)
+    {
+        const bool huge = fabsf(r) * fmaxf(q.c, q.c1) >= 0x1p100f;
+        ref = r;
+        c = huge ? 0x1p-40f : q.c;
+        c1 = huge ? 0x1p-40f : q.c1;
+        rc = r * c;
+        rc1 = r * c1;
+        lost = fmaf(r, c, -rc);                        // the exponents are this much too large
+        lost1 = fmaf(r, c1, -rc1);
+    }
+    __device__ __forceinline__ float soft(float x) const { return exp2_fast(fmaf(x, c, -rc)); }
+    __device__ __forceinline__ float hard(float x) const { return exp2_fast(fmaf(x, c1, -rc1)); }
+};
 
+// Running sums of a thread, relative to a reference that its wavefront shares: the largest logit of the first slots that
+// hold any, moved only when a slot's exponentials sum up to more than 2^24 (sums of 2^20 such terms are far from fp32's end),
+// so that the loop over a row needs neither a maximum nor a rescaling, only a comparison per 128 bits.
+template <int VEC, bool TAIL, int HARD> struct RowSums {
+    const Scales &q;
+    Reference at;
+    float st = 0.f, s1 = 0.f, so = 0.f;
+
+    __device__ __forceinline__ RowSums(const Scales &q) : q(q), at(q) {}
     // Whole wavefronts call it (lanes without a slot with an empty one).  skip: a bit for every element that is one of the
     // teacher's places.
-    __device__ __forceinline__ void add(const float (&x)[VEC], unsigned skip, const Scales &q)
+    __device__ __forceinline__ void add(const float (&x)[VEC], unsigned skip)
     {
-        float t = x[0];
+        float e[VEC], sum, h;
+        for (;;) {
 #pragma unroll
-        for (int i = 1; i < VEC; ++i) t = fmaxf(t, x[i]);
-        top = fmaxf(top, t);
-        if (__any(t > ref + q.margin)) {                // uniform for the wavefront
-            const float up = fmaxf(ref, wave_max(t));
-            const float f = ref == -INFINITY ? 0.f : q.soft(ref - up);
+            for (int i = 0; i < VEC; ++i) e[i] = at.soft(x[i]);
+            sum = e[0];
+#pragma unroll
+            for (int i = 1; i < VEC; ++i) sum += e[i];
+            bool high = !(sum <= 0x1p24f);              // NaN among them
+            if constexpr (HARD == HARD_EXP) {
+                h = at.hard(x[0]);
+#pragma unroll
+                for (int i = 1; i < VEC; ++i) h += at.hard(x[i]);
+                high = high || !(h <= 0x1p24f);
+            }
+            if (at.ref > -INFINITY && !__any(high)) break;      // uniform for the wavefront, and nearly always
+            float t = x[0];
+#pragma unroll
+            for (int i = 1; i < VEC; ++i) t = fmaxf(t, x[i]);
+            t = uniform(wave_max(t));
+            if (!(t > at.ref)) break;
+            const Reference old = at;
+            at.set(t, q);
+            const float f = change(old, at, q.c, old.lost, at.lost), f1 = change(old, at, q.c1, old.lost1, at.lost1);
             st *= f;
             so *= f;
-            s1 *= ref == -INFINITY ? 0.f : exp2_fast((ref - up) * q.c1);
-            ref = up;
+            s1 *= f1;
         }
-        const float m = ref == -INFINITY ? 0.f : ref;   // nothing but -inf so far: every exponential is 0
-        float e[VEC];
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) e[i] = q.soft(x[i] - m);
-        float sum = e[0];
-#pragma unroll
-        for (int i = 1; i < VEC; ++i) sum += e[i];
         st += sum;
+        if constexpr (HARD == HARD_EXP) s1 += h;
+        if constexpr (HARD == HARD_SQUARE) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) s1 = fmaf(e[i], e[i], s1);
+        }
         if constexpr (TAIL) {
             if (skip) {
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) so += (skip >> i & 1) ? 0.f : e[i];
             } else so += sum;
         }
-        if (q.hard >= HARD_SQUARE) {                    // uniform
-            if (q.hard == HARD_EXP) {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) s1 += exp2_fast((x[i] - m) * q.c1);
-            } else {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    const float e2 = e[i] * e[i];
-                    s1 = q.hard == HARD_SQUARE ? s1 + e2 : fmaf(e2, e2, s1);
-                }
-            }
-        }
     }
-    // the sums of the threads of a block relative to the maximum, in a fixed order; part: one float4 per wavefront
-    template <int BLOCK> __device__ __forceinline__ float4 combine(const Scales &q, float4 *part)
+    // what sums relative to `old` are multiplied with to be relative to `now`
+    __device__ static __forceinline__ float change(const Reference &old, const Reference &now, float c, float old_lost, float now_lost)
+    {
+        return old.ref == -INFINITY ? 1.f : exp2_fast((old.ref - now.ref) * c - old_lost + now_lost);
+    }
+    // the sums of the threads of a block relative to their largest reference, in a fixed order; part: one float4 per wavefront
+    template <int BLOCK> __device__ __forceinline__ float4 combine(float4 *part)
     {
         constexpr int WAVES = BLOCK / 64;
-        const float m = wave_max(top);
-        const float f = m == -INFINITY ? 1.f : ref == -INFINITY ? 0.f : q.soft(ref - m);
-        const float f1 = m == -INFINITY ? 1.f : ref == -INFINITY ? 0.f : exp2_fast((ref - m) * q.c1);
-        float4 w = make_float4(m, wave_sum(st) * f, wave_sum(s1) * f1, wave_sum(so) * f);
-        if constexpr (WAVES == 1) return w;
+        const float f = exp2_fast(-at.lost), f1 = exp2_fast(-at.lost1);
+        float4 w = make_float4(at.ref, wave_sum(st) * f, wave_sum(s1) * f1, wave_sum(so) * f);
+        static_assert(WAVES > 1, "part is used");
         if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = w;
         __syncthreads();
         w = part[threadIdx.x & (WAVES - 1)];
@@ -120,13 +144,14 @@ template <int VEC, bool TAIL> struct RowSums {
             all.z += __shfl_xor(all.z, o);
             all.w += __shfl_xor(all.w, o);
         }
+        if constexpr (HARD == HARD_PLAIN) all.z = all.y;
         return all;
     }
-    // adds the sums of a part, relative to its own maximum, to those relative to w.x, which is at least as large
+    // adds the sums of a part, relative to its own reference, to those relative to w.x, which is at least as large
     __device__ static __forceinline__ void join(float4 &w, const float4 &p, const Scales &q)
     {
-        const float d = p.x == w.x || w.x == -INFINITY ? 0.f : p.x - w.x;
-        const float f = q.soft(d);
+        const float d = p.x == w.x || p.x == -INFINITY ? 0.f : p.x - w.x;      // a part of masked places has sums of 0
+        const float f = exp2_fast(d * q.c);
         w.y += p.y * f;
         w.z += p.z * exp2_fast(d * q.c1);
         w.w += p.w * f;
@@ -143,22 +168,30 @@ struct TeacherLds {
     float fpart[16];
 };
 
-// Slot i goes through thread i; returns its place.
+// Slot i goes through thread i.
+struct Slot {
+    int place = -1;            // -1: not used
+    float value = 0.f;
+    __device__ __forceinline__ void load(const DistillArgs &a, size_t r)
+    {
+        place = -1;
+        if ((int)threadIdx.x < a.k) {
+            place = a.indices[r * a.k + threadIdx.x];
+            value = a.values[r * a.k + threadIdx.x];
+        }
+    }
+};
+
+// The row's slots and their probabilities into LDS; returns the place of the thread's slot.
 template <int BLOCK, bool TAIL>
-__device__ __forceinline__ int read_teacher(const DistillArgs &a, size_t r, TeacherLds &lds)
+__device__ __forceinline__ int read_teacher(const DistillArgs &a, size_t r, const Slot &slot, TeacherLds &lds)
 {
     static_assert(BLOCK >= LOGITS_MAX_TOP, "one thread per slot of the teacher");
     const int tid = threadIdx.x;
     const double T = (double)a.temperature;
-    int place = -1;
-    double logit = -INFINITY;
-    if (tid < a.k) {
-        place = a.indices[r * a.k + tid];
-        const float v = a.values[r * a.k + tid];
-        if ((unsigned)place >= (unsigned)a.V) place = -1;
-        else logit = (double)v / T;
-        lds.index[tid] = place;
-    }
+    const int place = (unsigned)slot.place < (unsigned)a.V ? slot.place : -1;
+    const double logit = place >= 0 ? (double)slot.value / T : -(double)INFINITY;
+    if (tid < a.k) lds.index[tid] = place;
     double lse;
     if constexpr (TAIL) lse = (double)a.teacher_lse[r];
     else {
@@ -234,44 +267,29 @@ struct Factors {
         outside = rest > 0.0 ? cover - rest * (double)s.y / (double)s.w : cover;
     }
 };
-__device__ __forceinline__ float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
 struct Slope {
-    float fq, f1, m;
+    float fq, f1;
+    Reference at;
     bool none;                 // nothing to learn: the gradient is 0
-    __device__ __forceinline__ Slope(const DistillArgs &a, size_t r, const TeacherLds &teacher, bool padding, const float4 &s)
+    __device__ __forceinline__ Slope(const DistillArgs &a, size_t r, const TeacherLds &teacher, bool padding, const float4 &s, const Scales &q)
+        : at(uniform(s.x), q)
     {
         none = padding || uniform(s.y) == 0.f;
         const Factors f(a, r, teacher, s);
-        fq = uniform((float)(f.soft * f.outside / (double)s.y));
-        f1 = a.hard > 0.f ? uniform((float)(f.up_hard / (double)s.z)) : 0.f;
-        m = uniform(s.x);
+        fq = uniform((float)(f.soft * f.outside / (double)s.y) * exp2_fast(-at.lost));
+        f1 = a.hard > 0.f ? uniform((float)(f.up_hard / (double)s.z) * exp2_fast(-at.lost1)) : 0.f;
     }
-};
-
-template <int VEC> __device__ __forceinline__ void slope_of(float (&x)[VEC], const Slope &g, const Scales &q)
-{
-    if (g.none) {                                      // uniform
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) x[i] = 0.f;
-        return;
-    }
-    if (q.hard == HARD_EXP) {
+    template <int HARD, int VEC> __device__ __forceinline__ void of(float (&x)[VEC]) const
+    {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            const float d = x[i] - g.m;
-            x[i] = fmaf(g.f1, exp2_fast(d * q.c1), g.fq * q.soft(d));
+            const float e = at.soft(x[i]);
+            if constexpr (HARD == HARD_PLAIN) x[i] = (fq + f1) * e;          // h = e
+            else if constexpr (HARD == HARD_SQUARE) x[i] = e * fmaf(f1, e, fq);
+            else x[i] = fmaf(f1, at.hard(x[i]), fq * e);
         }
-        return;
     }
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-        const float e = q.soft(x[i] - g.m);
-        if (q.hard == HARD_NONE) x[i] = g.fq * e;
-        else if (q.hard == HARD_SAME) x[i] = (g.fq + g.f1) * e;
-        else if (q.hard == HARD_SQUARE) x[i] = e * fmaf(g.f1, e, g.fq);
-        else x[i] = e * fmaf(g.f1, e * (e * e), g.fq);
-    }
-}
+};
 
 // The rows of the gradient, which may start at another alignment than the logits': whole slots where both agree (the
 // usual case: SAME), else element by element.
@@ -294,7 +312,10 @@ template <int DT> struct GradRow {
     {
         const int j = s * VEC - shift;
         if (same && full) {
-            *reinterpret_cast<uint4 *>(row + j) = Type::pack(x);
+            typedef unsigned Four __attribute__((ext_vector_type(4)));
+            const uint4 p = Type::pack(x);
+            const Four v = {p.x, p.y, p.z, p.w};
+            __builtin_nontemporal_store(v, reinterpret_cast<Four *>(row + j));
             return;
         }
 #pragma unroll
@@ -302,13 +323,19 @@ template <int DT> struct GradRow {
             if ((unsigned)(j + i) < (unsigned)V) row[j + i] = Type::narrow(x[i]);
     }
     __device__ __forceinline__ void put(int j, float d) const { row[j] = Type::narrow(d); }
+    // 0 for slots first + thread, first + thread + block, ... below last
+    __device__ __forceinline__ void clear(int last, int block, int first = 0) const
+    {
+        const float zero[VEC] = {};
+        for (int s = first + threadIdx.x; s < last; s += block) store(s, zero, s * VEC >= shift && (s + 1) * VEC <= shift + V);
+    }
 };
 
 // The places that the teacher or the label names, within elements [j0, j1) (j0 may lie before the row): each once, by the
 // first slot that names it, after a barrier behind the stores of all others.
 template <int DT>
-__device__ __forceinline__ void name_places(const DistillArgs &a, size_t r, const Row<DT> &row, const GradRow<DT> &out, int place, int label,
-                                            const float4 &s, const TeacherLds &lds, int j0, int j1)
+__device__ __forceinline__ void name_places(const DistillArgs &a, size_t r, const GradRow<DT> &out, int place, float z_place, int label,
+                                            float z_label, const float4 &s, const TeacherLds &lds, int j0, int j1)
 {
     const bool labelled = a.hard > 0.f;
     int at = -1;
@@ -322,8 +349,8 @@ __device__ __forceinline__ void name_places(const DistillArgs &a, size_t r, cons
         }
     }
     const Factors f(a, r, lds, s);
-    auto name = [&](int j, bool top, double goal) {
-        const double x = (double)row.load_one(j) - (double)s.x;
+    auto name = [&](int j, float z, bool top, double goal) {
+        const double x = (double)z - (double)s.x;
         double d = f.soft * ((top ? f.cover : f.outside) * exp(x / (double)a.temperature) / (double)s.y - goal);
         if (f.up_hard != 0.0) d += f.up_hard * (exp(x) / (double)s.z - (labelled && j == label ? 1.0 : 0.0));
         out.put(j, (float)d);
@@ -334,18 +361,18 @@ __device__ __forceinline__ void name_places(const DistillArgs &a, size_t r, cons
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {
         const int j = turn == 0 ? at : alone ? label : -1;
-        if (j >= 0) name(j, turn == 0, target);
+        if (j >= 0) name(j, turn == 0 ? z_place : z_label, turn == 0, target);
         target = 0.0;
     }
 }
 
 // ---- loss, and gradient with GRAD, of whole rows, a block each -----------------------------------------------------
-// The first NV * BLOCK slots of a row are requested at once and stay in registers between the two passes over it, so
-// that up to 256 KB of a row are read once; what is longer is read again.
-template <int DT, int BLOCK, int NV, bool TAIL, bool GRAD>
-__global__ __launch_bounds__(BLOCK) void distill_rows_kernel(DistillArgs a)
+// The first NV * BLOCK slots of a row are requested at once and stay in registers between the two passes over it; what is
+// longer is read again, from the last-level cache while no more rows are under way than it holds.
+template <int DT, int BLOCK, int NV, bool TAIL, int HARD, bool GRAD>
+__global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
 {
-    constexpr int VEC = Row<DT>::VEC;
+    constexpr int VEC = Row<DT>::VEC, DEEP = 4;
     using Type = LogitType<DT>;
     extern __shared__ unsigned in_top[];
     __shared__ TeacherLds lds;
@@ -356,13 +383,14 @@ __global__ __launch_bounds__(BLOCK) void distill_rows_kernel(DistillArgs a)
     const Scales q(a);
     const int label = a.labels ? a.labels[r] : 0;
     const bool padding = (unsigned)label >= (unsigned)a.V;
+    Slot slot;
+    slot.load(a, r);
 
     // full slots [f0, f1): thread t has f0 + t + i * BLOCK; threads 0 and 1 have the partial slots at the row's ends.  Loops run
-    // for whole wavefronts (first is the wavefront's first slot); lanes behind the end hold empty slots.
+    // for whole wavefronts (those whose first slot is there); lanes behind the end hold empty slots.
     const int f0 = row.first_full(), f1 = row.end_full();
     const int first = f0 + __builtin_amdgcn_readfirstlane(tid & ~63);
-    uint4 v[NV];
-    uint4 edge = make_uint4(0, 0, 0, 0);
+    uint4 v[NV], edge = Row<DT>::empty();
     int edge_slot = -1;
     if (tid == 0 && row.shift) edge_slot = 0;
     if (tid == 1 && row.slots > f1 && (row.slots > 1 || !row.shift)) edge_slot = row.slots - 1;
@@ -370,63 +398,75 @@ __global__ __launch_bounds__(BLOCK) void distill_rows_kernel(DistillArgs a)
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int s = f0 + tid + i * BLOCK;
-            if (first + i * BLOCK < f1) v[i] = s < f1 ? row.load_full(s) : Row<DT>::empty();
+            if (first + i * BLOCK < f1) v[i] = s < f1 ? row.load_once(s) : Row<DT>::empty();
         }
         if (edge_slot >= 0) edge = row.load(edge_slot);
     }
-    const int place = read_teacher<BLOCK, TAIL>(a, r, lds);
+    const int place = read_teacher<BLOCK, TAIL>(a, r, slot, lds);
     float4 sums = make_float4(0.f, 0.f, 0.f, 0.f);
     float z_place = 0.f, z_label = 0.f;
     if (!padding) {                                     // uniform
         if (place >= 0) z_place = row.load_one(place);
-        if (tid == 0) z_label = row.load_one(label);
+        z_label = row.load_one(label);
         if constexpr (TAIL) mark_places(in_top, (row.slots * VEC + 31) / 32, 0, place, row.shift, BLOCK);
-        RowSums<VEC, TAIL> acc;
+        RowSums<VEC, TAIL, HARD> acc(q);
         auto add = [&](const uint4 &raw, int s) {
             float x[VEC];
             Type::unpack(raw, x);
-            acc.add(x, TAIL ? marks_of<VEC>(in_top, s) : 0u, q);
+            acc.add(x, TAIL ? marks_of<VEC>(in_top, s) : 0u);
         };
-        if (tid < 64 && __any(edge_slot >= 0)) {        // the first wavefront; lanes without an edge add -inf
-            if (edge_slot < 0) edge = Row<DT>::empty();
-            add(edge, edge_slot < 0 ? 0 : edge_slot);
-        }
+        if (tid < 64) add(edge, max(edge_slot, 0));
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
+        for (int i = 0; i < NV; ++i)
             if (first + i * BLOCK < f1) add(v[i], min(f0 + tid + i * BLOCK, f1 - 1));
-        }
-        for (int i = NV; first + i * BLOCK < f1; ++i) {
-            const int s = f0 + tid + i * BLOCK;
-            add(s < f1 ? row.load_full(s) : Row<DT>::empty(), min(s, f1 - 1));
-        }
-        sums = acc.template combine<BLOCK>(q, part);
-        if (q.hard == HARD_SAME) sums.z = sums.y;
-    }
-    if constexpr (!GRAD) {
-        write_loss<BLOCK>(a, r, place, z_place, z_label, padding, sums, lds);
-        return;
-    }
-    const GradRow<DT> out(a, r, row);
-    const Slope g(a, r, lds, padding, sums);
-    auto put = [&](const uint4 &raw, int s, bool full) {
-        float x[VEC];
-        Type::unpack(raw, x);
-        slope_of<VEC>(x, g, q);
-        out.store(s, x, full);
-    };
-    if (edge_slot >= 0) put(edge, edge_slot, false);
+        for (int i0 = NV; first + i0 * BLOCK < f1; i0 += DEEP) {
+            uint4 w[DEEP];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int s = f0 + tid + i * BLOCK;
-        if (s < f1) put(v[i], s, true);
+            for (int i = 0; i < DEEP; ++i) {
+                const int s = f0 + tid + (i0 + i) * BLOCK;
+                w[i] = s < f1 ? row.load_full(s) : Row<DT>::empty();
+            }
+#pragma unroll
+            for (int i = 0; i < DEEP; ++i)
+                if (first + (i0 + i) * BLOCK < f1) add(w[i], min(f0 + tid + (i0 + i) * BLOCK, f1 - 1));
+        }
+        sums = acc.template combine<BLOCK>(part);
     }
-    for (int s = f0 + tid + NV * BLOCK; s < f1; s += BLOCK) put(g.none ? make_uint4(0, 0, 0, 0) : row.load_full(s), s, true);
-    write_loss<BLOCK>(a, r, place, z_place, z_label, padding, sums, lds);       // its barriers stand between the stores above and below
-    if (!g.none) name_places<DT>(a, r, row, out, place, label, sums, lds, 0, a.V);
+    if constexpr (GRAD) {
+        const GradRow<DT> out(a, r, row);
+        const Slope g(a, r, lds, padding, sums, q);
+        auto put = [&](const uint4 &raw, int s, bool full) {
+            float x[VEC];
+            Type::unpack(raw, x);
+            g.template of<HARD, VEC>(x);
+            out.store(s, x, full);
+        };
+        if (g.none) {                                   // uniform
+            out.clear(row.slots, BLOCK);
+        } else {
+            for (int s0 = f0 + tid + NV * BLOCK; s0 < f1; s0 += DEEP * BLOCK) {
+                uint4 w[DEEP];
+#pragma unroll
+                for (int i = 0; i < DEEP; ++i)
+                    if (s0 + i * BLOCK < f1) w[i] = row.load_full(s0 + i * BLOCK);
+#pragma unroll
+                for (int i = 0; i < DEEP; ++i)
+                    if (s0 + i * BLOCK < f1) put(w[i], s0 + i * BLOCK, true);
+            }
+            if (edge_slot >= 0) put(edge, edge_slot, false);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (f0 + tid + i * BLOCK < f1) put(v[i], f0 + tid + i * BLOCK, true);
+        }
+        write_loss<BLOCK>(a, r, place, z_place, z_label, padding, sums, lds);       // its barriers stand between the stores above and below
+        if (!g.none) name_places<DT>(a, r, out, place, z_place, label, z_label, sums, lds, 0, a.V);
+    } else {
+        write_loss<BLOCK>(a, r, place, z_place, z_label, padding, sums, lds);
+    }
 }
 
 // ---- few rows: sums of parts of rows ----------------------------------------------------------------------------------
-template <int DT, int BLOCK, bool TAIL>
+template <int DT, int BLOCK, bool TAIL, int HARD>
 __global__ __launch_bounds__(BLOCK) void distill_sums_kernel(DistillArgs a)
 {
     constexpr int VEC = Row<DT>::VEC, DEEP = 4;
@@ -446,11 +486,11 @@ __global__ __launch_bounds__(BLOCK) void distill_sums_kernel(DistillArgs a)
         if ((unsigned)place >= (unsigned)a.V) place = -1;
         mark_places(in_top, (a.seg_slots * VEC + 31) / 32, s0 * VEC, place, row.shift, BLOCK);
     }
-    RowSums<VEC, TAIL> acc;
+    RowSums<VEC, TAIL, HARD> acc(q);
     auto add = [&](const uint4 &raw, int s) {
         float x[VEC];
         Type::unpack(raw, x);
-        acc.add(x, TAIL ? marks_of<VEC>(in_top, s - s0) : 0u, q);
+        acc.add(x, TAIL ? marks_of<VEC>(in_top, s - s0) : 0u);
     };
     const int lead = __builtin_amdgcn_readfirstlane(tid & ~63);
     int s = s0 + tid;
@@ -462,8 +502,7 @@ __global__ __launch_bounds__(BLOCK) void distill_sums_kernel(DistillArgs a)
         for (int i = 0; i < DEEP; ++i) add(v[i], s + i * BLOCK);
     }
     for (; s - tid + lead < s1; s += BLOCK) add(s < s1 ? row.load(s) : Row<DT>::empty(), min(s, s1 - 1));      // whole wavefronts
-    float4 sums = acc.template combine<BLOCK>(q, part);
-    if (q.hard == HARD_SAME) sums.z = sums.y;
+    const float4 sums = acc.template combine<BLOCK>(part);
     if (tid == 0) a.partial[r * a.segments + seg] = sums;
 }
 
@@ -477,7 +516,9 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a)
     const Scales q(a);
     const int label = a.labels ? a.labels[r] : 0;
     const bool padding = (unsigned)label >= (unsigned)a.V;
-    const int place = read_teacher<256, TAIL>(a, r, lds);
+    Slot slot;
+    slot.load(a, r);
+    const int place = read_teacher<256, TAIL>(a, r, slot, lds);
     float4 sums = make_float4(0.f, 0.f, 0.f, 0.f);
     float z_place = 0.f, z_label = 0.f;
     if (!padding) {
@@ -485,13 +526,13 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a)
         if (threadIdx.x == 0) z_label = row.load_one(label);
         sums.x = -INFINITY;
         for (int i = 0; i < a.segments; ++i) sums.x = fmaxf(sums.x, a.partial[r * a.segments + i].x);
-        for (int i = 0; i < a.segments; ++i) RowSums<4, TAIL>::join(sums, a.partial[r * a.segments + i], q);
+        for (int i = 0; i < a.segments; ++i) RowSums<4, TAIL, HARD_EXP>::join(sums, a.partial[r * a.segments + i], q);
     }
     write_loss<256>(a, r, place, z_place, z_label, padding, sums, lds);
 }
 
 // ---- backward: gradients of parts of rows ----------------------------------------------------------------------------
-template <int DT, int BLOCK, bool TAIL>
+template <int DT, int BLOCK, bool TAIL, int HARD>
 __global__ __launch_bounds__(BLOCK) void distill_grad_kernel(DistillArgs a)
 {
     constexpr int VEC = Row<DT>::VEC, DEEP = 4;
@@ -505,31 +546,34 @@ __global__ __launch_bounds__(BLOCK) void distill_grad_kernel(DistillArgs a)
     const int label = a.labels ? a.labels[r] : 0;
     const bool padding = (unsigned)label >= (unsigned)a.V;
     const int s0 = seg * a.seg_slots, s1 = min(s0 + a.seg_slots, row.slots);
-    const int place = read_teacher<BLOCK, TAIL>(a, r, lds);
+    Slot slot;
+    slot.load(a, r);
+    const int place = read_teacher<BLOCK, TAIL>(a, r, slot, lds);
     const float4 sums = reinterpret_cast<const float4 *>(a.state)[r];
-    const Slope g(a, r, lds, padding, sums);
+    const Slope g(a, r, lds, padding, sums, q);
     const GradRow<DT> out(a, r, row);
     auto put = [&](const uint4 &raw, int s) {
         float x[VEC];
         Type::unpack(raw, x);
-        slope_of<VEC>(x, g, q);
+        g.template of<HARD, VEC>(x);
         out.store(s, x, row.full(s));
     };
     int s = s0 + tid;
     if (g.none) {
-        for (; s < s1; s += BLOCK) put(make_uint4(0, 0, 0, 0), s);
+        out.clear(s1, BLOCK, s0);
         return;
     }
+    const float z_place = place >= 0 ? row.load_one(place) : 0.f, z_label = row.load_one(label);
     for (; s - tid + DEEP * BLOCK <= s1; s += DEEP * BLOCK) {
         uint4 v[DEEP];
 #pragma unroll
-        for (int i = 0; i < DEEP; ++i) v[i] = row.load(s + i * BLOCK);
+        for (int i = 0; i < DEEP; ++i) v[i] = row.full(s + i * BLOCK) ? row.load_once(s + i * BLOCK) : row.load(s + i * BLOCK);
 #pragma unroll
         for (int i = 0; i < DEEP; ++i) put(v[i], s + i * BLOCK);
     }
     for (; s < s1; s += BLOCK) put(row.load(s), s);
     __syncthreads();
-    name_places<DT>(a, r, row, out, place, label, sums, lds, s0 * VEC - row.shift, s1 * VEC - row.shift);
+    name_places<DT>(a, r, out, place, z_place, label, z_label, sums, lds, s0 * VEC - row.shift, s1 * VEC - row.shift);
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------------
@@ -573,10 +617,10 @@ static int most_slots(int dtype, int V)
 }
 
 // Into how many parts rows are cut: enough blocks to fill the chip, and at least 1024 slots (four per thread) a part.
-static constexpr int SPLIT_BLOCKS = 1024, SPLIT_SLOTS = 1024;
+static constexpr int SPLIT_ROWS = 256, SPLIT_BLOCKS = 1024, SPLIT_SLOTS = 1024;
 static int segments_of(size_t rows, int slots)
 {
-    if (rows >= SPLIT_BLOCKS || slots < 2 * SPLIT_SLOTS) return 1;
+    if (rows >= SPLIT_ROWS || slots < 2 * SPLIT_SLOTS) return 1;
     const int want = (int)((SPLIT_BLOCKS + rows - 1) / rows), most = slots / SPLIT_SLOTS;
     return want < most ? want : most;
 }
@@ -586,39 +630,50 @@ static void set_segments(DistillArgs &a, int segments, int slots)
     a.seg_slots = ((slots + segments - 1) / segments + 7) / 8 * 8;      // a multiple of 8: parts of the bit map begin at whole words
 }
 
-template <int DT> static void launch_sums(DistillArgs a, size_t rows, hipStream_t s)
+// calls f with the kind of the hard exponentials and whether there is a teacher's log-sum-exp as constants
+template <typename F> static void by_kind(const DistillArgs &a, F f)
 {
-    constexpr int VEC = LogitType<DT>::VEC;
-    const size_t bits = ((size_t)a.seg_slots * VEC + 31) / 32 * 4;
-    const dim3 grid((unsigned)(rows * a.segments));
-    if (a.teacher_lse) EASGD_LAUNCH((distill_sums_kernel<DT, 256, true>), grid, dim3(256), bits, s, a);
-    else EASGD_LAUNCH((distill_sums_kernel<DT, 256, false>), grid, dim3(256), 0, s, a);
-    if (a.teacher_lse) EASGD_LAUNCH((distill_join_kernel<DT, true>), dim3((unsigned)rows), dim3(256), 0, s, a);
-    else EASGD_LAUNCH((distill_join_kernel<DT, false>), dim3((unsigned)rows), dim3(256), 0, s, a);
+    auto with = [&](auto tail) {
+        if (!(a.hard > 0.f) || a.temperature == 1.f) f(tail, std::integral_constant<int, HARD_PLAIN>{});
+        else if (a.temperature == 2.f) f(tail, std::integral_constant<int, HARD_SQUARE>{});
+        else f(tail, std::integral_constant<int, HARD_EXP>{});
+    };
+    if (a.teacher_lse) with(std::true_type{});
+    else with(std::false_type{});
 }
 
-template <int DT> static void launch_grad(DistillArgs a, size_t rows, hipStream_t s)
+template <int DT> static void launch_sums(const DistillArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)(rows * a.segments));
-    if (a.teacher_lse) EASGD_LAUNCH((distill_grad_kernel<DT, 256, true>), grid, dim3(256), 0, s, a);
-    else EASGD_LAUNCH((distill_grad_kernel<DT, 256, false>), grid, dim3(256), 0, s, a);
+    const size_t bits = a.teacher_lse ? ((size_t)a.seg_slots * LogitType<DT>::VEC + 31) / 32 * 4 : 0;
+    by_kind(a, [&](auto tail, auto hard) {
+        EASGD_LAUNCH((distill_sums_kernel<DT, 256, decltype(tail)::value, decltype(hard)::value>), dim3((unsigned)(a.rows * a.segments)), dim3(256), bits, s, a);
+    });
+    if (a.teacher_lse) EASGD_LAUNCH((distill_join_kernel<DT, true>), dim3((unsigned)a.rows), dim3(256), 0, s, a);
+    else EASGD_LAUNCH((distill_join_kernel<DT, false>), dim3((unsigned)a.rows), dim3(256), 0, s, a);
 }
 
-template <int DT, int BLOCK, int NV, bool GRAD> static void launch_block(const DistillArgs &a, size_t rows, hipStream_t s)
+template <int DT> static void launch_grad(const DistillArgs &a, hipStream_t s)
+{
+    by_kind(a, [&](auto tail, auto hard) {
+        EASGD_LAUNCH((distill_grad_kernel<DT, 256, decltype(tail)::value, decltype(hard)::value>), dim3((unsigned)(a.rows * a.segments)), dim3(256), 0, s, a);
+    });
+}
+
+template <int DT, int BLOCK, int NV, bool GRAD> static void launch_block(const DistillArgs &a, hipStream_t s)
 {
     constexpr int VEC = LogitType<DT>::VEC;
-    const size_t bits = ((size_t)a.V + VEC - 1 + 31) / 32 * 4 + 4;
-    if (a.teacher_lse) EASGD_LAUNCH((distill_rows_kernel<DT, BLOCK, NV, true, GRAD>), dim3((unsigned)rows), dim3(BLOCK), bits, s, a);
-    else EASGD_LAUNCH((distill_rows_kernel<DT, BLOCK, NV, false, GRAD>), dim3((unsigned)rows), dim3(BLOCK), 0, s, a);
+    const size_t bits = a.teacher_lse ? ((size_t)a.V + VEC - 1 + 31) / 32 * 4 + 4 : 0;
+    by_kind(a, [&](auto tail, auto hard) {
+        EASGD_LAUNCH((distill_rows_kernel<DT, BLOCK, NV, decltype(tail)::value, decltype(hard)::value, GRAD>), dim3((unsigned)a.rows), dim3(BLOCK), bits, s, a);
+    });
 }
 
 // The block's size goes by the row's length alone, so that the forward pass adds in the same order with and without the gradient.
-template <int DT, bool GRAD> static void launch_rows(const DistillArgs &a, size_t rows, int slots, hipStream_t s)
+template <int DT, bool GRAD> static void launch_rows(const DistillArgs &a, int slots, hipStream_t s)
 {
-    if (slots <= 256 * 4) launch_block<DT, 256, 4, GRAD>(a, rows, s);
-    else if (slots <= 256 * 16) launch_block<DT, 256, 16, GRAD>(a, rows, s);
-    else if (slots <= 512 * 16) launch_block<DT, 512, 16, GRAD>(a, rows, s);
-    else launch_block<DT, 1024, 16, GRAD>(a, rows, s);
+    if (slots <= 256 * 4) launch_block<DT, 256, 4, GRAD>(a, s);
+    else if (slots <= 256 * 16) launch_block<DT, 256, 12, GRAD>(a, s);
+    else launch_block<DT, 512, 8, GRAD>(a, s);
 }
 
 // Rows cut into parts: a workspace for the parts' sums, then for the states of the rows.
@@ -641,12 +696,12 @@ template <int MODE> static int launch_distill(const DistillCall &q, void *stream
     a.partial = static_cast<float4 *>(q.workspace);
     by_dtype(q.dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        if constexpr (MODE == DISTILL_GRAD) launch_grad<DT>(a, q.rows, s);
-        else if (segments == 1) launch_rows<DT, MODE == DISTILL_BOTH>(a, q.rows, slots, s);
+        if constexpr (MODE == DISTILL_GRAD) launch_grad<DT>(a, s);
+        else if (segments == 1) launch_rows<DT, MODE == DISTILL_BOTH>(a, slots, s);
         else {
             if constexpr (MODE == DISTILL_BOTH) a.state = reinterpret_cast<float *>(a.partial + q.rows * segments);
-            launch_sums<DT>(a, q.rows, s);
-            if constexpr (MODE == DISTILL_BOTH) launch_grad<DT>(a, q.rows, s);
+            launch_sums<DT>(a, s);
+            if constexpr (MODE == DISTILL_BOTH) launch_grad<DT>(a, s);
         }
     });
     return check_launch(q.name);
@@ -669,7 +724,7 @@ int easgd_distill_loss(const void *logits, int dtype, size_t rows, int V, size_t
                        void *workspace, size_t workspace_bytes, void *stream)
 {
     easgd::DistillCall q = {"easgd_distill_loss", dtype, rows, {}, workspace, workspace_bytes};
-    q.a = {logits, ld, V, k, indices, values, teacher_lse, labels, temperature, hard, loss, state, nullptr, 1.f, nullptr, 0, nullptr, 1, 0};
+    q.a = {logits, ld, V, k, indices, values, teacher_lse, labels, temperature, hard, loss, state, nullptr, 1.f, nullptr, 0, rows, nullptr, 1, 0};
     return easgd::launch_distill<easgd::DISTILL_LOSS>(q, stream);
 }
 
@@ -678,7 +733,7 @@ int easgd_distill_grad(const void *logits, int dtype, size_t rows, int V, size_t
                        const float *dloss, float scale, void *dlogits, size_t dld, void *stream)
 {
     easgd::DistillCall q = {"easgd_distill_grad", dtype, rows, {}, nullptr, 0};
-    q.a = {logits, ld, V, k, indices, values, teacher_lse, labels, temperature, hard, nullptr, const_cast<float *>(state), dloss, scale, dlogits, dld, nullptr, 1, 0};
+    q.a = {logits, ld, V, k, indices, values, teacher_lse, labels, temperature, hard, nullptr, const_cast<float *>(state), dloss, scale, dlogits, dld, rows, nullptr, 1, 0};
     return easgd::launch_distill<easgd::DISTILL_GRAD>(q, stream);
 }
 
@@ -687,7 +742,7 @@ int easgd_distill(const void *logits, int dtype, size_t rows, int V, size_t ld, 
                   void *dlogits, size_t dld, void *workspace, size_t workspace_bytes, void *stream)
 {
     easgd::DistillCall q = {"easgd_distill", dtype, rows, {}, workspace, workspace_bytes};
-    q.a = {logits, ld, V, k, indices, values, teacher_lse, labels, temperature, hard, loss, nullptr, nullptr, scale, dlogits, dld, nullptr, 1, 0};
+    q.a = {logits, ld, V, k, indices, values, teacher_lse, labels, temperature, hard, loss, nullptr, nullptr, scale, dlogits, dld, rows, nullptr, 1, 0};
     return easgd::launch_distill<easgd::DISTILL_BOTH>(q, stream);
 }
 

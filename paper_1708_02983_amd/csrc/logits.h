@@ -112,6 +112,13 @@ template <int DT> struct Row {
     __device__ __forceinline__ int end_full() const { return end / VEC; }         // full slots are [first_full, end_full)
     __device__ __forceinline__ bool full(int s) const { return s * VEC >= shift && (s + 1) * VEC <= end; }
     __device__ __forceinline__ uint4 load_full(int s) const { return reinterpret_cast<const uint4 *>(base)[s]; }
+    // for what is read once and no more by anyone soon
+    __device__ __forceinline__ uint4 load_once(int s) const
+    {
+        typedef unsigned Four __attribute__((ext_vector_type(4)));
+        const Four v = __builtin_nontemporal_load(reinterpret_cast<const Four *>(base) + s);
+        return make_uint4(v[0], v[1], v[2], v[3]);
+    }
     __device__ __forceinline__ float load_one(int j) const { return Type::widen(base[shift + j]); }
     __device__ __forceinline__ uint4 load(int s) const
     {
