@@ -24,6 +24,8 @@ struct DistillArgs {
     void *dlogits;
     size_t dld;
     size_t rows;
+    int parts;                // logits are the sum of this many matrices (fp32, short rows)
+    size_t part_stride;
     float4 *partial;          // [rows][segments]: (m, ST, S1, SO) of a part of a row
     int segments, seg_slots;  // slots of a part of a row
 };
@@ -576,6 +578,181 @@ __global__ __launch_bounds__(BLOCK) void distill_grad_kernel(DistillArgs a)
     name_places<DT>(a, r, out, place, z_place, label, z_label, sums, lds, s0 * VEC - row.shift, s1 * VEC - row.shift);
 }
 
+// ---- short rows: a wavefront each, all three calls --------------------------------------------------------------------
+// Rows of at most 64 * NQ logits sit in a wavefront's registers, element lane + 64 q in x[q]; maximum and sums are shuffles,
+// and nothing waits for other wavefronts.  LDS holds the teacher's slots and, for every element, its target (-1: not one
+// of the teacher's places).  Bound: latency (one trip to memory, two chains of 64-bit exponentials and logarithms).
+template <int DT, int NQ, bool TAIL, int MODE>
+__global__ __launch_bounds__(256) void distill_short_kernel(DistillArgs a)
+{
+    using Type = LogitType<DT>;
+    constexpr int SLOTS = LOGITS_MAX_TOP / 64;
+    __shared__ int all_index[4][LOGITS_MAX_TOP];
+    __shared__ double all_p[4][LOGITS_MAX_TOP];
+    __shared__ float all_target[4][NQ * 64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const size_t r = (size_t)blockIdx.x * 4 + wave;
+    if (r >= a.rows) return;                            // wavefronts of a block have nothing in common
+    int *index = all_index[wave];
+    double *probability = all_p[wave];
+    float *target = all_target[wave];
+    // LDS accesses of one wavefront are executed in order: only the compiler has to keep them so
+    auto in_order = []() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); };
+
+    const Row<DT> row(a.logits, r, a.ld, a.V);
+    const Scales q(a);
+    const double T = (double)a.temperature;
+    const int label = a.labels ? a.labels[r] : 0;
+    const bool padding = (unsigned)label >= (unsigned)a.V, hard = a.hard > 0.f;
+    int place[SLOTS];
+    float value[SLOTS], z_place[SLOTS], x[NQ];
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) {
+        const int i = lane + 64 * j;
+        place[j] = i < a.k ? a.indices[r * a.k + i] : -1;
+        value[j] = i < a.k ? a.values[r * a.k + i] : 0.f;
+    }
+    const float lse_given = TAIL ? a.teacher_lse[r] : 0.f;
+#pragma unroll
+    for (int c = 0; c < NQ; ++c) {
+        const int j = lane + 64 * c;
+        x[c] = -INFINITY;
+        if (j < a.V && !padding) {
+            x[c] = row.load_one(j);
+            if constexpr (DT == EASGD_F32)              // logits that come as partial sums: added in ascending order
+                for (int s = 1; s < a.parts; ++s) x[c] += row.base[row.shift + j + s * a.part_stride];
+        }
+    }
+    float z_label = 0.f;
+#pragma unroll
+    for (int c = 0; c < NQ; ++c) z_label = lane + 64 * c == label ? x[c] : z_label;
+    z_label = wave_only(z_label);
+
+    // the teacher
+    double logit[SLOTS], p[SLOTS], lse = (double)lse_given, mass = 0.0;
+    float top = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) {
+        if ((unsigned)place[j] >= (unsigned)a.V) place[j] = -1;
+        logit[j] = place[j] >= 0 ? (double)value[j] / T : -(double)INFINITY;
+        top = fmaxf(top, (float)logit[j]);
+    }
+    if constexpr (!TAIL) {
+        top = wave_max(top);
+        double total = 0.0;
+#pragma unroll
+        for (int j = 0; j < SLOTS; ++j)
+            if (64 * j < a.k && place[j] >= 0 && top > -INFINITY) total += exp(logit[j] - (double)top);
+        total = wave_sum(total);
+        lse = (double)top + log(total);
+        if (!(top > -INFINITY)) lse = isnan(total) ? (double)NAN : 0.0;
+    }
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) {
+        const int i = lane + 64 * j;
+        p[j] = 0.0;
+        if (64 * j < a.k) {
+            p[j] = place[j] >= 0 ? exp(logit[j] - lse) : 0.0;
+            if (i < a.k) {
+                index[i] = place[j];
+                probability[i] = p[j];
+            }
+        }
+        mass += p[j];
+    }
+    mass = wave_sum(mass);
+    double rest = TAIL && mass < 1.0 ? 1.0 - mass : 0.0;
+#pragma unroll
+    for (int c = 0; c < NQ; ++c) target[lane + 64 * c] = -1.f;
+    in_order();
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) {
+        if (64 * j >= a.k) break;                       // uniform
+        double sum = 0.0;
+        bool first = place[j] >= 0;
+        for (int i = 0; i < a.k; ++i) {
+            if (index[i] != place[j]) continue;
+            if (i < lane + 64 * j) first = false;
+            sum += probability[i];
+        }
+        if (first) target[place[j]] = (float)sum;
+    }
+    in_order();
+
+    // maximum and sums
+    float e[NQ], h[NQ], t[NQ];
+    float4 s;
+    if constexpr (MODE & DISTILL_LOSS) {
+        float m = x[0];
+#pragma unroll
+        for (int c = 1; c < NQ; ++c) m = fmaxf(m, x[c]);
+        s.x = wave_max(m);
+    } else s = reinterpret_cast<const float4 *>(a.state)[r];
+    const float m = s.x == -INFINITY ? 0.f : s.x;
+    float st = 0.f, s1 = 0.f, so = 0.f;
+#pragma unroll
+    for (int c = 0; c < NQ; ++c) {
+        t[c] = target[lane + 64 * c];
+        e[c] = exp2_fast((x[c] - m) * q.c);
+        h[c] = !hard ? 0.f : a.temperature == 1.f ? e[c] : exp2_fast((x[c] - m) * q.c1);
+        st += e[c];
+        s1 += h[c];
+        so += t[c] >= 0.f ? 0.f : e[c];
+    }
+    if constexpr (MODE & DISTILL_LOSS) {
+        s.y = wave_sum(st);
+        s.z = hard ? wave_sum(s1) : 0.f;
+        s.w = TAIL ? wave_sum(so) : 0.f;
+    }
+    const bool none = padding || s.y == 0.f;
+    if (!(s.w > 0.f)) rest = 0.0;
+
+    if constexpr (MODE & DISTILL_LOSS) {
+        const double log_st = log((double)s.y);
+        double kl = 0.0;
+#pragma unroll
+        for (int j = 0; j < SLOTS; ++j) {
+            if (64 * j >= a.k) break;
+            z_place[j] = 0.f;
+            if (!none && place[j] >= 0) {
+                z_place[j] = row.load_one(place[j]);
+                if constexpr (DT == EASGD_F32)
+                    for (int u = 1; u < a.parts; ++u) z_place[j] += row.base[row.shift + place[j] + u * a.part_stride];
+            }
+            if (!none && p[j] > 0.0) kl += p[j] * (logit[j] - lse - (((double)z_place[j] - (double)s.x) / T - log_st));
+            if (isnan(p[j])) kl += p[j];
+        }
+        kl = wave_sum(kl);
+        if (lane == 0) {
+            if (rest > 0.0) kl += rest * (log(rest) - log((double)s.w) + log_st);
+            double loss = 0.0;
+            if (!none) {
+                if (a.hard < 1.f) loss = (1.0 - (double)a.hard) * T * T * kl;
+                if (hard) loss += (double)a.hard * (((double)s.x - (double)z_label) + log((double)s.z));
+                if (isnan(s.y)) loss = NAN;
+            }
+            a.loss[r] = (float)loss;
+            if (a.state) reinterpret_cast<float4 *>(a.state)[r] = padding ? make_float4(0.f, 0.f, 0.f, 0.f) : s;
+        }
+    }
+    if constexpr (MODE & DISTILL_GRAD) {
+        const double up = (double)a.scale * (a.dloss ? (double)a.dloss[r] : 1.0), soft = up * (1.0 - (double)a.hard) * T;
+        const double cover = mass + rest, outside = rest > 0.0 ? cover - rest * (double)s.y / (double)s.w : cover;
+        const float f_in = (float)(soft * cover / (double)s.y), f_out = (float)(soft * outside / (double)s.y), f_t = (float)soft;
+        const float f1 = hard ? (float)(up * (double)a.hard / (double)s.z) : 0.f, f_y = (float)(up * (double)a.hard);
+        const Row<DT> out(a.dlogits, r, a.dld, a.V);
+#pragma unroll
+        for (int c = 0; c < NQ; ++c) {
+            const int j = lane + 64 * c;
+            const bool in = t[c] >= 0.f;
+            float d = fmaf(f1, h[c], (in ? f_in : f_out) * e[c]);
+            if (in) d = fmaf(-f_t, t[c], d);
+            if (hard && j == label) d -= f_y;
+            if (j < a.V) out.base[out.shift + j] = Type::narrow(none ? 0.f : d);
+        }
+    }
+}
+
 // ---- host --------------------------------------------------------------------------------------------------------------
 struct DistillCall {
     const char *name;
@@ -676,6 +853,21 @@ template <int DT, bool GRAD> static void launch_rows(const DistillArgs &a, int s
     else launch_block<DT, 512, 8, GRAD>(a, s);
 }
 
+// Rows that a wavefront holds
+static constexpr int SHORT_V = 1024;
+
+template <int DT, int NQ, int MODE> static void launch_short_nq(const DistillArgs &a, hipStream_t s)
+{
+    const dim3 grid((unsigned)((a.rows + 3) / 4));
+    if (a.teacher_lse) EASGD_LAUNCH((distill_short_kernel<DT, NQ, true, MODE>), grid, dim3(256), 0, s, a);
+    else EASGD_LAUNCH((distill_short_kernel<DT, NQ, false, MODE>), grid, dim3(256), 0, s, a);
+}
+template <int DT, int MODE> static void launch_short(const DistillArgs &a, hipStream_t s)
+{
+    if (a.V <= 128) launch_short_nq<DT, 2, MODE>(a, s);
+    else launch_short_nq<DT, SHORT_V / 64, MODE>(a, s);
+}
+
 // Rows cut into parts: a workspace for the parts' sums, then for the states of the rows.
 static size_t split_bytes(size_t rows, int segments) { return segments == 1 ? 0 : (rows * (segments + 1) * sizeof(float4) + 255) / 256 * 256; }
 
@@ -696,7 +888,8 @@ template <int MODE> static int launch_distill(const DistillCall &q, void *stream
     a.partial = static_cast<float4 *>(q.workspace);
     by_dtype(q.dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
-        if constexpr (MODE == DISTILL_GRAD) launch_grad<DT>(a, s);
+        if (a.V <= SHORT_V) launch_short<DT, MODE>(a, s);
+        else if constexpr (MODE == DISTILL_GRAD) launch_grad<DT>(a, s);
         else if (segments == 1) launch_rows<DT, MODE == DISTILL_BOTH>(a, slots, s);
         else {
             if constexpr (MODE == DISTILL_BOTH) a.state = reinterpret_cast<float *>(a.partial + q.rows * segments);
@@ -724,7 +917,7 @@ int easgd_distill_loss(const void *logits, int dtype, size_t rows, int V, size_t
                        void *workspace, size_t workspace_bytes, void *stream)
 {
     easgd::DistillCall q = {"easgd_distill_loss", dtype, rows, {}, workspace, workspace_bytes};
-    q.a = {logits, ld, V, k, indices, values, teacher_lse, labels, temperature, hard, loss, state, nullptr, 1.f, nullptr, 0, rows, nullptr, 1, 0};
+    q.a = {logits, ld, V, k, indices, values, teacher_lse, labels, temperature, hard, loss, state, nullptr, 1.f, nullptr, 0, rows, 1, 0, nullptr, 1, 0};
     return easgd::launch_distill<easgd::DISTILL_LOSS>(q, stream);
 }
 
@@ -733,7 +926,7 @@ int easgd_distill_grad(const void *logits, int dtype, size_t rows, int V, size_t
                        const float *dloss, float scale, void *dlogits, size_t dld, void *stream)
 {
     easgd::DistillCall q = {"easgd_distill_grad", dtype, rows, {}, nullptr, 0};
-    q.a = {logits, ld, V, k, indices, values, teacher_lse, labels, temperature, hard, nullptr, const_cast<float *>(state), dloss, scale, dlogits, dld, rows, nullptr, 1, 0};
+    q.a = {logits, ld, V, k, indices, values, teacher_lse, labels, temperature, hard, nullptr, const_cast<float *>(state), dloss, scale, dlogits, dld, rows, 1, 0, nullptr, 1, 0};
     return easgd::launch_distill<easgd::DISTILL_GRAD>(q, stream);
 }
 
@@ -742,7 +935,7 @@ int easgd_distill(const void *logits, int dtype, size_t rows, int V, size_t ld, 
                   void *dlogits, size_t dld, void *workspace, size_t workspace_bytes, void *stream)
 {
     easgd::DistillCall q = {"easgd_distill", dtype, rows, {}, workspace, workspace_bytes};
-    q.a = {logits, ld, V, k, indices, values, teacher_lse, labels, temperature, hard, loss, nullptr, nullptr, scale, dlogits, dld, rows, nullptr, 1, 0};
+    q.a = {logits, ld, V, k, indices, values, teacher_lse, labels, temperature, hard, loss, nullptr, nullptr, scale, dlogits, dld, rows, 1, 0, nullptr, 1, 0};
     return easgd::launch_distill<easgd::DISTILL_BOTH>(q, stream);
 }
 

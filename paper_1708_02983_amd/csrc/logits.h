@@ -177,6 +177,16 @@ __device__ __forceinline__ float wave_max(float v)
     for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
     return v;
 }
+// the one value among the lanes that is not 0 (or 0)
+__device__ __forceinline__ float wave_only(float v)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        const float other = __shfl_xor(v, o);
+        v = v != 0.f ? v : other;
+    }
+    return v;
+}
 // scratch: one T per wavefront; ends with every thread holding the sum, and with scratch free again
 template <int BLOCK, typename T> __device__ __forceinline__ T block_sum(T v, T *scratch)
 {
