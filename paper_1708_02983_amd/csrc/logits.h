@@ -241,6 +241,18 @@ static inline int check_logits(const char *name, const void *logits, int dtype, 
     if (!aligned_to(logits, dtype_bytes(dtype))) return fail(EASGD_EINVAL, "%s: logits must be aligned to their elements (%zu bytes)", name, dtype_bytes(dtype));
     return EASGD_OK;
 }
+// Slots of a row of V elements at the worst alignment
+static inline int most_slots(int dtype, int V)
+{
+    const int vec = dtype == EASGD_F32 ? 4 : 8;
+    return (V + 2 * (vec - 1)) / vec;
+}
+static inline int check_workspace(const char *name, const void *workspace, size_t bytes, size_t need)
+{
+    if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || bytes < need))
+        return fail(EASGD_EWORKSPACE, "%s: workspace must be 256-byte aligned and hold %zu bytes (got %zu)", name, need, bytes);
+    return EASGD_OK;
+}
 static inline int check_temperature(const char *name, float T)
 {
     if (!(T >= 1e-6f && T <= 1e6f)) return fail(EASGD_EINVAL, "%s: temperature must be in [1e-6, 1e6], got %g", name, (double)T);

@@ -1,10 +1,10 @@
-// Finding a place in the order of a row of logits: the order word of its n-th token, or of the token at which the mass of
-// the tokens before it reaches a target.  General and exact for every row (ties, masked places, constant rows).
+// Finding the first tokens of the order of a row of logits.
 #pragma once
 #include "logits.h"
 
 namespace easgd {
 
+// ---- a place in the order, exactly and for every row (ties, masked places, constant rows) ----------------------------
 // Order words are walked down digit by digit, largest first: 32 bits of key, then the 20 index bits that differ.
 // The digits' bins are counted in LDS; the bin in which the target falls is the next level's interval.
 static constexpr int SELECT_BINS = 2048;
@@ -12,18 +12,18 @@ static constexpr int SELECT_LEVELS = 5;
 __host__ __device__ static constexpr int select_shift(int level) { return level == 0 ? 53 : level == 1 ? 42 : level == 2 ? 32 : level == 3 ? 10 : 0; }
 __host__ __device__ static constexpr int select_bits(int level) { return level < 2 ? 11 : 10; }
 
-struct SelectLds {
-    unsigned long long mass[SELECT_BINS];
+template <bool MASS> struct SelectLds {
     unsigned count[SELECT_BINS];
+    unsigned long long mass[MASS ? SELECT_BINS : 1];
     unsigned long long part[16];
     unsigned long long above;      // mass (or tokens) before the chosen bin
     unsigned bin, bin_count;
 };
 
 // The bin, from the last (largest) one down, at which the running sum of the weights first reaches target - above.
-// weight(bin) is read by one thread each.  Every thread returns with the block's choice in lds.bin, lds.above, lds.bin_count.
-template <int BLOCK, bool MASS>
-__device__ __forceinline__ void select_bin(SelectLds &lds, int bins, unsigned long long above, unsigned long long target)
+// Every thread returns with the block's choice in lds.bin, lds.above, lds.bin_count.
+template <int BLOCK, bool BY_MASS, bool MASS>
+__device__ __forceinline__ void select_bin(SelectLds<MASS> &lds, int bins, unsigned long long above, unsigned long long target)
 {
     constexpr int PER = SELECT_BINS / BLOCK;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -31,7 +31,7 @@ __device__ __forceinline__ void select_bin(SelectLds &lds, int bins, unsigned lo
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int b = bins - 1 - (tid * PER + i);
-        w[i] = b < 0 ? 0ull : MASS ? lds.mass[b] : (unsigned long long)lds.count[b];
+        w[i] = b < 0 ? 0ull : BY_MASS ? lds.mass[MASS ? b : 0] : (unsigned long long)lds.count[b];
         sum += w[i];
     }
     unsigned long long run = sum;                       // inclusive over the lanes
@@ -59,14 +59,13 @@ __device__ __forceinline__ void select_bin(SelectLds &lds, int bins, unsigned lo
     __syncthreads();
 }
 
-// The smallest order word of the shortest prefix of the row's order whose weights reach `target` (>= 1; the weights of all
-// words >= floor must reach it).  MASS: the weight of an element is mass(x), else 1.  Only words >= floor count.
-// Passes over the row: one per level, until the chosen bin holds one element, or (counting) all of it is in the prefix.
-template <int DT, int BLOCK, bool MASS, typename F>
-__device__ __forceinline__ unsigned long long select_word(const Row<DT> &row, unsigned long long floor, unsigned long long target,
-                                                          SelectLds &lds, F mass)
+// The smallest order word of the shortest prefix of the order whose weights reach `target` (>= 1; the weights of all words
+// >= floor must reach it).  each(f) calls f(word, logit) for every element (or order word) there is, through the threads
+// of the block; words below `floor` do not count.  BY_MASS: the weight of an element is mass(logit), else 1.
+// Calls of each: one per level, until the chosen bin holds one element, or (counting) all of it is in the prefix.
+template <int BLOCK, bool BY_MASS, bool MASS, typename E, typename F>
+__device__ __forceinline__ unsigned long long select_word(E each, unsigned long long floor, unsigned long long target, SelectLds<MASS> &lds, F mass)
 {
-    constexpr int VEC = Row<DT>::VEC;
     unsigned long long prefix = 0, above = 0;
 #pragma unroll 1
     for (int level = 0; level < SELECT_LEVELS; ++level) {
@@ -75,29 +74,198 @@ __device__ __forceinline__ unsigned long long select_word(const Row<DT> &row, un
         __syncthreads();
         for (int b = threadIdx.x; b < bins; b += BLOCK) {
             lds.count[b] = 0;
-            if constexpr (MASS) lds.mass[b] = 0;
+            if constexpr (BY_MASS) lds.mass[b] = 0;
         }
         __syncthreads();
-        for (int s = threadIdx.x; s < row.slots; s += BLOCK) {
-            float x[VEC];
+        each([&](unsigned long long word, float x) {
+            if (word >= FIRST_WORD && word >= floor && (level == 0 || ((word ^ prefix) >> (shift + bits)) == 0)) {
+                const unsigned b = (unsigned)(word >> shift) & (bins - 1);
+                atomicAdd(&lds.count[b], 1u);
+                if constexpr (BY_MASS) atomicAdd(&lds.mass[b], mass(x));
+            }
+        });
+        __syncthreads();
+        select_bin<BLOCK, BY_MASS>(lds, bins, above, target);
+        prefix |= (unsigned long long)lds.bin << shift;
+        above = lds.above;
+        if (lds.bin_count == 1 || (!BY_MASS && above + lds.bin_count == target)) break;
+    }
+    __syncthreads();
+    return prefix > floor ? prefix : floor;
+}
+template <int BLOCK, bool MASS, typename E>
+__device__ __forceinline__ unsigned long long select_nth(E each, unsigned long long floor, unsigned n, SelectLds<MASS> &lds)
+{
+    return select_word<BLOCK, false>(each, floor, (unsigned long long)n, lds, [](float) { return 0ull; });
+}
+
+// the elements of slots [s0, s1) of a row, as select_word takes them
+template <int DT, int BLOCK> struct EachElement {
+    const Row<DT> &row;
+    int s0, s1;
+    template <typename F> __device__ __forceinline__ void operator()(F f) const
+    {
+        for (int s = s0 + threadIdx.x; s < s1; s += BLOCK) {
+            float x[Row<DT>::VEC];
             Row<DT>::Type::unpack(row.load(s), x);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const unsigned long long word = order_word(logit_key(x[i]), row.index(s, i));
-                if (word >= FIRST_WORD && word >= floor && (level == 0 || ((word ^ prefix) >> (shift + bits)) == 0)) {
-                    const unsigned b = (unsigned)(word >> shift) & (bins - 1);
-                    atomicAdd(&lds.count[b], 1u);
-                    if constexpr (MASS) atomicAdd(&lds.mass[b], mass(x[i]));
+            for (int i = 0; i < Row<DT>::VEC; ++i) f(order_word(logit_key(x[i]), row.index(s, i)), x[i]);
+        }
+    }
+};
+
+// ---- the first k of the order in one pass -----------------------------------------------------------------------------
+// A list in LDS takes every element above a floor that rises as the row goes by: first to the k-th largest of the threads'
+// maxima over the first round of slots (k of them are at least as large, so the k-th of the row is), then, whenever the
+// list has grown, to the k-th of the list.  On average a round adds k over the number of rounds gone by, so the list stays
+// short and the loop over the row has one maximum and one comparison per 128 bits.  Rows that overflow the list all the
+// same (ascending ones, more ties than it holds) are walked down digit by digit instead.
+static constexpr int TOP_LIST = 2048;
+struct TopLds {
+    unsigned long long list[TOP_LIST];
+    unsigned n;
+    SelectLds<false> select;
+};
+struct EachListed {
+    const unsigned long long *list;
+    unsigned n;
+    int block;
+    template <typename F> __device__ __forceinline__ void operator()(F f) const
+    {
+        for (unsigned i = threadIdx.x; i < n; i += block) f(list[i], 0.f);
+    }
+};
+
+// the list's words from `floor` on to its front; returns their number.  Ends with a barrier.
+template <int BLOCK> __device__ __forceinline__ unsigned keep_from(TopLds &lds, unsigned n, unsigned long long floor)
+{
+    constexpr int PER = TOP_LIST / BLOCK;
+    unsigned long long w[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const unsigned at = threadIdx.x + i * BLOCK;
+        w[i] = at < n ? lds.list[at] : 0;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) lds.n = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+        if (w[i] >= FIRST_WORD && w[i] >= floor) lds.list[atomicAdd(&lds.n, 1u)] = w[i];
+    __syncthreads();
+    return lds.n;
+}
+
+// The order words of the first k (<= LOGITS_MAX_TOP) elements of slots [s0, s1), unordered, at the front of lds.list; returns how
+// many there are (fewer than k where fewer are above -inf).  seen(x, slot) is called for every slot by whole wavefronts
+// (an empty slot where a lane has none).  Ends with a barrier.
+template <int DT, int BLOCK, typename F>
+__device__ __forceinline__ unsigned first_of(const Row<DT> &row, int s0, int s1, unsigned k, TopLds &lds, F seen)
+{
+    constexpr int VEC = Row<DT>::VEC, DEEP = 4;
+    static_assert(BLOCK >= LOGITS_MAX_TOP && TOP_LIST % BLOCK == 0, "one maximum per thread has to do for the first floor");
+    using Type = typename Row<DT>::Type;
+    const int tid = threadIdx.x;
+    const unsigned grown = max(4 * k, 256u);            // words after which the floor is raised again
+    uint4 v[DEEP];
+    auto load = [&](int s) {
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) v[i] = s + i * BLOCK < s1 ? row.load(s + i * BLOCK) : Row<DT>::empty();
+    };
+    load(s0 + tid);
+    unsigned long long floor = FIRST_WORD;
+    if (tid == 0) lds.n = 0;
+    if ((s1 - s0) * VEC > TOP_LIST) {
+        float t = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) {
+            float x[VEC];
+            Type::unpack(v[i], x);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) t = fmaxf(t, x[j]);
+        }
+        lds.list[tid] = order_word(logit_key(t), tid);
+        const unsigned some = __syncthreads_count(t > -INFINITY);
+        if (some >= k) floor = select_nth<BLOCK>(EachListed{lds.list, (unsigned)BLOCK, BLOCK}, FIRST_WORD, k, lds.select) >> 32 << 32;
+        if (floor < FIRST_WORD) floor = FIRST_WORD;
+    }
+    __syncthreads();
+    float least = 0.f;                                  // the floor as a logit; every logit that may be taken is at least -FLT_MAX
+    auto set_least = [&]() { least = key_logit(max((unsigned)(floor >> 32), 0x00800000u)); };
+    set_least();
+    unsigned n = 0;
+    bool over = false;
+    for (int s = s0 + tid;;) {
+        uint4 w[DEEP];
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) w[i] = v[i];
+        const int now = s;
+        s += DEEP * BLOCK;
+        const bool more = s - tid < s1;                 // uniform
+        if (more) load(s);
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) {
+            const int at = now + i * BLOCK;
+            if (at - (tid & 63) >= s1) break;           // the whole wavefront is behind the end
+            float x[VEC];
+            Type::unpack(w[i], x);
+            seen(x, at);
+            float t = x[0];
+#pragma unroll
+            for (int j = 1; j < VEC; ++j) t = fmaxf(t, x[j]);
+            if (!over && t >= least) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    if (x[j] >= least) {
+                        const unsigned long long word = order_word(logit_key(x[j]), row.index(at, j));
+                        if (word >= floor) {
+                            const unsigned to = atomicAdd(&lds.n, 1u);
+                            if (to < TOP_LIST) lds.list[to] = word;
+                        }
+                    }
                 }
             }
         }
+        if (!more) break;
         __syncthreads();
-        select_bin<BLOCK, MASS>(lds, bins, above, target);
-        prefix |= (unsigned long long)lds.bin << shift;
-        above = lds.above;
-        if (lds.bin_count == 1 || (!MASS && above + lds.bin_count == target)) break;
+        n = lds.n;
+        over = over || n > TOP_LIST;                    // uniform
+        if (!over && n > grown) {
+            floor = select_nth<BLOCK>(EachListed{lds.list, n, BLOCK}, floor, k, lds.select);
+            keep_from<BLOCK>(lds, n, floor);
+            set_least();
+        } else __syncthreads();                         // everyone has read n before it grows again
     }
-    return prefix > floor ? prefix : floor;
+    __syncthreads();
+    n = lds.n;
+    over = over || n > TOP_LIST;
+    if (over) {
+        // k elements are above the floor: its first value came from k maxima, later ones from k listed words
+        floor = select_nth<BLOCK>(EachElement<DT, BLOCK>{row, s0, s1}, FIRST_WORD, k, lds.select);
+        if (tid == 0) lds.n = 0;
+        __syncthreads();
+        EachElement<DT, BLOCK>{row, s0, s1}([&](unsigned long long word, float) {
+            if (word >= floor && word >= FIRST_WORD) {
+                const unsigned to = atomicAdd(&lds.n, 1u);
+                if (to < TOP_LIST) lds.list[to] = word;         // always, unless the logits change under the kernel
+            }
+        });
+        __syncthreads();
+        return min(lds.n, k);
+    }
+    if (n > k) {
+        floor = select_nth<BLOCK>(EachListed{lds.list, n, BLOCK}, floor, k, lds.select);
+        n = keep_from<BLOCK>(lds, n, floor);
+    }
+    return n;
+}
+
+// The number of words of lds.list[0..n) before each of the threads' own (thread i's word is word i).
+__device__ __forceinline__ unsigned rank_of(const unsigned long long *list, unsigned n, unsigned long long word)
+{
+    unsigned rank = 0;
+    for (unsigned j = 0; j < n; ++j) rank += list[j] > word;
+    return rank;
 }
 
 }  // namespace easgd

@@ -33,7 +33,7 @@ template <int DT, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
 {
     constexpr int VEC = Row<DT>::VEC, WAVES = BLOCK / 64;
-    __shared__ SelectLds sel;
+    __shared__ SelectLds<true> sel;
     __shared__ unsigned long long part[WAVES];
     const size_t r = blockIdx.x;
     const Row<DT> row(a.logits, r, a.ld, a.V);
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
         }
         const unsigned long long n = block_sum<BLOCK>((unsigned long long)taken, part);
         if (n > (unsigned long long)top_k)
-            floor = select_word<DT, BLOCK, false>(row, FIRST_WORD, top_k, sel, weight);
+            floor = select_nth<BLOCK>(EachElement<DT, BLOCK>{row, 0, row.slots}, FIRST_WORD, top_k, sel);
     }
     if (top_p < 1.f) {
         unsigned long long mass = 0;
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
         }
         mass = block_sum<BLOCK>(mass, part);
         const double target = ceil((double)top_p * (double)mass);
-        floor = select_word<DT, BLOCK, true>(row, floor, target >= 1.0 ? (unsigned long long)target : 1ull, sel, weight);
+        floor = select_word<BLOCK, true>(EachElement<DT, BLOCK>{row, 0, row.slots}, floor, target >= 1.0 ? (unsigned long long)target : 1ull, sel, weight);
     }
 
     // the mass of what is kept, by wavefront: wavefront v owns a run of whole slots

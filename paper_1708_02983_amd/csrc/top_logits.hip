@@ -1,96 +1,193 @@
 // easgd_top_logits: the k first logits of every row's order, and the row's log-sum-exp.
+//
+// One pass: the sums of exponentials (row_sums.h) and the first k (logits_select.h) ride on the same loads.  Bound: HBM for many
+// long rows (each logit once), latency for few or short ones.
 #include "logits.h"
 #include "logits_select.h"
+#include "row_sums.h"
 
 namespace easgd {
 
 struct TopArgs {
     const void *logits;
-    size_t ld;
+    size_t ld, rows;
     int V, k;
     float temperature;
     float *values;
     int *indices;
     float *lse;
+    int segments, seg_slots;           // slots of a part of a row
+    unsigned long long *words;         // [rows][segments][k]: the first k of every part (0: none left)
+    float4 *partial;                   // [rows][segments]: its sums
 };
 
+__device__ __forceinline__ void write_top(const TopArgs &a, size_t r, unsigned at, unsigned long long word)
+{
+    a.values[r * a.k + at] = word ? key_logit((unsigned)(word >> 32)) : -INFINITY;
+    a.indices[r * a.k + at] = word ? (int)~(unsigned)word : -1;
+}
+__device__ __forceinline__ void write_lse(const TopArgs &a, size_t r, const float4 &s)
+{
+    if (a.lse) a.lse[r] = s.x == INFINITY ? INFINITY : (float)((double)(s.x == -INFINITY ? 0.f : s.x) / (double)a.temperature + log((double)s.y));
+}
+// the n words at the front of the list, by rank; places that are left over
+__device__ __forceinline__ void write_ranked(const TopArgs &a, size_t r, const unsigned long long *list, unsigned n)
+{
+    const unsigned i = threadIdx.x;
+    if (i >= (unsigned)a.k) return;
+    if (i < n) write_top(a, r, rank_of(list, n, list[i]), list[i]);
+    else write_top(a, r, i, 0);
+}
+
+// ---- a block per row, or per part of a row ------------------------------------------------------------------------------
 template <int DT, int BLOCK>
-__global__ __launch_bounds__(BLOCK) void top_logits_kernel(TopArgs a)
+__global__ __launch_bounds__(BLOCK) void top_rows_kernel(TopArgs a)
 {
     constexpr int VEC = Row<DT>::VEC;
-    __shared__ SelectLds sel;
-    __shared__ unsigned long long best[LOGITS_MAX_TOP];
-    __shared__ float fpart[BLOCK / 64];
-    __shared__ unsigned n_best;
-    const size_t r = blockIdx.x;
+    __shared__ TopLds lds;
+    __shared__ float4 part[BLOCK / 64];
+    const size_t r = blockIdx.x / a.segments;
+    const int seg = blockIdx.x % a.segments;
     const Row<DT> row(a.logits, r, a.ld, a.V);
-    const int tid = threadIdx.x;
-    const float c = (float)(LOG2E / (double)a.temperature);
-
-    float m = -FLT_MAX, sum = 0.f;
-    unsigned taken = 0;
-    for (int s = tid; s < row.slots; s += BLOCK) {
-        float x[VEC];
-        Row<DT>::Type::unpack(row.load(s), x);
-        float top = x[0];
-#pragma unroll
-        for (int i = 1; i < VEC; ++i) top = fmaxf(top, x[i]);
-        if (top > m) {
-            sum *= exp2_fast((m - top) * c);
-            m = top;
-        }
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            sum += exp2_fast((x[i] - m) * c);
-            taken += logit_key(x[i]) != 0;
-        }
+    const Scales q(a.temperature);
+    const int s0 = seg * a.seg_slots, s1 = min(s0 + a.seg_slots, row.slots);
+    RowSums<VEC, false, HARD_PLAIN> acc(q);
+    const unsigned n = first_of<DT, BLOCK>(row, s0, s1, (unsigned)a.k, lds, [&](const float (&x)[VEC], int) { acc.add(x, 0u); });
+    const float4 sums = acc.template combine<BLOCK>(part);
+    if (a.segments == 1) {
+        if (threadIdx.x == 0) write_lse(a, r, sums);
+        write_ranked(a, r, lds.list, n);
+        return;
     }
-    const float M = block_max<BLOCK>(m, fpart);
-    const float S = block_sum<BLOCK>(sum * exp2_fast((m - M) * c), fpart);
-    const unsigned n = block_sum<BLOCK>(taken, reinterpret_cast<unsigned *>(fpart));
-    if (a.lse && tid == 0) a.lse[r] = M == INFINITY ? INFINITY : (float)((double)M / (double)a.temperature + log((double)S));
+    if (threadIdx.x == 0) a.partial[blockIdx.x] = sums;
+    if ((int)threadIdx.x < a.k) a.words[(size_t)blockIdx.x * a.k + threadIdx.x] = threadIdx.x < n ? lds.list[threadIdx.x] : 0;
+}
 
-    const unsigned want = n < (unsigned)a.k ? n : (unsigned)a.k;
-    unsigned long long floor = FIRST_WORD;
-    if (n > want) floor = select_word<DT, BLOCK, false>(row, FIRST_WORD, want, sel, [](float) { return 0ull; });
-    if (tid == 0) n_best = 0;
+// ---- the parts of a row together ------------------------------------------------------------------------------------------
+template <int BLOCK>
+__global__ __launch_bounds__(BLOCK) void top_join_kernel(TopArgs a)
+{
+    __shared__ TopLds lds;
+    const size_t r = blockIdx.x;
+    const unsigned all = (unsigned)(a.segments * a.k);             // <= TOP_LIST
+    if (threadIdx.x == 0) {
+        const Scales q(a.temperature);
+        float4 s = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+        for (int i = 0; i < a.segments; ++i) s.x = fmaxf(s.x, a.partial[r * a.segments + i].x);
+        for (int i = 0; i < a.segments; ++i) RowSums<4, false, HARD_PLAIN>::join(s, a.partial[r * a.segments + i], q);
+        write_lse(a, r, s);
+        lds.n = all;
+    }
+    for (unsigned i = threadIdx.x; i < all; i += BLOCK) lds.list[i] = a.words[r * all + i];
     __syncthreads();
-    for (int s = tid; s < row.slots; s += BLOCK) {
-        float x[VEC];
-        Row<DT>::Type::unpack(row.load(s), x);
+    unsigned n = keep_from<BLOCK>(lds, all, FIRST_WORD);           // the words that are there
+    if (n > (unsigned)a.k) n = keep_from<BLOCK>(lds, n, select_nth<BLOCK>(EachListed{lds.list, n, BLOCK}, FIRST_WORD, a.k, lds.select));
+    write_ranked(a, r, lds.list, n);
+}
+
+// ---- short rows: a wavefront each ---------------------------------------------------------------------------------------------
+// Element lane + 64 q sits in register q.  The k-th largest key is found bit by bit with votes; equal keys are taken by
+// ascending index, which is the order of registers, then lanes.
+template <int DT, int NQ>
+__global__ __launch_bounds__(256) void top_short_kernel(TopArgs a)
+{
+    __shared__ unsigned long long all_words[4][LOGITS_MAX_TOP];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const size_t r = (size_t)blockIdx.x * 4 + wave;
+    if (r >= a.rows) return;                            // wavefronts of a block have nothing in common
+    unsigned long long *words = all_words[wave];
+    const Row<DT> row(a.logits, r, a.ld, a.V);
+    float x[NQ];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const unsigned long long word = order_word(logit_key(x[i]), row.index(s, i));
-            if (word >= floor) {
-                const unsigned at = atomicAdd(&n_best, 1u);
-                if (at < LOGITS_MAX_TOP) best[at] = word;         // always, unless the logits change under the kernel
+    for (int q = 0; q < NQ; ++q) x[q] = lane + 64 * q < a.V ? row.load_one(lane + 64 * q) : -INFINITY;
+
+    unsigned key[NQ], there = 0;
+    float m = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        key[q] = logit_key(x[q]);
+        there += __popcll(__ballot(key[q] != 0));
+        m = fmaxf(m, x[q]);
+    }
+    if (a.lse) {
+        m = wave_max(m);
+        const float c = Scales(a.temperature).c, from = m == -INFINITY ? 0.f : m;
+        float sum = 0.f;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) sum += exp2_fast((x[q] - from) * c);
+        sum = wave_sum(sum);
+        if (lane == 0) write_lse(a, r, make_float4(m, sum, 0.f, 0.f));
+    }
+    const unsigned k = min((unsigned)a.k, there);
+    unsigned least = 1, above = there;                  // `above` keys are >= least
+    if (there > k) {
+        least = 0;
+        for (unsigned bit = 0x80000000u; bit && above != k; bit >>= 1) {
+            const unsigned next = least | bit;
+            unsigned n = 0;
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) n += __popcll(__ballot(key[q] >= next));
+            if (n >= k) {
+                least = next;
+                above = n;
             }
         }
     }
-    __syncthreads();
-    // every word's rank is the number of larger ones
-    for (int i = tid; i < a.k; i += BLOCK) {
-        if (i < (int)want) {
-            const unsigned long long mine = best[i];
-            int rank = 0;
-            for (unsigned j = 0; j < want; ++j) rank += best[j] > mine;
-            a.values[r * a.k + rank] = key_logit((unsigned)(mine >> 32));
-            a.indices[r * a.k + rank] = (int)~(unsigned)mine;
-        } else {
-            a.values[r * a.k + i] = -INFINITY;
-            a.indices[r * a.k + i] = -1;
-        }
+    // keys above `least`, then as many equal ones as are wanted
+    unsigned equal_left = k;
+    if (above != k) {
+        unsigned n = 0;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) n += __popcll(__ballot(key[q] > least));
+        equal_left = k - n;
     }
+    unsigned n = 0;
+    const unsigned long long below = (1ull << lane) - 1;
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        const unsigned long long equal = __ballot(key[q] == least && key[q] != 0);
+        const bool take = key[q] > least || (key[q] == least && key[q] != 0 && (unsigned)__popcll(equal & below) < equal_left);
+        equal_left -= min(equal_left, (unsigned)__popcll(equal));
+        const unsigned long long taken = __ballot(take);
+        if (take) words[n + __popcll(taken & below)] = order_word(key[q], lane + 64 * q);
+        n += __popcll(taken);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");         // LDS accesses of one wavefront are executed in order
+    for (unsigned i = lane; i < (unsigned)a.k; i += 64) {
+        if (i < n) write_top(a, r, rank_of(words, n, words[i]), words[i]);
+        else write_top(a, r, i, 0);
+    }
+}
+
+// Few long rows are cut into parts, so that there are blocks for the whole chip: each part's first k go through the workspace.
+static constexpr int TOP_BLOCK = 512, TOP_SHORT_V = 1024;
+static constexpr int TOP_SPLIT_ROWS = 256, TOP_SPLIT_SLOTS = 2048;
+static int top_segments(size_t rows, int slots, int k)
+{
+    if (rows >= TOP_SPLIT_ROWS || slots < 2 * TOP_SPLIT_SLOTS) return 1;
+    int n = (int)((512 + rows - 1) / rows);
+    if (n > slots / TOP_SPLIT_SLOTS) n = slots / TOP_SPLIT_SLOTS;
+    if (n > TOP_LIST / k) n = TOP_LIST / k;
+    return n < 1 ? 1 : n;
+}
+static size_t top_bytes(size_t rows, int segments, int k)
+{
+    return segments == 1 ? 0 : (rows * segments * (sizeof(float4) + (size_t)k * 8) + 255) / 256 * 256;
 }
 
 }  // namespace easgd
 
 extern "C" {
 
-size_t easgd_top_logits_workspace_bytes(size_t, int, int) { return 0; }
+size_t easgd_top_logits_workspace_bytes(size_t rows, int V, int k)
+{
+    using namespace easgd;
+    if (rows == 0 || rows > 0x3fffffffull || V < 1 || V > LOGITS_MAX_V || k < 1 || k > LOGITS_MAX_TOP) return 0;
+    return top_bytes(rows, top_segments(rows, most_slots(EASGD_F32, V), k), k);     // fp32 rows have the most slots
+}
 
 int easgd_top_logits(const void *logits, int dtype, size_t rows, int V, size_t ld, int k, float temperature,
-                     float *values, int32_t *indices, float *lse, void *, size_t, void *stream)
+                     float *values, int32_t *indices, float *lse, void *workspace, size_t workspace_bytes, void *stream)
 {
     using namespace easgd;
     const char *name = "easgd_top_logits";
@@ -99,12 +196,22 @@ int easgd_top_logits(const void *logits, int dtype, size_t rows, int V, size_t l
     if (int rc = check_temperature(name, temperature)) return rc;
     if (rows > 0 && (!values || !indices)) return fail(EASGD_EINVAL, "%s: NULL pointer", name);
     if (!aligned_to(values, 4) || !aligned_to(indices, 4) || !aligned_to(lse, 4)) return fail(EASGD_EINVAL, "%s: values, indices, lse must be 4-byte aligned", name);
+    const size_t need = easgd_top_logits_workspace_bytes(rows, V, k);
+    if (int rc = check_workspace(name, workspace, workspace_bytes, need)) return rc;
     clear_error();
     if (rows == 0) return EASGD_OK;
-    const TopArgs a = {logits, ld, V, k, temperature, values, indices, lse};
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const int slots = most_slots(dtype, V), segments = top_segments(rows, slots, k);
+    TopArgs a = {logits, ld, rows, V, k, temperature, values, indices, lse, segments, (slots + segments - 1) / segments, nullptr, nullptr};
+    a.partial = static_cast<float4 *>(workspace);
+    a.words = reinterpret_cast<unsigned long long *>(a.partial + rows * segments);
     by_dtype(dtype, [&](auto dt) {
-        EASGD_LAUNCH((top_logits_kernel<decltype(dt)::value, 256>), dim3((unsigned)rows), dim3(256), 0, static_cast<hipStream_t>(stream), a);
+        constexpr int DT = decltype(dt)::value;
+        if (V <= 128) EASGD_LAUNCH((top_short_kernel<DT, 2>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
+        else if (V <= TOP_SHORT_V) EASGD_LAUNCH((top_short_kernel<DT, TOP_SHORT_V / 64>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
+        else EASGD_LAUNCH((top_rows_kernel<DT, TOP_BLOCK>), dim3((unsigned)(rows * segments)), dim3(TOP_BLOCK), 0, s, a);
     });
+    if (V > TOP_SHORT_V && segments > 1) EASGD_LAUNCH((top_join_kernel<TOP_BLOCK>), dim3((unsigned)rows), dim3(TOP_BLOCK), 0, s, a);
     return check_launch(name);
 }
 
