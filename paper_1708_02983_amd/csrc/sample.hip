@@ -1,4 +1,13 @@
 // easgd_sample_tokens: one token of every row, drawn with a given random number.
+//
+// All three filters keep a prefix of the row's order, so what is kept is "every order word from some word on" (and w >= min_p),
+// and the draw in index order needs no sorting: the kept mass by wavefront, then by 64 slots, then by element.  Masses are
+// whole numbers of units, whose sums are the same in every order, so the passes over a row agree to the last bit.
+//   top_k <= 256, or greedy:  the first k in one pass (logits_select.h), everything else on at most 256 words in LDS
+//   top_p:                    the mass of the row in bins of equal width below the largest logit, then the bin of the border
+//   neither:                  no border to find
+// Bound: latency of the passes over a row (which stays in the caches) and, where masses of whole rows are asked for, the vector
+// ALUs: some 25 instructions a logit for a 64-bit exponential.
 #include "logits.h"
 #include "logits_select.h"
 
@@ -13,111 +22,294 @@ struct SampleArgs {
     const float *top_p, *min_p;
     int *tokens;
     float *logprob;
-    double unit;              // units of mass in the largest weight, a power of two
+    int unit;                 // log2 of the units of mass in the largest weight
 };
 
-// w = exp((z - max) / T) as a whole number of units: adding 2^52 rounds to the nearest whole number and leaves it in the
-// low bits of the sum (w * unit <= 2^51).
+// w = 2^y with y = (z - max) log2(e) / T <= 0: 2^n 2^f with |f| <= 1/2 and the Taylor polynomial of 2^f, whose remainder is below
+// (ln 2 / 2)^12 / 12! = 6e-15.  Below 2^-200 the value no longer matters (a unit is at least 2^-51, min_p at least 2^-149).
 struct Weight {
-    double inv_t, unit;
-    float max;
-    __device__ __forceinline__ double real(float z) const { return z == max ? 1.0 : exp(((double)z - (double)max) * inv_t); }
-    __device__ __forceinline__ unsigned long long units(double w) const
+    double scale, max;        // log2(e) / T
+    int unit;
+    bool infinite;            // the largest logit is +inf: logits are in or out
+    __device__ __forceinline__ Weight(float T, float top, int unit)
+        : scale(LOG2E / (double)T), max((double)top), unit(unit), infinite(top == INFINITY) {}
+    __device__ __forceinline__ void split(float z, double &p, int &n) const
     {
-        return __builtin_bit_cast(unsigned long long, fma(w, unit, 0x1p52)) - 0x4330000000000000ull;
+        const double y = fmax(((double)z - max) * scale, -200.0), whole = rint(y), f = y - whole;
+        n = (int)whole;
+        p = 4.4455382718708101e-10;
+        p = fma(p, f, 7.0549116208011209e-09);
+        p = fma(p, f, 1.0178086009239696e-07);
+        p = fma(p, f, 1.3215486790144305e-06);
+        p = fma(p, f, 1.5252733804059838e-05);
+        p = fma(p, f, 1.5403530393381606e-04);
+        p = fma(p, f, 1.3333558146428441e-03);
+        p = fma(p, f, 9.6181291076284769e-03);
+        p = fma(p, f, 5.5504108664821576e-02);
+        p = fma(p, f, 2.4022650695910069e-01);
+        p = fma(p, f, 6.9314718055994529e-01);
+        p = fma(p, f, 1.0);
     }
-    __device__ __forceinline__ unsigned long long operator()(float z) const { return units(real(z)); }
+    static __device__ __forceinline__ double power(int n) { return __builtin_bit_cast(double, (unsigned long long)(n + 1023) << 52); }
+    // adding 2^52 rounds to the nearest whole number and leaves it in the low bits of the sum (units <= 2^51)
+    __device__ __forceinline__ unsigned long long units(float z) const
+    {
+        if (infinite) return (double)z == max ? 1ull << unit : 0ull;      // uniform
+        double p;
+        int n;
+        split(z, p, n);
+        return __builtin_bit_cast(unsigned long long, fma(p, power(n + unit), 0x1p52)) - 0x4330000000000000ull;
+    }
+    __device__ __forceinline__ double real(float z) const
+    {
+        if (infinite) return (double)z == max ? 1.0 : 0.0;
+        double p;
+        int n;
+        split(z, p, n);
+        return p * power(n);
+    }
+    // log of w over a mass
+    __device__ __forceinline__ float log_share(float z, unsigned long long mass) const
+    {
+        const double ln_w = (double)z == max ? 0.0 : ((double)z - max) * scale * 0.69314718055994530942;
+        return (float)(ln_w - log((double)mass * power(-unit)));
+    }
+};
+
+// exclusive sum over the threads of the block, and the sum of all; part: one word per wavefront.  Ends with a barrier.
+template <int BLOCK>
+__device__ __forceinline__ unsigned long long scan(unsigned long long v, unsigned long long *part, unsigned long long &all)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    unsigned long long run = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const unsigned long long up = __shfl_up(run, o);
+        if (lane >= o) run += up;
+    }
+    if (lane == 63) part[wave] = run;
+    __syncthreads();
+    unsigned long long before = run - v;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < BLOCK / 64; ++w) {
+        if (w < wave) before += part[w];
+        all += part[w];
+    }
+    __syncthreads();
+    return before;
+}
+
+// the place of the drawn number in a mass: the token is the first at which the running sum exceeds it
+__device__ __forceinline__ unsigned long long drawn(float u, unsigned long long mass)
+{
+    const double at = (double)(u > 0.f ? fminf(u, 1.f - 0x1p-24f) : 0.f) * (double)mass;
+    const unsigned long long whole = (unsigned long long)at;
+    return whole < mass ? whole : mass - 1;
+}
+// the mass that a prefix has to reach: top_p of `mass`, at least one unit
+__device__ __forceinline__ unsigned long long wanted(float top_p, unsigned long long mass)
+{
+    const double target = ceil((double)top_p * (double)mass);
+    return target >= 1.0 ? (unsigned long long)target : 1ull;
+}
+
+// Bins of equal width below the largest logit: 2047 of them over 18 units of T, the last for all that is further below.
+static constexpr int MASS_BINS = SELECT_BINS, BORDER_LIST = TOP_LIST / 2;
+
+union SampleLds {
+    TopLds top;
+    SelectLds<true> mass;
 };
 
 template <int DT, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
 {
     constexpr int VEC = Row<DT>::VEC, WAVES = BLOCK / 64;
-    __shared__ SelectLds<true> sel;
+    using Type = LogitType<DT>;
+    __shared__ SampleLds lds;
     __shared__ unsigned long long part[WAVES];
+    __shared__ unsigned long long words[LOGITS_MAX_TOP], mass_of[LOGITS_MAX_TOP];
+    __shared__ float fpart[WAVES];
     const size_t r = blockIdx.x;
     const Row<DT> row(a.logits, r, a.ld, a.V);
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const float T = a.temperature ? a.temperature[r] : 1.f, top_p = a.top_p ? a.top_p[r] : 1.f, min_p = a.min_p ? a.min_p[r] : 0.f, u = a.u[r];
+    const int asked = a.top_k ? a.top_k[r] : 0, top_k = T > 0.f && !(min_p > 1.f) ? asked : 1;      // nothing reaches a min_p above 1: the first token is left
+    auto answer = [&](int token, float lp) {
+        a.tokens[r] = token;
+        if (a.logprob) a.logprob[r] = lp;
+    };
 
-    // the first token of the order
-    unsigned long long first = 0;
-    for (int s = tid; s < row.slots; s += BLOCK) {
-        float x[VEC];
-        Row<DT>::Type::unpack(row.load(s), x);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const unsigned long long word = order_word(logit_key(x[i]), row.index(s, i));
-            first = word > first ? word : first;
+    // ---- few tokens: all further work is on their order words ----
+    if (top_k >= 1 && top_k <= LOGITS_MAX_TOP) {
+        const unsigned n = first_of<DT, BLOCK>(row, 0, row.slots, (unsigned)top_k, lds.top, [](const float (&)[VEC], int) {});
+        if (n <= 1) {
+            if (tid == 0) answer(n ? (int)~(unsigned)lds.top.list[0] : -1, n ? 0.f : NAN);
+            return;
         }
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        const unsigned long long other = __shfl_xor(first, o);
-        first = other > first ? other : first;
-    }
-    if (lane == 0) part[wave] = first;
-    __syncthreads();
-    for (int v = 0; v < WAVES; ++v) first = part[v] > first ? part[v] : first;
-    __syncthreads();
-    const float T = a.temperature ? a.temperature[r] : 1.f;
-    if (first < FIRST_WORD || !(T > 0.f)) {
-        if (tid == 0) {
-            a.tokens[r] = first < FIRST_WORD ? -1 : (int)~(unsigned)first;
-            if (a.logprob) a.logprob[r] = first < FIRST_WORD ? NAN : 0.f;
+        // by rank
+        const unsigned i = tid;
+        if (i < n) words[rank_of(lds.top.list, n, lds.top.list[i])] = lds.top.list[i];
+        __syncthreads();
+        const Weight weight(T, key_logit((unsigned)(words[0] >> 32)), a.unit);
+        const float z = i < n ? key_logit((unsigned)(words[i] >> 32)) : 0.f;
+        unsigned long long w = i < n ? weight.units(z) : 0, all;
+        const unsigned long long before = scan<BLOCK>(w, part, all);
+        bool keep = i < n;
+        if (top_p < 1.f && before >= wanted(top_p, all)) keep = false;
+        if (min_p > 0.f && i > 0 && i < n && weight.real(z) < (double)min_p) keep = false;
+        if (!keep) w = 0;
+        // by index
+        unsigned at = 0;
+        if (i < n) {
+            const unsigned mine = (unsigned)words[i];              // ~index
+            for (unsigned j = 0; j < n; ++j) at += (unsigned)words[j] > mine;
+            mass_of[at] = w;
         }
+        __syncthreads();
+        const unsigned long long w_at = i < n ? mass_of[i] : 0;
+        const unsigned long long lead = scan<BLOCK>(w_at, part, all);
+        __syncthreads();
+        if (i < n) mass_of[i] = lead;
+        __syncthreads();
+        const unsigned long long target = drawn(u, all);
+        if (i < n && w && mass_of[at] <= target && target - mass_of[at] < w) answer((int)~(unsigned)words[i], weight.log_share(z, all));
         return;
     }
-    const float max = key_logit((unsigned)(first >> 32));
-    const Weight weight = {T == INFINITY && max == INFINITY ? 1.0 : 1.0 / (double)T, a.unit, max};      // a difference of -inf stays one
-    unsigned long long floor = FIRST_WORD;
-    const int top_k = a.top_k ? a.top_k[r] : 0;
-    const float top_p = a.top_p ? a.top_p[r] : 1.f;
-    const float min_p = a.min_p ? a.min_p[r] : 0.f;
 
-    if (top_k >= 1 && top_k < a.V) {
-        unsigned taken = 0;
-        for (int s = tid; s < row.slots; s += BLOCK) {
-            float x[VEC];
-            Row<DT>::Type::unpack(row.load(s), x);
+    // ---- the largest logit ----
+    float M = -INFINITY;
+    for (int s = tid; s < row.slots; s += BLOCK) {
+        float x[VEC];
+        Type::unpack(row.load(s), x);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) taken += logit_key(x[i]) != 0;
-        }
-        const unsigned long long n = block_sum<BLOCK>((unsigned long long)taken, part);
-        if (n > (unsigned long long)top_k)
-            floor = select_nth<BLOCK>(EachElement<DT, BLOCK>{row, 0, row.slots}, FIRST_WORD, top_k, sel);
+        for (int i = 0; i < VEC; ++i) M = fmaxf(M, x[i]);
+    }
+    M = block_max<BLOCK>(M, fpart);
+    if (M == -INFINITY) {
+        if (tid == 0) answer(-1, NAN);
+        return;
+    }
+    const Weight weight(T, M, a.unit);
+    const EachElement<DT, BLOCK> elements{row, 0, row.slots};
+    unsigned long long floor = FIRST_WORD;
+
+    if (top_k > LOGITS_MAX_TOP && top_k < a.V) {
+        unsigned long long n = 0;
+        elements([&](unsigned long long word, float) { n += word >= FIRST_WORD; });
+        n = block_sum<BLOCK>(n, part);
+        if (n > (unsigned long long)top_k) floor = select_nth<BLOCK>(elements, FIRST_WORD, top_k, lds.mass);
     }
     if (top_p < 1.f) {
-        unsigned long long mass = 0;
-        for (int s = tid; s < row.slots; s += BLOCK) {
-            float x[VEC];
-            Row<DT>::Type::unpack(row.load(s), x);
+        const float width = fminf((float)(MASS_BINS - 1) / (18.f * fminf(T, FLT_MAX / 32.f)), FLT_MAX);
+        auto bin_of = [&](float z) {
+            const float b = (M - z) * width;                        // descending logits have ascending bins, whatever is rounded
+            return b < (float)(MASS_BINS - 1) ? (int)b : MASS_BINS - 1;      // NaN (+inf twice): the last
+        };
+        for (int b = tid; b < MASS_BINS; b += BLOCK) lds.mass.mass[b] = 0;
+        __syncthreads();
+        unsigned long long far = 0;
+        elements([&](unsigned long long word, float z) {
+            if (word < floor) return;
+            const unsigned long long w = weight.units(z);
+            const int b = bin_of(z);
+            if (b < MASS_BINS - 1) atomicAdd(&lds.mass.mass[b], w);
+            else far += w;
+        });
+        __syncthreads();
+        unsigned long long near = 0;
+        for (int b = tid; b < MASS_BINS; b += BLOCK) near += lds.mass.mass[b];
+        const unsigned long long all = block_sum<BLOCK>(near + far, part);
+        const unsigned long long target = wanted(top_p, all);
+        // the bin of the border: thread t sums bins 4t .. 4t + 3
+        constexpr int PER = MASS_BINS / BLOCK;
+        unsigned long long w[PER], sum = 0, total;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i)
-                if (order_word(logit_key(x[i]), row.index(s, i)) >= floor) mass += weight(x[i]);
+        for (int i = 0; i < PER; ++i) {
+            w[i] = lds.mass.mass[tid * PER + i];
+            sum += w[i];
         }
-        mass = block_sum<BLOCK>(mass, part);
-        const double target = ceil((double)top_p * (double)mass);
-        floor = select_word<BLOCK, true>(EachElement<DT, BLOCK>{row, 0, row.slots}, floor, target >= 1.0 ? (unsigned long long)target : 1ull, sel, weight);
+        unsigned long long before = scan<BLOCK>(sum, part, total);
+        if (tid == 0) lds.mass.bin = MASS_BINS - 1;
+        __syncthreads();
+        if (before < target && before + sum >= target) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                if (before < target && before + w[i] >= target) {
+                    lds.mass.bin = (unsigned)(tid * PER + i);
+                    lds.mass.above = before;
+                }
+                before += w[i];
+            }
+        }
+        __syncthreads();
+        const int border = (int)lds.mass.bin;
+        const unsigned long long above = lds.mass.above;
+        __syncthreads();
+        bool listed = border < MASS_BINS - 1;
+        if (listed) {
+            if (tid == 0) lds.top.n = 0;
+            __syncthreads();
+            elements([&](unsigned long long word, float z) {
+                if (word >= floor && bin_of(z) == border) {
+                    const unsigned at = atomicAdd(&lds.top.n, 1u);
+                    if (at < BORDER_LIST) lds.top.list[at] = word;
+                }
+            });
+            __syncthreads();
+            const unsigned n = lds.top.n;
+            listed = n <= BORDER_LIST;
+            __syncthreads();
+            if (listed) {
+                // every listed word's mass, and the mass before it in the order
+                unsigned long long *masses = lds.top.list + BORDER_LIST;
+                for (unsigned i = tid; i < n; i += BLOCK) masses[i] = weight.units(key_logit((unsigned)(lds.top.list[i] >> 32)));
+                if (tid == 0) part[0] = floor;
+                __syncthreads();
+                for (unsigned i = tid; i < n; i += BLOCK) {
+                    const unsigned long long mine = lds.top.list[i];
+                    unsigned long long lead = above;
+                    for (unsigned j = 0; j < n; ++j) lead += lds.top.list[j] > mine ? masses[j] : 0;
+                    if (lead < target && lead + masses[i] >= target) part[0] = mine;      // one word
+                }
+                __syncthreads();
+                floor = part[0];
+                __syncthreads();
+            }
+        }
+        if (!listed) floor = select_word<BLOCK, true>(elements, floor, target, lds.mass, [&](float z) { return weight.units(z); });
     }
 
-    // the mass of what is kept, by wavefront: wavefront v owns a run of whole slots
+    // ---- the mass of what is kept, by wavefront: each owns a run of whole slots ----
     const int chunk = ((row.slots + BLOCK - 1) / BLOCK) * 64;
     const int s0 = wave * chunk, s1 = min(s0 + chunk, row.slots);
+    // logits below `least` are not kept: the floor's, or what min_p leaves with room for rounding
+    float least = key_logit(max((unsigned)(floor >> 32), 0x00800000u));
+    if (min_p > 0.f && T < INFINITY) {
+        const double edge = (double)M + (double)T * (log((double)fminf(min_p, 1.f)) * (1.0 + 1e-9) - 1e-9);
+        least = fmaxf(least, (float)(edge - fabs(edge) * 1e-6));
+    }
+    const bool filtered = min_p > 0.f;
     auto kept_units = [&](float x, int index) -> unsigned long long {
-        const unsigned long long word = order_word(logit_key(x), index);
-        if (word < floor || word < FIRST_WORD) return 0;
-        const double w = weight.real(x);
-        return word == first || !(w < (double)min_p) ? weight.units(w) : 0;
+        if (!(x >= least) || order_word(logit_key(x), index) < floor) return 0;
+        if (filtered && weight.real(x) < (double)min_p) return 0;
+        return weight.units(x);
     };
     auto slot_units = [&](int s) {
-        unsigned long long u = 0;
+        unsigned long long sum = 0;
         if (s < s1) {
             float x[VEC];
-            Row<DT>::Type::unpack(row.load(s), x);
+            Type::unpack(row.load(s), x);
+            float t = x[0];
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) u += kept_units(x[i], row.index(s, i));
+            for (int i = 1; i < VEC; ++i) t = fmaxf(t, x[i]);
+            if (t >= least) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) sum += kept_units(x[i], row.index(s, i));
+            }
         }
-        return u;
+        return sum;
     };
     unsigned long long mass = 0;
     for (int s = s0 + lane; s < s1; s += 64) mass += slot_units(s);
@@ -129,10 +321,7 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
         if (v < wave) before += part[v];
         total += part[v];
     }
-    const float u = a.u[r];
-    const double drawn = (double)(u > 0.f ? fminf(u, 1.f - 0x1p-24f) : 0.f) * (double)total;
-    unsigned long long target = (unsigned long long)drawn;
-    if (target >= total) target = total - 1;
+    const unsigned long long target = drawn(u, total);
     if (before > target || before + mass <= target) return;      // uniform for the wavefront: one is left
     for (int s = s0 + lane; s - lane < s1; s += 64) {
         const unsigned long long mine = slot_units(s);
@@ -147,14 +336,11 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
             unsigned long long at = before + run - mine;
             if (at <= target && at + mine > target) {
                 float x[VEC];
-                Row<DT>::Type::unpack(row.load(s), x);
+                Type::unpack(row.load(s), x);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
                     const unsigned long long w = kept_units(x[i], row.index(s, i));
-                    if (at <= target && at + w > target) {
-                        a.tokens[r] = row.index(s, i);
-                        if (a.logprob) a.logprob[r] = (float)log(weight.real(x[i]) * a.unit / (double)total);
-                    }
+                    if (at <= target && at + w > target) answer(row.index(s, i), weight.log_share(x[i], total));
                     at += w;
                 }
             }
@@ -185,8 +371,7 @@ int easgd_sample_tokens(const void *logits, int dtype, size_t rows, int V, size_
     if (rows == 0) return EASGD_OK;
     int log2_v = 0;
     while ((1 << log2_v) < V) ++log2_v;
-    const double unit = (double)(1ull << (62 - log2_v < 51 ? 62 - log2_v : 51));
-    const SampleArgs a = {logits, ld, V, u, temperature, top_k, top_p, min_p, tokens, logprob, unit};
+    const SampleArgs a = {logits, ld, V, u, temperature, top_k, top_p, min_p, tokens, logprob, 62 - log2_v < 51 ? 62 - log2_v : 51};
     by_dtype(dtype, [&](auto dt) {
         EASGD_LAUNCH((sample_kernel<decltype(dt)::value, 512>), dim3((unsigned)rows), dim3(512), 0, static_cast<hipStream_t>(stream), a);
     });
