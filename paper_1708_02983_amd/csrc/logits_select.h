@@ -99,18 +99,33 @@ __device__ __forceinline__ unsigned long long select_nth(E each, unsigned long l
     return select_word<BLOCK, false>(each, floor, (unsigned long long)n, lds, [](float) { return 0ull; });
 }
 
+// Every slot of [s0, s1) through the threads of a block, eight loads under way at a time: f(raw, slot).
+template <int DT, int BLOCK, typename F> __device__ __forceinline__ void each_slot(const Row<DT> &row, int s0, int s1, F f)
+{
+    constexpr int DEEP = 8;
+    for (int s = s0 + (int)threadIdx.x; s < s1; s += DEEP * BLOCK) {
+        uint4 v[DEEP];
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i)
+            if (s + i * BLOCK < s1) v[i] = row.load(s + i * BLOCK);
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i)
+            if (s + i * BLOCK < s1) f(v[i], s + i * BLOCK);
+    }
+}
+
 // the elements of slots [s0, s1) of a row, as select_word takes them
 template <int DT, int BLOCK> struct EachElement {
     const Row<DT> &row;
     int s0, s1;
     template <typename F> __device__ __forceinline__ void operator()(F f) const
     {
-        for (int s = s0 + threadIdx.x; s < s1; s += BLOCK) {
+        each_slot<DT, BLOCK>(row, s0, s1, [&](const uint4 &raw, int s) {
             float x[Row<DT>::VEC];
-            Row<DT>::Type::unpack(row.load(s), x);
+            Row<DT>::Type::unpack(raw, x);
 #pragma unroll
             for (int i = 0; i < Row<DT>::VEC; ++i) f(order_word(logit_key(x[i]), row.index(s, i)), x[i]);
-        }
+        });
     }
 };
 

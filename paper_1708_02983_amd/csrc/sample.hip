@@ -25,53 +25,56 @@ struct SampleArgs {
     int unit;                 // log2 of the units of mass in the largest weight
 };
 
-// w = 2^y with y = (z - max) log2(e) / T <= 0: 2^n 2^f with |f| <= 1/2 and the Taylor polynomial of 2^f, whose remainder is below
-// (ln 2 / 2)^12 / 12! = 6e-15.  Below 2^-200 the value no longer matters (a unit is at least 2^-51, min_p at least 2^-149).
+// w = 2^y with y = (z - max) log2(e) / T <= 0, in 64 bits: y = j / 512 + f with |f| <= 2^-10 (adding 1.5 * 2^43 rounds to the
+// multiple of 2^-9 and leaves j in the low bits), 2^(j / 512) from a table in LDS and an exponent, 2^f from its Taylor polynomial,
+// whose remainder is below (2^-10 ln 2)^4 / 24 = 9e-15.  Below 2^-200 the value no longer matters (a unit is at least 2^-51 of
+// the largest weight, min_p at least 2^-149).
+static constexpr int WEIGHT_TABLE = 512;
 struct Weight {
     double scale, max;        // log2(e) / T
+    float top;                // the largest logit
     int unit;
     bool infinite;            // the largest logit is +inf: logits are in or out
-    __device__ __forceinline__ Weight(float T, float top, int unit)
-        : scale(LOG2E / (double)T), max((double)top), unit(unit), infinite(top == INFINITY) {}
-    __device__ __forceinline__ void split(float z, double &p, int &n) const
+    const double *table;      // units of 2^(i / 512)
+    __device__ __forceinline__ Weight(float T, float top, int unit, const double *table)
+        : scale(LOG2E / (double)T), max((double)top), top(top), unit(unit), infinite(top == INFINITY), table(table) {}
+    // every thread of the block; ends with a barrier
+    template <int BLOCK> static __device__ __forceinline__ void fill(double *table, int unit)
     {
-        const double y = fmax(((double)z - max) * scale, -200.0), whole = rint(y), f = y - whole;
-        n = (int)whole;
-        p = 4.4455382718708101e-10;
-        p = fma(p, f, 7.0549116208011209e-09);
-        p = fma(p, f, 1.0178086009239696e-07);
-        p = fma(p, f, 1.3215486790144305e-06);
-        p = fma(p, f, 1.5252733804059838e-05);
-        p = fma(p, f, 1.5403530393381606e-04);
-        p = fma(p, f, 1.3333558146428441e-03);
-        p = fma(p, f, 9.6181291076284769e-03);
-        p = fma(p, f, 5.5504108664821576e-02);
-        p = fma(p, f, 2.4022650695910069e-01);
-        p = fma(p, f, 6.9314718055994529e-01);
-        p = fma(p, f, 1.0);
+        for (int i = threadIdx.x; i < WEIGHT_TABLE; i += BLOCK) table[i] = power(unit) * exp2((double)i / WEIGHT_TABLE);
+        __syncthreads();
     }
     static __device__ __forceinline__ double power(int n) { return __builtin_bit_cast(double, (unsigned long long)(n + 1023) << 52); }
-    // adding 2^52 rounds to the nearest whole number and leaves it in the low bits of the sum (units <= 2^51)
-    __device__ __forceinline__ unsigned long long units(float z) const
+    // 2^y units as factors that are still to be multiplied
+    __device__ __forceinline__ void split(float z, double &a, double &b) const
     {
-        if (infinite) return (double)z == max ? 1ull << unit : 0ull;      // uniform
-        double p;
-        int n;
-        split(z, p, n);
-        return __builtin_bit_cast(unsigned long long, fma(p, power(n + unit), 0x1p52)) - 0x4330000000000000ull;
+        const double y = fmax(((double)z - max) * scale, -200.0), t = y + 0x1.8p43, f = y - (t - 0x1.8p43);
+        const int j = (int)(unsigned)__builtin_bit_cast(unsigned long long, t);
+        const unsigned long long e = __builtin_bit_cast(unsigned long long, table[j & (WEIGHT_TABLE - 1)]);
+        a = __builtin_bit_cast(double, e + ((unsigned long long)(unsigned)((j >> 9) << 20) << 32));
+        b = fma(fma(fma(5.5504108664821576e-02, f, 2.4022650695910069e-01), f, 6.9314718055994529e-01), f, 1.0);
     }
+    // adding 2^52 rounds to the nearest whole number and leaves it in the low bits of the sum (units <= 2^51)
+    static constexpr unsigned long long BIAS = 0x4330000000000000ull;
+    __device__ __forceinline__ unsigned long long biased_units(float z) const
+    {
+        if (infinite) return BIAS + (z == top ? 1ull << unit : 0ull);        // uniform
+        double a, b;
+        split(z, a, b);
+        return __builtin_bit_cast(unsigned long long, fma(a, b, 0x1p52));
+    }
+    __device__ __forceinline__ unsigned long long units(float z) const { return biased_units(z) - BIAS; }
     __device__ __forceinline__ double real(float z) const
     {
-        if (infinite) return (double)z == max ? 1.0 : 0.0;
-        double p;
-        int n;
-        split(z, p, n);
-        return p * power(n);
+        if (infinite) return z == top ? 1.0 : 0.0;
+        double a, b;
+        split(z, a, b);
+        return a * b * power(-unit);
     }
     // log of w over a mass
     __device__ __forceinline__ float log_share(float z, unsigned long long mass) const
     {
-        const double ln_w = (double)z == max ? 0.0 : ((double)z - max) * scale * 0.69314718055994530942;
+        const double ln_w = z == top ? 0.0 : ((double)z - max) * scale * 0.69314718055994530942;
         return (float)(ln_w - log((double)mass * power(-unit)));
     }
 };
@@ -131,6 +134,7 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
     __shared__ unsigned long long part[WAVES];
     __shared__ unsigned long long words[LOGITS_MAX_TOP], mass_of[LOGITS_MAX_TOP];
     __shared__ float fpart[WAVES];
+    __shared__ double table[WEIGHT_TABLE];
     const size_t r = blockIdx.x;
     const Row<DT> row(a.logits, r, a.ld, a.V);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -140,6 +144,8 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
         a.tokens[r] = token;
         if (a.logprob) a.logprob[r] = lp;
     };
+
+    Weight::fill<BLOCK>(table, a.unit);
 
     // ---- few tokens: all further work is on their order words ----
     if (top_k >= 1 && top_k <= LOGITS_MAX_TOP) {
@@ -152,7 +158,7 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
         const unsigned i = tid;
         if (i < n) words[rank_of(lds.top.list, n, lds.top.list[i])] = lds.top.list[i];
         __syncthreads();
-        const Weight weight(T, key_logit((unsigned)(words[0] >> 32)), a.unit);
+        const Weight weight(T, key_logit((unsigned)(words[0] >> 32)), a.unit, table);
         const float z = i < n ? key_logit((unsigned)(words[i] >> 32)) : 0.f;
         unsigned long long w = i < n ? weight.units(z) : 0, all;
         const unsigned long long before = scan<BLOCK>(w, part, all);
@@ -180,18 +186,18 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
 
     // ---- the largest logit ----
     float M = -INFINITY;
-    for (int s = tid; s < row.slots; s += BLOCK) {
+    each_slot<DT, BLOCK>(row, 0, row.slots, [&](const uint4 &raw, int) {
         float x[VEC];
-        Type::unpack(row.load(s), x);
+        Type::unpack(raw, x);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) M = fmaxf(M, x[i]);
-    }
+    });
     M = block_max<BLOCK>(M, fpart);
     if (M == -INFINITY) {
         if (tid == 0) answer(-1, NAN);
         return;
     }
-    const Weight weight(T, M, a.unit);
+    const Weight weight(T, M, a.unit, table);
     const EachElement<DT, BLOCK> elements{row, 0, row.slots};
     unsigned long long floor = FIRST_WORD;
 
@@ -290,63 +296,72 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
         const double edge = (double)M + (double)T * (log((double)fminf(min_p, 1.f)) * (1.0 + 1e-9) - 1e-9);
         least = fmaxf(least, (float)(edge - fabs(edge) * 1e-6));
     }
-    const bool filtered = min_p > 0.f;
+    const bool filtered = min_p > 0.f, whole = floor == FIRST_WORD && !filtered;
     auto kept_units = [&](float x, int index) -> unsigned long long {
         if (!(x >= least) || order_word(logit_key(x), index) < floor) return 0;
         if (filtered && weight.real(x) < (double)min_p) return 0;
         return weight.units(x);
     };
-    auto slot_units = [&](int s) {
+    auto slot_units = [&](const uint4 &raw, int s) {
         unsigned long long sum = 0;
-        if (s < s1) {
-            float x[VEC];
-            Type::unpack(row.load(s), x);
-            float t = x[0];
+        float x[VEC];
+        Type::unpack(raw, x);
+        if (whole) {                                    // uniform: masked logits (-inf and NaN) are all that is not kept
 #pragma unroll
-            for (int i = 1; i < VEC; ++i) t = fmaxf(t, x[i]);
-            if (t >= least) {
+            for (int i = 0; i < VEC; ++i) sum += x[i] >= -FLT_MAX ? weight.biased_units(x[i]) : Weight::BIAS;
+            return sum - VEC * Weight::BIAS;
+        }
+        float t = x[0];
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) sum += kept_units(x[i], row.index(s, i));
-            }
+        for (int i = 1; i < VEC; ++i) t = fmaxf(t, x[i]);
+        if (t >= least) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) sum += kept_units(x[i], row.index(s, i));
         }
         return sum;
     };
     unsigned long long mass = 0;
-    for (int s = s0 + lane; s < s1; s += 64) mass += slot_units(s);
+    constexpr int DEEP = 8;
+    for (int s = s0 + lane; s < s1; s += DEEP * 64) {
+        uint4 v[DEEP];
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i)
+            if (s + i * 64 < s1) v[i] = row.load(s + i * 64);
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i)
+            if (s + i * 64 < s1) mass += slot_units(v[i], s + i * 64);
+    }
     mass = wave_sum(mass);
     if (lane == 0) part[wave] = mass;
     __syncthreads();
     unsigned long long before = 0, total = 0;
-    for (int v = 0; v < WAVES; ++v) {
-        if (v < wave) before += part[v];
-        total += part[v];
-    }
+    for (int v = 0; v < WAVES; ++v) total += part[v];
     const unsigned long long target = drawn(u, total);
-    if (before > target || before + mass <= target) return;      // uniform for the wavefront: one is left
-    for (int s = s0 + lane; s - lane < s1; s += 64) {
-        const unsigned long long mine = slot_units(s);
-        unsigned long long run = mine;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const unsigned long long up = __shfl_up(run, o);
-            if (lane >= o) run += up;
+    int chosen = 0;
+    while (chosen < WAVES - 1 && before + part[chosen] <= target) before += part[chosen++];
+    __syncthreads();
+    // the chosen wavefront's run, a slot per thread of the whole block
+    const int end = min((chosen + 1) * chunk, row.slots);
+    for (int s = chosen * chunk + tid; s - tid < end; s += BLOCK) {            // uniform
+        uint4 raw = Row<DT>::empty();
+        unsigned long long mine = 0, all;
+        if (s < end) {
+            raw = row.load(s);
+            mine = slot_units(raw, s);
         }
-        const unsigned long long all = __shfl(run, 63);
-        if (before + all > target) {
-            unsigned long long at = before + run - mine;
-            if (at <= target && at + mine > target) {
-                float x[VEC];
-                Type::unpack(row.load(s), x);
+        unsigned long long at = before + scan<BLOCK>(mine, part, all);
+        if (at <= target && target - at < mine) {
+            float x[VEC];
+            Type::unpack(raw, x);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    const unsigned long long w = kept_units(x[i], row.index(s, i));
-                    if (at <= target && at + w > target) answer(row.index(s, i), weight.log_share(x[i], total));
-                    at += w;
-                }
+            for (int i = 0; i < VEC; ++i) {
+                const unsigned long long w = kept_units(x[i], row.index(s, i));
+                if (at <= target && target - at < w) answer(row.index(s, i), weight.log_share(x[i], total));
+                at += w;
             }
-            return;
         }
         before += all;
+        if (before > target) return;
     }
 }
 
@@ -372,8 +387,16 @@ int easgd_sample_tokens(const void *logits, int dtype, size_t rows, int V, size_
     int log2_v = 0;
     while ((1 << log2_v) < V) ++log2_v;
     const SampleArgs a = {logits, ld, V, u, temperature, top_k, top_p, min_p, tokens, logprob, 62 - log2_v < 51 ? 62 - log2_v : 51};
+    const int slots = most_slots(dtype, V);
     by_dtype(dtype, [&](auto dt) {
-        EASGD_LAUNCH((sample_kernel<decltype(dt)::value, 512>), dim3((unsigned)rows), dim3(512), 0, static_cast<hipStream_t>(stream), a);
+        constexpr int DT = decltype(dt)::value;
+        const auto launch = [&](auto block) {
+            constexpr int BLOCK = decltype(block)::value;
+            EASGD_LAUNCH((sample_kernel<DT, BLOCK>), dim3((unsigned)rows), dim3(BLOCK), 0, static_cast<hipStream_t>(stream), a);
+        };
+        if (slots <= 1024) launch(std::integral_constant<int, 256>{});
+        else if (slots <= 4096) launch(std::integral_constant<int, 512>{});
+        else launch(std::integral_constant<int, 1024>{});
     });
     return check_launch(name);
 }
