@@ -171,8 +171,51 @@ template <int BLOCK> __device__ __forceinline__ unsigned keep_from(TopLds &lds, 
     return lds.n;
 }
 
-// The order words of the first k (<= LOGITS_MAX_TOP) elements of slots [s0, s1), unordered, at the front of lds.list; returns how
-// many there are (fewer than k where fewer are above -inf).  seen(x, slot) is called for every slot by whole wavefronts
+// The list's n words in the order, at its front: every word's rank is the number of larger ones.  n <= 2 * BLOCK; only the first
+// k are wanted.  Ends with a barrier.
+template <int BLOCK> __device__ __forceinline__ void rank_list(TopLds &lds, unsigned n, unsigned k)
+{
+    const unsigned i = threadIdx.x, j = i + BLOCK;
+    const unsigned long long one = i < n ? lds.list[i] : 0, two = j < n ? lds.list[j] : 0;
+    unsigned rank_one = 0, rank_two = 0;
+    if (n <= BLOCK) {                                   // uniform
+#pragma unroll 4
+        for (unsigned q = 0; q < n; ++q) rank_one += lds.list[q] > one;
+    } else {
+#pragma unroll 4
+        for (unsigned q = 0; q < n; ++q) {
+            const unsigned long long w = lds.list[q];
+            rank_one += w > one;
+            rank_two += w > two;
+        }
+    }
+    __syncthreads();
+    if (i < n && rank_one < k) lds.list[rank_one] = one;
+    if (j < n && rank_two < k) lds.list[rank_two] = two;
+    __syncthreads();
+}
+
+// A floor that at least k of the threads' logits t reach (k <= number of threads with t > -inf), a little below the k-th largest:
+// the lower edge of its bin among 2048 of equal width between the smallest and the largest t.  lds.select is scratch.
+template <int BLOCK> __device__ __forceinline__ float floor_of(float t, unsigned k, TopLds &lds)
+{
+    float *part = reinterpret_cast<float *>(lds.select.part);
+    const float top = block_max<BLOCK>(t, part), bottom = -block_max<BLOCK>(t > -INFINITY ? -t : -INFINITY, part);
+    // halves: the range of all finite logits fits
+    const float range = top * 0.5f - bottom * 0.5f;
+    if (!(range > 0.f) || range == INFINITY) return bottom;
+    const float width = (float)(SELECT_BINS - 1) / range;
+    for (int b = threadIdx.x; b < SELECT_BINS; b += BLOCK) lds.select.count[b] = 0;
+    __syncthreads();
+    if (t > -INFINITY) atomicAdd(&lds.select.count[(int)fminf((t * 0.5f - bottom * 0.5f) * width, (float)(SELECT_BINS - 1))], 1u);
+    __syncthreads();
+    select_bin<BLOCK, false>(lds.select, SELECT_BINS, 0, k);
+    const float edge = ((float)lds.select.bin / width + bottom * 0.5f) * 2.f, room = (fabsf(top) + fabsf(bottom)) * 1e-6f;
+    return width < INFINITY && edge - room > bottom ? edge - room : bottom;
+}
+
+// The order words of the first k (<= LOGITS_MAX_TOP) elements of slots [s0, s1), in the order, at the front of lds.list; returns
+// how many there are (fewer than k where fewer are above -inf).  seen(x, slot) is called for every slot by whole wavefronts
 // (an empty slot where a lane has none).  Ends with a barrier.
 template <int DT, int BLOCK, typename F>
 __device__ __forceinline__ unsigned first_of(const Row<DT> &row, int s0, int s1, unsigned k, TopLds &lds, F seen)
@@ -190,7 +233,7 @@ __device__ __forceinline__ unsigned first_of(const Row<DT> &row, int s0, int s1,
     load(s0 + tid);
     unsigned long long floor = FIRST_WORD;
     if (tid == 0) lds.n = 0;
-    if ((s1 - s0) * VEC > TOP_LIST) {
+    if ((s1 - s0) * VEC > TOP_LIST / 4) {
         float t = -INFINITY;
 #pragma unroll
         for (int i = 0; i < DEEP; ++i) {
@@ -199,10 +242,7 @@ __device__ __forceinline__ unsigned first_of(const Row<DT> &row, int s0, int s1,
 #pragma unroll
             for (int j = 0; j < VEC; ++j) t = fmaxf(t, x[j]);
         }
-        lds.list[tid] = order_word(logit_key(t), tid);
-        const unsigned some = __syncthreads_count(t > -INFINITY);
-        if (some >= k) floor = select_nth<BLOCK>(EachListed{lds.list, (unsigned)BLOCK, BLOCK}, FIRST_WORD, k, lds.select) >> 32 << 32;
-        if (floor < FIRST_WORD) floor = FIRST_WORD;
+        if ((unsigned)__syncthreads_count(t > -INFINITY) >= k) floor = order_word(logit_key(floor_of<BLOCK>(t, k, lds)), -1);
     }
     __syncthreads();
     float least = 0.f;                                  // the floor as a logit; every logit that may be taken is at least -FLT_MAX
@@ -266,21 +306,13 @@ __device__ __forceinline__ unsigned first_of(const Row<DT> &row, int s0, int s1,
             }
         });
         __syncthreads();
-        return min(lds.n, k);
-    }
-    if (n > k) {
+        n = min(lds.n, k);
+    } else if (n > 512) {                               // more than a look at every pair is worth
         floor = select_nth<BLOCK>(EachListed{lds.list, n, BLOCK}, floor, k, lds.select);
         n = keep_from<BLOCK>(lds, n, floor);
     }
-    return n;
-}
-
-// The number of words of lds.list[0..n) before each of the threads' own (thread i's word is word i).
-__device__ __forceinline__ unsigned rank_of(const unsigned long long *list, unsigned n, unsigned long long word)
-{
-    unsigned rank = 0;
-    for (unsigned j = 0; j < n; ++j) rank += list[j] > word;
-    return rank;
+    rank_list<BLOCK>(lds, n, k);
+    return min(n, k);
 }
 
 }  // namespace easgd

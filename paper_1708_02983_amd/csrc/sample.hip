@@ -71,6 +71,15 @@ struct Weight {
         split(z, a, b);
         return a * b * power(-unit);
     }
+    // units, or 0 where there is a limit (in units, not whole) and w is below it
+    __device__ __forceinline__ unsigned long long units_from(float z, bool limited, double limit) const
+    {
+        if (infinite) return units(z);                  // w is 0 or 1
+        double a, b;
+        split(z, a, b);
+        if (limited && a * b < limit) return 0;
+        return __builtin_bit_cast(unsigned long long, fma(a, b, 0x1p52)) - BIAS;
+    }
     // log of w over a mass
     __device__ __forceinline__ float log_share(float z, unsigned long long mass) const
     {
@@ -132,7 +141,7 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
     using Type = LogitType<DT>;
     __shared__ SampleLds lds;
     __shared__ unsigned long long part[WAVES];
-    __shared__ unsigned long long words[LOGITS_MAX_TOP], mass_of[LOGITS_MAX_TOP];
+    __shared__ unsigned long long mass_of[LOGITS_MAX_TOP];
     __shared__ float fpart[WAVES];
     __shared__ double table[WEIGHT_TABLE];
     const size_t r = blockIdx.x;
@@ -154,10 +163,8 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
             if (tid == 0) answer(n ? (int)~(unsigned)lds.top.list[0] : -1, n ? 0.f : NAN);
             return;
         }
-        // by rank
         const unsigned i = tid;
-        if (i < n) words[rank_of(lds.top.list, n, lds.top.list[i])] = lds.top.list[i];
-        __syncthreads();
+        const unsigned long long *words = lds.top.list;
         const Weight weight(T, key_logit((unsigned)(words[0] >> 32)), a.unit, table);
         const float z = i < n ? key_logit((unsigned)(words[i] >> 32)) : 0.f;
         unsigned long long w = i < n ? weight.units(z) : 0, all;
@@ -198,45 +205,49 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
         return;
     }
     const Weight weight(T, M, a.unit, table);
-    const EachElement<DT, BLOCK> elements{row, 0, row.slots};
     unsigned long long floor = FIRST_WORD;
 
-    if (top_k > LOGITS_MAX_TOP && top_k < a.V) {
-        unsigned long long n = 0;
-        elements([&](unsigned long long word, float) { n += word >= FIRST_WORD; });
-        n = block_sum<BLOCK>(n, part);
-        if (n > (unsigned long long)top_k) floor = select_nth<BLOCK>(elements, FIRST_WORD, top_k, lds.mass);
-    }
-    if (top_p < 1.f) {
-        const float width = fminf((float)(MASS_BINS - 1) / (18.f * fminf(T, FLT_MAX / 32.f)), FLT_MAX);
+    // The word at which the weights (masses, or 1 each) of the words from `floor` on reach what `want` says of their sum (0: no
+    // such border).  The weights are summed in bins of equal width below the largest logit; the bin of the border is listed, and
+    // every listed word's sum of weights before it taken in the order.  Where the border is further below than the bins reach,
+    // or its bin holds more words than the list, the order words are walked down digit by digit.
+    auto border_word = [&](auto by_mass, float reach, auto want) -> unsigned long long {
+        constexpr bool BY_MASS = decltype(by_mass)::value;
+        auto weight_of = [&](float z) { return BY_MASS ? weight.units(z) : 1ull; };
+        const float width = fminf((float)(MASS_BINS - 1) / reach, FLT_MAX);
         auto bin_of = [&](float z) {
             const float b = (M - z) * width;                        // descending logits have ascending bins, whatever is rounded
             return b < (float)(MASS_BINS - 1) ? (int)b : MASS_BINS - 1;      // NaN (+inf twice): the last
         };
+        const float floor_logit = key_logit(max((unsigned)(floor >> 32), 0x00800000u));
+        auto above_floor = [&](float z, int index) {                // the floor's index is the last of its value that counts
+            return z > floor_logit || (z == floor_logit && (unsigned)index <= ~(unsigned)floor);
+        };
         for (int b = tid; b < MASS_BINS; b += BLOCK) lds.mass.mass[b] = 0;
         __syncthreads();
         unsigned long long far = 0;
-        elements([&](unsigned long long word, float z) {
-            if (word < floor) return;
-            const unsigned long long w = weight.units(z);
-            const int b = bin_of(z);
-            if (b < MASS_BINS - 1) atomicAdd(&lds.mass.mass[b], w);
-            else far += w;
+        each_slot<DT, BLOCK>(row, 0, row.slots, [&](const uint4 &raw, int s) {
+            float x[VEC];
+            Type::unpack(raw, x);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                if (!above_floor(x[i], row.index(s, i))) continue;
+                const int b = bin_of(x[i]);
+                if (b < MASS_BINS - 1) atomicAdd(&lds.mass.mass[b], weight_of(x[i]));
+                else far += weight_of(x[i]);
+            }
         });
         __syncthreads();
-        unsigned long long near = 0;
-        for (int b = tid; b < MASS_BINS; b += BLOCK) near += lds.mass.mass[b];
-        const unsigned long long all = block_sum<BLOCK>(near + far, part);
-        const unsigned long long target = wanted(top_p, all);
-        // the bin of the border: thread t sums bins 4t .. 4t + 3
         constexpr int PER = MASS_BINS / BLOCK;
-        unsigned long long w[PER], sum = 0, total;
+        unsigned long long w[PER], sum = 0, near;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             w[i] = lds.mass.mass[tid * PER + i];
             sum += w[i];
         }
-        unsigned long long before = scan<BLOCK>(sum, part, total);
+        unsigned long long before = scan<BLOCK>(sum, part, near);
+        const unsigned long long target = want(near + block_sum<BLOCK>(far, part));
+        if (target == 0) return floor;
         if (tid == 0) lds.mass.bin = MASS_BINS - 1;
         __syncthreads();
         if (before < target && before + sum >= target) {
@@ -253,39 +264,53 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
         const int border = (int)lds.mass.bin;
         const unsigned long long above = lds.mass.above;
         __syncthreads();
-        bool listed = border < MASS_BINS - 1;
-        if (listed) {
-            if (tid == 0) lds.top.n = 0;
+        if (border < MASS_BINS - 1) {
+            if (tid == 0) {
+                lds.top.n = 0;
+                part[0] = floor;
+            }
             __syncthreads();
-            elements([&](unsigned long long word, float z) {
-                if (word >= floor && bin_of(z) == border) {
-                    const unsigned at = atomicAdd(&lds.top.n, 1u);
-                    if (at < BORDER_LIST) lds.top.list[at] = word;
+            // logits of the border's bin, with room for the rounding of M - z and of its product
+            const float high = M - (float)border / width * 0.999999f + fabsf(M) * 1e-6f, low = M - (float)(border + 1) / width * 1.000001f - fabsf(M) * 1e-6f;
+            each_slot<DT, BLOCK>(row, 0, row.slots, [&](const uint4 &raw, int s) {
+                float x[VEC];
+                Type::unpack(raw, x);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    if (x[i] <= high && x[i] >= low && bin_of(x[i]) == border && above_floor(x[i], row.index(s, i))) {
+                        const unsigned at = atomicAdd(&lds.top.n, 1u);
+                        if (at < BORDER_LIST) lds.top.list[at] = order_word(logit_key(x[i]), row.index(s, i));
+                    }
                 }
             });
             __syncthreads();
             const unsigned n = lds.top.n;
-            listed = n <= BORDER_LIST;
-            __syncthreads();
-            if (listed) {
-                // every listed word's mass, and the mass before it in the order
-                unsigned long long *masses = lds.top.list + BORDER_LIST;
-                for (unsigned i = tid; i < n; i += BLOCK) masses[i] = weight.units(key_logit((unsigned)(lds.top.list[i] >> 32)));
-                if (tid == 0) part[0] = floor;
+            if (n <= BORDER_LIST) {
+                unsigned long long *weights = lds.top.list + BORDER_LIST;
+                for (unsigned i = tid; i < n; i += BLOCK) weights[i] = weight_of(key_logit((unsigned)(lds.top.list[i] >> 32)));
                 __syncthreads();
                 for (unsigned i = tid; i < n; i += BLOCK) {
                     const unsigned long long mine = lds.top.list[i];
                     unsigned long long lead = above;
-                    for (unsigned j = 0; j < n; ++j) lead += lds.top.list[j] > mine ? masses[j] : 0;
-                    if (lead < target && lead + masses[i] >= target) part[0] = mine;      // one word
+#pragma unroll 4
+                    for (unsigned j = 0; j < n; ++j) lead += lds.top.list[j] > mine ? weights[j] : 0;
+                    if (lead < target && lead + weights[i] >= target) part[0] = mine;      // one word
                 }
                 __syncthreads();
-                floor = part[0];
+                const unsigned long long found = part[0];
                 __syncthreads();
+                return found;
             }
         }
-        if (!listed) floor = select_word<BLOCK, true>(elements, floor, target, lds.mass, [&](float z) { return weight.units(z); });
-    }
+        __syncthreads();
+        const EachElement<DT, BLOCK> elements{row, 0, row.slots};
+        return select_word<BLOCK, BY_MASS>(elements, floor, target, lds.mass, weight_of);
+    };
+    const float cool = fminf(T, FLT_MAX / 32.f);
+    if (top_k > LOGITS_MAX_TOP && top_k < a.V)
+        floor = border_word(std::false_type{}, 18.f * fmaxf(cool, 1.f), [&](unsigned long long n) { return n > (unsigned long long)top_k ? (unsigned long long)top_k : 0ull; });
+    if (top_p < 1.f)
+        floor = border_word(std::true_type{}, 18.f * cool, [&](unsigned long long mass) { return wanted(top_p, mass); });
 
     // ---- the mass of what is kept, by wavefront: each owns a run of whole slots ----
     const int chunk = ((row.slots + BLOCK - 1) / BLOCK) * 64;
@@ -297,10 +322,12 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
         least = fmaxf(least, (float)(edge - fabs(edge) * 1e-6));
     }
     const bool filtered = min_p > 0.f, whole = floor == FIRST_WORD && !filtered;
+    const float floor_logit = key_logit(max((unsigned)(floor >> 32), 0x00800000u));
+    const unsigned floor_index = ~(unsigned)floor;     // the last of the floor's value that is kept
+    const double least_mass = (double)min_p * Weight::power(a.unit);
     auto kept_units = [&](float x, int index) -> unsigned long long {
-        if (!(x >= least) || order_word(logit_key(x), index) < floor) return 0;
-        if (filtered && weight.real(x) < (double)min_p) return 0;
-        return weight.units(x);
+        if (!(x >= least) || (x == floor_logit && (unsigned)index > floor_index)) return 0;
+        return weight.units_from(x, filtered, least_mass);
     };
     auto slot_units = [&](const uint4 &raw, int s) {
         unsigned long long sum = 0;

@@ -30,13 +30,11 @@ __device__ __forceinline__ void write_lse(const TopArgs &a, size_t r, const floa
 {
     if (a.lse) a.lse[r] = s.x == INFINITY ? INFINITY : (float)((double)(s.x == -INFINITY ? 0.f : s.x) / (double)a.temperature + log((double)s.y));
 }
-// the n words at the front of the list, by rank; places that are left over
-__device__ __forceinline__ void write_ranked(const TopArgs &a, size_t r, const unsigned long long *list, unsigned n)
+// the n words at the front of the list; places that are left over
+__device__ __forceinline__ void write_list(const TopArgs &a, size_t r, const unsigned long long *list, unsigned n)
 {
     const unsigned i = threadIdx.x;
-    if (i >= (unsigned)a.k) return;
-    if (i < n) write_top(a, r, rank_of(list, n, list[i]), list[i]);
-    else write_top(a, r, i, 0);
+    if (i < (unsigned)a.k) write_top(a, r, i, i < n ? list[i] : 0);
 }
 
 // ---- a block per row, or per part of a row ------------------------------------------------------------------------------
@@ -56,7 +54,7 @@ __global__ __launch_bounds__(BLOCK) void top_rows_kernel(TopArgs a)
     const float4 sums = acc.template combine<BLOCK>(part);
     if (a.segments == 1) {
         if (threadIdx.x == 0) write_lse(a, r, sums);
-        write_ranked(a, r, lds.list, n);
+        write_list(a, r, lds.list, n);
         return;
     }
     if (threadIdx.x == 0) a.partial[blockIdx.x] = sums;
@@ -81,8 +79,9 @@ __global__ __launch_bounds__(BLOCK) void top_join_kernel(TopArgs a)
     for (unsigned i = threadIdx.x; i < all; i += BLOCK) lds.list[i] = a.words[r * all + i];
     __syncthreads();
     unsigned n = keep_from<BLOCK>(lds, all, FIRST_WORD);           // the words that are there
-    if (n > (unsigned)a.k) n = keep_from<BLOCK>(lds, n, select_nth<BLOCK>(EachListed{lds.list, n, BLOCK}, FIRST_WORD, a.k, lds.select));
-    write_ranked(a, r, lds.list, n);
+    if (n > 512) n = keep_from<BLOCK>(lds, n, select_nth<BLOCK>(EachListed{lds.list, n, BLOCK}, FIRST_WORD, a.k, lds.select));
+    rank_list<BLOCK>(lds, n, a.k);
+    write_list(a, r, lds.list, min(n, (unsigned)a.k));
 }
 
 // ---- short rows: a wavefront each ---------------------------------------------------------------------------------------------
@@ -154,8 +153,12 @@ __global__ __launch_bounds__(256) void top_short_kernel(TopArgs a)
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");         // LDS accesses of one wavefront are executed in order
     for (unsigned i = lane; i < (unsigned)a.k; i += 64) {
-        if (i < n) write_top(a, r, rank_of(words, n, words[i]), words[i]);
-        else write_top(a, r, i, 0);
+        unsigned rank = i;
+        if (i < n) {
+            rank = 0;
+            for (unsigned j = 0; j < n; ++j) rank += words[j] > words[i];
+        }
+        write_top(a, r, rank, i < n ? words[i] : 0);
     }
 }
 
