@@ -391,7 +391,8 @@ _LOGIT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # eas
 
 
 def _logit_rows(name: str, t: torch.Tensor):
-    """Address, element type, rows, row length and stride of a matrix of logits (rows may be strided, a row's elements not)."""
+    """Address, element type, rows, row length and stride of a matrix of logits (rows may be strided, a row's elements not)
+    on the current device, where the kernels run."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA/HIP tensor")
     code = _LOGIT_TYPES.get(t.dtype)
@@ -407,32 +408,25 @@ def _logit_rows(name: str, t: torch.Tensor):
         ld = max(V, 1)
     elif ld < V:
         raise ValueError(f"{name}: rows must not overlap (stride {ld}, length {V})")
+    here = torch.cuda.current_device()
+    if t.get_device() != here:
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{here}")
     return t.data_ptr(), code, rows, V, ld
 
 
-def _on_device_of(logits, **others) -> None:
-    """Everything a call touches is on the current device, where its kernels run."""
-    here = torch.cuda.current_device()
-    if logits.device.index != here:
-        raise ValueError(f"logits are on {logits.device}, the current device is cuda:{here}")
-    for name, t in others.items():
-        if t is not None and t.device != logits.device:
-            raise ValueError(f"{name} must be on {logits.device}, is on {t.device}")
-
-
-def _row_vector(name: str, t, dtype, rows: int):
-    """Address of an optional [rows] tensor."""
+def _given(name: str, t, dtype, shape: tuple, device: int):
+    """Address of a tensor of this type and shape on the device with this number; None for None."""
     if t is None:
         return None
-    if isinstance(t, torch.Tensor) and t.shape != (rows,):
-        raise ValueError(f"{name} must be [{rows}], got {list(t.shape)}")
-    return _dev(name, t, dtype, rows)
-
-
-def _teacher_slots(name: str, t, dtype, rows: int, k: int) -> int:
-    if isinstance(t, torch.Tensor) and t.shape != (rows, k):
-        raise ValueError(f"{name} must be [{rows}][{k}], got {list(t.shape)}")
-    return _dev(name, t, dtype, rows * k)
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA/HIP tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous and {list(shape)}, got {list(t.shape)}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on cuda:{device}, is on {t.device}")
+    return t.data_ptr()
 
 
 def _new(shape, dtype, like, stream):
@@ -444,6 +438,7 @@ def _new(shape, dtype, like, stream):
 
 
 def _scratch(nbytes: int, workspace, like, stream):
+    """The workspace (kept by the caller until the call is made), its address and size."""
     if workspace is None:
         if nbytes == 0:
             return None, None, 0
@@ -468,24 +463,26 @@ def easgd_sample_tokens_workspace_bytes(rows: int, V: int) -> int:
     return int(_lib.easgd_sample_tokens_workspace_bytes(rows, V))
 
 
+_F32, _I32 = torch.float32, torch.int32
+
+
 def easgd_top_logits(logits, k: int, temperature: float = 1.0, values=None, indices=None, lse=None, workspace=None, stream=None):
     """The k first logits of every row's order and the row's log-sum-exp at `temperature`: what a teacher hands on.
     logits [rows][V] (fp32, bf16 or fp16, rows may be strided) -> values [rows][k] fp32, indices [rows][k] int32,
     lse [rows] fp32; places left over hold -inf and -1."""
     ptr, code, rows, V, ld = _logit_rows("logits", logits)
-    _on_device_of(logits, values=values, indices=indices, lse=lse)
-    k = int(k)
+    k, on = int(k), logits.get_device()
     if k < 1 or k > MAX_TOP:
         raise ValueError(f"k must be in [1, {MAX_TOP}], got {k}")
     if values is None:
-        values = _new((rows, k), torch.float32, logits, stream)
+        values = _new((rows, k), _F32, logits, stream)
     if indices is None:
-        indices = _new((rows, k), torch.int32, logits, stream)
+        indices = _new((rows, k), _I32, logits, stream)
     if lse is None:
-        lse = _new((rows,), torch.float32, logits, stream)
-    _ws, ws, nbytes = _scratch(easgd_top_logits_workspace_bytes(rows, V, k), workspace, logits, stream)
-    _check(_lib.easgd_top_logits(ptr, code, rows, V, ld, k, temperature, _teacher_slots("values", values, torch.float32, rows, k),
-                                 _teacher_slots("indices", indices, torch.int32, rows, k), _row_vector("lse", lse, torch.float32, rows),
+        lse = _new((rows,), _F32, logits, stream)
+    keep, ws, nbytes = _scratch(easgd_top_logits_workspace_bytes(rows, V, k), workspace, logits, stream)
+    _check(_lib.easgd_top_logits(ptr, code, rows, V, ld, k, temperature, _given("values", values, _F32, (rows, k), on),
+                                 _given("indices", indices, _I32, (rows, k), on), _given("lse", lse, _F32, (rows,), on),
                                  ws, nbytes, _stream(stream)))
     return values, indices, lse
 
@@ -494,20 +491,18 @@ def _distill_args(logits, indices, values, temperature, teacher_lse, labels, har
     ptr, code, rows, V, ld = _logit_rows("logits", logits)
     if not isinstance(indices, torch.Tensor) or indices.dim() != 2:
         raise ValueError("indices must be [rows][k]")
-    k = indices.shape[1]
-    _on_device_of(logits, indices=indices, values=values, teacher_lse=teacher_lse, labels=labels)
-    return rows, V, k, (ptr, code, rows, V, ld, _teacher_slots("indices", indices, torch.int32, rows, k),
-                        _teacher_slots("values", values, torch.float32, rows, k), _row_vector("teacher_lse", teacher_lse, torch.float32, rows),
-                        k, _row_vector("labels", labels, torch.int32, rows), temperature, hard)
+    k, on = indices.shape[1], logits.get_device()
+    return rows, V, k, on, (ptr, code, rows, V, ld, _given("indices", indices, _I32, (rows, k), on), _given("values", values, _F32, (rows, k), on),
+                            _given("teacher_lse", teacher_lse, _F32, (rows,), on), k, _given("labels", labels, _I32, (rows,), on),
+                            temperature, hard)
 
 
 def _gradient_rows(logits, dlogits, rows: int, V: int, stream):
     if dlogits is None:
         dlogits = _new((rows, V), logits.dtype, logits, stream)
     ptr, code, drows, dV, dld = _logit_rows("dlogits", dlogits)
-    if dlogits.dtype != logits.dtype or (drows, dV) != (rows, V):
+    if dlogits.dtype != logits.dtype or drows != rows or dV != V:
         raise ValueError(f"dlogits must be [{rows}][{V}] {logits.dtype}, got {list(dlogits.shape)} {dlogits.dtype}")
-    _on_device_of(logits, dlogits=dlogits)
     return dlogits, ptr, dld
 
 
@@ -516,14 +511,13 @@ def easgd_distill_loss(logits, indices, values, temperature: float = 1.0, teache
     """Forward pass of distillation: the loss of every row of student logits [rows][V] against the teacher's top logits
     (indices, values [rows][k]; teacher_lse [rows] turns what they leave over into one more outcome), mixed with the
     cross-entropy of labels [rows] by `hard`.  Returns loss [rows] and state [rows][4], which easgd_distill_grad takes."""
-    rows, V, k, args = _distill_args(logits, indices, values, temperature, teacher_lse, labels, hard)
+    rows, V, k, on, args = _distill_args(logits, indices, values, temperature, teacher_lse, labels, hard)
     if loss is None:
-        loss = _new((rows,), torch.float32, logits, stream)
+        loss = _new((rows,), _F32, logits, stream)
     if state is None:
-        state = _new((rows, 4), torch.float32, logits, stream)
-    _on_device_of(logits, loss=loss, state=state)
-    _ws, ws, nbytes = _scratch(easgd_distill_workspace_bytes(rows, V, k), workspace, logits, stream)
-    _check(_lib.easgd_distill_loss(*args, _row_vector("loss", loss, torch.float32, rows), _teacher_slots("state", state, torch.float32, rows, 4),
+        state = _new((rows, 4), _F32, logits, stream)
+    keep, ws, nbytes = _scratch(easgd_distill_workspace_bytes(rows, V, k), workspace, logits, stream)
+    _check(_lib.easgd_distill_loss(*args, _given("loss", loss, _F32, (rows,), on), _given("state", state, _F32, (rows, 4), on),
                                    ws, nbytes, _stream(stream)))
     return loss, state
 
@@ -532,10 +526,9 @@ def easgd_distill_grad(logits, indices, values, state, temperature: float = 1.0,
                        scale: float = 1.0, dloss=None, dlogits=None, stream=None):
     """Backward pass of easgd_distill_loss: the gradient of scale * sum(dloss * loss) (dloss None: all ones) with respect to
     the student's logits, in their type."""
-    rows, V, k, args = _distill_args(logits, indices, values, temperature, teacher_lse, labels, hard)
+    rows, V, k, on, args = _distill_args(logits, indices, values, temperature, teacher_lse, labels, hard)
     dlogits, dptr, dld = _gradient_rows(logits, dlogits, rows, V, stream)
-    _on_device_of(logits, state=state, dloss=dloss)
-    _check(_lib.easgd_distill_grad(*args, _teacher_slots("state", state, torch.float32, rows, 4), _row_vector("dloss", dloss, torch.float32, rows),
+    _check(_lib.easgd_distill_grad(*args, _given("state", state, _F32, (rows, 4), on), _given("dloss", dloss, _F32, (rows,), on),
                                    scale, dptr, dld, _stream(stream)))
     return dlogits
 
@@ -543,13 +536,12 @@ def easgd_distill_grad(logits, indices, values, state, temperature: float = 1.0,
 def easgd_distill(logits, indices, values, temperature: float = 1.0, teacher_lse=None, labels=None, hard: float = 0.0,
                   scale: float = 1.0, loss=None, dlogits=None, workspace=None, stream=None):
     """Loss and gradient of distillation in one call: easgd_distill_loss, and the gradient of scale * sum(loss)."""
-    rows, V, k, args = _distill_args(logits, indices, values, temperature, teacher_lse, labels, hard)
+    rows, V, k, on, args = _distill_args(logits, indices, values, temperature, teacher_lse, labels, hard)
     if loss is None:
-        loss = _new((rows,), torch.float32, logits, stream)
-    _on_device_of(logits, loss=loss)
+        loss = _new((rows,), _F32, logits, stream)
     dlogits, dptr, dld = _gradient_rows(logits, dlogits, rows, V, stream)
-    _ws, ws, nbytes = _scratch(easgd_distill_workspace_bytes(rows, V, k), workspace, logits, stream)
-    _check(_lib.easgd_distill(*args, scale, _row_vector("loss", loss, torch.float32, rows), dptr, dld, ws, nbytes, _stream(stream)))
+    keep, ws, nbytes = _scratch(easgd_distill_workspace_bytes(rows, V, k), workspace, logits, stream)
+    _check(_lib.easgd_distill(*args, scale, _given("loss", loss, _F32, (rows,), on), dptr, dld, ws, nbytes, _stream(stream)))
     return loss, dlogits
 
 
@@ -561,17 +553,16 @@ def easgd_sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min
     ptr, code, rows, V, ld = _logit_rows("logits", logits)
     if u is None:
         raise TypeError("u must be a CUDA/HIP tensor")
+    on, shape = logits.get_device(), (rows,)
     if tokens is None:
-        tokens = _new((rows,), torch.int32, logits, stream)
+        tokens = _new(shape, _I32, logits, stream)
     if logprob is None:
-        logprob = _new((rows,), torch.float32, logits, stream)
-    _on_device_of(logits, u=u, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, tokens=tokens, logprob=logprob)
-    _ws, ws, nbytes = _scratch(easgd_sample_tokens_workspace_bytes(rows, V), workspace, logits, stream)
-    _check(_lib.easgd_sample_tokens(ptr, code, rows, V, ld, _row_vector("u", u, torch.float32, rows),
-                                    _row_vector("temperature", temperature, torch.float32, rows), _row_vector("top_k", top_k, torch.int32, rows),
-                                    _row_vector("top_p", top_p, torch.float32, rows), _row_vector("min_p", min_p, torch.float32, rows),
-                                    _row_vector("tokens", tokens, torch.int32, rows), _row_vector("logprob", logprob, torch.float32, rows),
-                                    ws, nbytes, _stream(stream)))
+        logprob = _new(shape, _F32, logits, stream)
+    keep, ws, nbytes = _scratch(easgd_sample_tokens_workspace_bytes(rows, V), workspace, logits, stream)
+    _check(_lib.easgd_sample_tokens(ptr, code, rows, V, ld, _given("u", u, _F32, shape, on), _given("temperature", temperature, _F32, shape, on),
+                                    _given("top_k", top_k, _I32, shape, on), _given("top_p", top_p, _F32, shape, on),
+                                    _given("min_p", min_p, _F32, shape, on), _given("tokens", tokens, _I32, shape, on),
+                                    _given("logprob", logprob, _F32, shape, on), ws, nbytes, _stream(stream)))
     return tokens, logprob
 
 

@@ -11,6 +11,13 @@ namespace easgd {
 static constexpr int LOGITS_MAX_V = 1 << 20;      // an index fits 20 bits of an order word
 static constexpr int LOGITS_MAX_TOP = EASGD_MAX_TOP;
 
+// one of four words by number, without an indexed register
+__device__ __forceinline__ unsigned word_of(const uint4 &v, int i)
+{
+    const unsigned low = i & 1 ? v.y : v.x, high = i & 1 ? v.w : v.z;
+    return i & 2 ? high : low;
+}
+
 // Element types: 128 bits hold VEC elements; every type widens to fp32 without loss.
 template <int DT> struct LogitType;
 template <> struct LogitType<EASGD_F32> {
@@ -18,6 +25,7 @@ template <> struct LogitType<EASGD_F32> {
     static constexpr int VEC = 4;
     static constexpr unsigned NEG_INF = 0xff800000u;
     __device__ static __forceinline__ float widen(Stored b) { return b; }
+    __device__ static __forceinline__ float pick(const uint4 &v, int j) { return __uint_as_float(word_of(v, j)); }
     __device__ static __forceinline__ void unpack(const uint4 &v, float (&x)[VEC])
     {
         x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
@@ -34,6 +42,11 @@ template <> struct LogitType<EASGD_BF16> {
     static constexpr int VEC = 8;
     static constexpr unsigned NEG_INF = 0xff80u;
     __device__ static __forceinline__ float widen(Stored b) { return (float)b; }
+    __device__ static __forceinline__ float pick(const uint4 &v, int j)
+    {
+        const unsigned w = word_of(v, j >> 1);
+        return __uint_as_float(j & 1 ? w & 0xffff0000u : w << 16);
+    }
     __device__ static __forceinline__ void unpack(const uint4 &v, float (&x)[VEC])
     {
         const unsigned u[4] = {v.x, v.y, v.z, v.w};
@@ -62,6 +75,10 @@ template <> struct LogitType<EASGD_F16> {
     static constexpr int VEC = 8;
     static constexpr unsigned NEG_INF = 0xfc00u;
     __device__ static __forceinline__ float widen(Stored b) { return (float)b; }
+    __device__ static __forceinline__ float pick(const uint4 &v, int j)
+    {
+        return (float)__builtin_bit_cast(_Float16, (unsigned short)(word_of(v, j >> 1) >> (j & 1 ? 16 : 0)));
+    }
     __device__ static __forceinline__ void unpack(const uint4 &v, float (&x)[VEC])
     {
         typedef _Float16 Pair __attribute__((ext_vector_type(2)));
@@ -131,6 +148,13 @@ template <int DT> struct Row {
         }
         if constexpr (VEC == 4) return make_uint4(e[0], e[1], e[2], e[3]);
         else return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4 % VEC] | e[5 % VEC] << 16, e[6 % VEC] | e[7 % VEC] << 16);
+    }
+    // slot s, or an empty one from `last` on: for lanes of a wavefront on consecutive slots, whose place is looked at once
+    __device__ __forceinline__ uint4 load_wave(int s, int last) const
+    {
+        const int first = __builtin_amdgcn_readfirstlane(s - (int)(threadIdx.x & 63));
+        if (first * VEC >= shift && first + 64 <= last && (first + 64) * VEC <= end) return load_full(s);
+        return s < last ? load(s) : empty();
     }
     __device__ static __forceinline__ uint4 empty()
     {

@@ -107,7 +107,7 @@ template <int DT, int BLOCK, typename F> __device__ __forceinline__ void each_sl
         uint4 v[DEEP];
 #pragma unroll
         for (int i = 0; i < DEEP; ++i)
-            if (s + i * BLOCK < s1) v[i] = row.load(s + i * BLOCK);
+            if (s + i * BLOCK < s1) v[i] = row.load_wave(s + i * BLOCK, s1);
 #pragma unroll
         for (int i = 0; i < DEEP; ++i)
             if (s + i * BLOCK < s1) f(v[i], s + i * BLOCK);
@@ -226,11 +226,8 @@ __device__ __forceinline__ unsigned first_of(const Row<DT> &row, int s0, int s1,
     const int tid = threadIdx.x;
     const unsigned grown = max(4 * k, 256u);            // words after which the floor is raised again
     uint4 v[DEEP];
-    auto load = [&](int s) {
 #pragma unroll
-        for (int i = 0; i < DEEP; ++i) v[i] = s + i * BLOCK < s1 ? row.load(s + i * BLOCK) : Row<DT>::empty();
-    };
-    load(s0 + tid);
+    for (int i = 0; i < DEEP; ++i) v[i] = row.load_wave(s0 + tid + i * BLOCK, s1);
     unsigned long long floor = FIRST_WORD;
     if (tid == 0) lds.n = 0;
     if ((s1 - s0) * VEC > TOP_LIST / 4) {
@@ -251,35 +248,35 @@ __device__ __forceinline__ unsigned first_of(const Row<DT> &row, int s0, int s1,
     unsigned n = 0;
     bool over = false;
     for (int s = s0 + tid;;) {
-        uint4 w[DEEP];
-#pragma unroll
-        for (int i = 0; i < DEEP; ++i) w[i] = v[i];
         const int now = s;
         s += DEEP * BLOCK;
         const bool more = s - tid < s1;                 // uniform
-        if (more) load(s);
 #pragma unroll
         for (int i = 0; i < DEEP; ++i) {
-            const int at = now + i * BLOCK;
+            const int at = now + i * BLOCK, ahead = s + i * BLOCK;
             if (at - (tid & 63) >= s1) break;           // the whole wavefront is behind the end
             float x[VEC];
-            Type::unpack(w[i], x);
+            Type::unpack(v[i], x);
             seen(x, at);
             float t = x[0];
 #pragma unroll
             for (int j = 1; j < VEC; ++j) t = fmaxf(t, x[j]);
-            if (!over && t >= least) {
+            if (!over && __any(t >= least)) {           // uniform for the wavefront
+                // a bit per element, the last one's lowest; nearly always a few lanes have one
+                unsigned hits = 0;
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    if (x[j] >= least) {
-                        const unsigned long long word = order_word(logit_key(x[j]), row.index(at, j));
-                        if (word >= floor) {
-                            const unsigned to = atomicAdd(&lds.n, 1u);
-                            if (to < TOP_LIST) lds.list[to] = word;
-                        }
+                for (int j = 0; j < VEC; ++j) hits = hits + hits + (x[j] >= least ? 1u : 0u);
+                while (hits) {
+                    const int j = VEC - __ffs(hits);
+                    hits &= hits - 1;
+                    const unsigned long long word = order_word(logit_key(Type::pick(v[i], j)), row.index(at, j));
+                    if (word >= floor) {
+                        const unsigned to = atomicAdd(&lds.n, 1u);
+                        if (to < TOP_LIST) lds.list[to] = word;
                     }
                 }
             }
+            if (more) v[i] = row.load_wave(ahead, s1);  // the next round's slot
         }
         if (!more) break;
         __syncthreads();

@@ -163,6 +163,8 @@ __global__ __launch_bounds__(256) void top_short_kernel(TopArgs a)
 }
 
 // Few long rows are cut into parts, so that there are blocks for the whole chip: each part's first k go through the workspace.
+// Many rows take blocks of 256 threads, five of which a compute unit holds (2048 x 131072 bf16, k = 64: 168 us against 180 with 512);
+// few rows, and more than 64 tokens (whose first floor wants many maxima), 512 (8 x 50001: 15.8 us against 18.5 with 256).
 static constexpr int TOP_BLOCK = 512, TOP_SHORT_V = 1024;
 static constexpr int TOP_SPLIT_ROWS = 256, TOP_SPLIT_SLOTS = 2048;
 static int top_segments(size_t rows, int slots, int k)
@@ -212,6 +214,7 @@ int easgd_top_logits(const void *logits, int dtype, size_t rows, int V, size_t l
         constexpr int DT = decltype(dt)::value;
         if (V <= 128) EASGD_LAUNCH((top_short_kernel<DT, 2>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
         else if (V <= TOP_SHORT_V) EASGD_LAUNCH((top_short_kernel<DT, TOP_SHORT_V / 64>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
+        else if (segments == 1 && rows >= TOP_SPLIT_ROWS && k <= 64) EASGD_LAUNCH((top_rows_kernel<DT, 256>), dim3((unsigned)rows), dim3(256), 0, s, a);
         else EASGD_LAUNCH((top_rows_kernel<DT, TOP_BLOCK>), dim3((unsigned)(rows * segments)), dim3(TOP_BLOCK), 0, s, a);
     });
     if (V > TOP_SHORT_V && segments > 1) EASGD_LAUNCH((top_join_kernel<TOP_BLOCK>), dim3((unsigned)rows), dim3(TOP_BLOCK), 0, s, a);
