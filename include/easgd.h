@@ -442,6 +442,18 @@ int easgd_distill(const void *logits, int dtype, size_t rows, int V, size_t ld,
                   void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Step (1) of a round as easgd_grad does it, with distillation in the place of the softmax cross-entropy: the gradients of all
+ * workers' mean losses (sums of easgd_distill's losses over the worker's b samples, padding among them, over b).
+ *   indices [P][b][k], values [P][b][k], teacher_lse [P][b] or NULL, labels [P][b] or NULL, k, temperature, hard as for
+ *   easgd_distill; every other argument, the workspace (easgd_grad_workspace_bytes), requirements and errors as for easgd_grad.
+ * The teacher may be any model, the center of the replicas among them.
+ */
+int easgd_grad_distill(const int *dims, int n_layers, const float *W, size_t ld, const float *X,
+                       const int32_t *indices, const float *values, const float *teacher_lse, int k, const int32_t *labels,
+                       int P, int b, float temperature, float hard, float *G, float *loss,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * One token of every row, drawn with a given random number.  With w[j] = exp((z[j] - max z) / temperature), the tokens
  * that may be drawn are the shortest of three prefixes of the row's order (at least its first token):
  *   top_k   its first top_k tokens;

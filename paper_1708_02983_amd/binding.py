@@ -90,6 +90,8 @@ def _load() -> ctypes.CDLL:
     lib.easgd_distill_grad.restype = i
     lib.easgd_distill.argtypes = [vp, i, sz, i, sz, vp, vp, vp, i, vp, f, f, f, vp, vp, sz, vp, sz, vp]
     lib.easgd_distill.restype = i
+    lib.easgd_grad_distill.argtypes = [ip, i, vp, sz, vp, vp, vp, vp, i, vp, i, i, f, f, vp, vp, vp, sz, vp]
+    lib.easgd_grad_distill.restype = i
     lib.easgd_sample_tokens_workspace_bytes.argtypes = [sz, i]
     lib.easgd_sample_tokens_workspace_bytes.restype = sz
     lib.easgd_sample_tokens.argtypes = [vp, i, sz, i, sz, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
@@ -543,6 +545,28 @@ def easgd_distill(logits, indices, values, temperature: float = 1.0, teacher_lse
     keep, ws, nbytes = _scratch(easgd_distill_workspace_bytes(rows, V, k), workspace, logits, stream)
     _check(_lib.easgd_distill(*args, scale, _given("loss", loss, _F32, (rows,), on), dptr, dld, ws, nbytes, _stream(stream)))
     return loss, dlogits
+
+
+def easgd_grad_distill(dims: Sequence[int], W, X, indices, values, G, loss=None, temperature: float = 1.0, teacher_lse=None, labels=None,
+                       hard: float = 0.0, workspace=None, stream=None):
+    """Step (1) with distillation in the place of the softmax cross-entropy: gradients of all P workers into G[P][ld] from the
+    teacher's top logits (indices, values [P][b][k]; teacher_lse, labels [P][b]); returns the workspace used."""
+    arr, L = _dims(dims)
+    if W.dim() != 2 or X.dim() != 3 or indices.dim() != 3:
+        raise ValueError("expected W[P][ld], X[P][b][d_in], indices[P][b][k]")
+    P, ld = W.shape
+    b, k, on = X.shape[1], indices.shape[2], torch.cuda.current_device()
+    N = easgd_mlp_num_params(dims)
+    if N == 0:
+        raise ValueError(f"invalid layer widths {list(dims)}")
+    need = (P - 1) * ld + N
+    nbytes = easgd_grad_workspace_bytes(dims, P, b)
+    workspace, ws, size = _scratch(nbytes, workspace, W, stream)
+    _check(_lib.easgd_grad_distill(arr, L, _dev("W", W, _F32, need), ld, _given("X", X, _F32, (P, b, dims[0]), on),
+                                   _given("indices", indices, _I32, (P, b, k), on), _given("values", values, _F32, (P, b, k), on),
+                                   _given("teacher_lse", teacher_lse, _F32, (P, b), on), k, _given("labels", labels, _I32, (P, b), on),
+                                   P, b, temperature, hard, _dev("G", G, _F32, need), _given("loss", loss, _F32, (P,), on), ws, size, _stream(stream)))
+    return workspace
 
 
 def easgd_sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None, logprob=None,

@@ -6,7 +6,7 @@
 //   grad = soft (c e_j / ST - target_j - [j outside] r e_j / SO) + up hard (h_j / S1 - [j = y]),  soft = up (1 - hard) T
 // so a row is read for its maximum and its sums, and once more for its gradient.  Bound: HBM (each logit once in, each
 // gradient once out), with the vector ALUs close behind (an exponential takes four issue slots, and either pass has one).
-#include "logits.h"
+#include "distill.h"
 #include "row_sums.h"
 
 namespace easgd {
@@ -636,19 +636,26 @@ struct DistillCall {
     size_t workspace_bytes;
 };
 
+int check_teacher(const char *name, const TeacherGiven &t, bool rows)
+{
+    if (t.k < 1 || t.k > LOGITS_MAX_TOP) return fail(EASGD_EINVAL, "%s: k must be in [1, %d], got %d", name, LOGITS_MAX_TOP, t.k);
+    if (int rc = check_temperature(name, t.temperature)) return rc;
+    if (!(t.hard >= 0.f && t.hard <= 1.f)) return fail(EASGD_EINVAL, "%s: hard must be in [0, 1], got %g", name, (double)t.hard);
+    if (!t.labels && t.hard != 0.f) return fail(EASGD_EINVAL, "%s: hard = %g needs labels", name, (double)t.hard);
+    if (rows && (!t.indices || !t.values)) return fail(EASGD_EINVAL, "%s: NULL pointer", name);
+    if (!aligned_to(t.indices, 4) || !aligned_to(t.values, 4) || !aligned_to(t.lse, 4) || !aligned_to(t.labels, 4))
+        return fail(EASGD_EINVAL, "%s: indices, values, teacher_lse, labels must be 4-byte aligned", name);
+    return EASGD_OK;
+}
+
 static int check_distill(const DistillCall &q, int mode)
 {
     const DistillArgs &a = q.a;
     if (int rc = check_logits(q.name, a.logits, q.dtype, q.rows, a.V, a.ld)) return rc;
-    if (a.k < 1 || a.k > LOGITS_MAX_TOP) return fail(EASGD_EINVAL, "%s: k must be in [1, %d], got %d", q.name, LOGITS_MAX_TOP, a.k);
-    if (int rc = check_temperature(q.name, a.temperature)) return rc;
-    if (!(a.hard >= 0.f && a.hard <= 1.f)) return fail(EASGD_EINVAL, "%s: hard must be in [0, 1], got %g", q.name, (double)a.hard);
-    if (!a.labels && a.hard != 0.f) return fail(EASGD_EINVAL, "%s: hard = %g needs labels", q.name, (double)a.hard);
-    if (q.rows > 0 && (!a.indices || !a.values || ((mode & DISTILL_LOSS) && !a.loss) || (mode == DISTILL_GRAD && !a.state) || ((mode & DISTILL_GRAD) && !a.dlogits)))
+    if (int rc = check_teacher(q.name, {a.indices, a.values, a.teacher_lse, a.k, a.labels, a.temperature, a.hard}, q.rows > 0)) return rc;
+    if (q.rows > 0 && (((mode & DISTILL_LOSS) && !a.loss) || (mode == DISTILL_GRAD && !a.state) || ((mode & DISTILL_GRAD) && !a.dlogits)))
         return fail(EASGD_EINVAL, "%s: NULL pointer", q.name);
-    if (!aligned_to(a.indices, 4) || !aligned_to(a.values, 4) || !aligned_to(a.teacher_lse, 4) || !aligned_to(a.labels, 4) || !aligned_to(a.loss, 4) ||
-        !aligned_to(a.dloss, 4))
-        return fail(EASGD_EINVAL, "%s: indices, values, teacher_lse, labels, loss, dloss must be 4-byte aligned", q.name);
+    if (!aligned_to(a.loss, 4) || !aligned_to(a.dloss, 4)) return fail(EASGD_EINVAL, "%s: loss, dloss must be 4-byte aligned", q.name);
     if (!aligned16(a.state)) return fail(EASGD_EINVAL, "%s: state must be 16-byte aligned", q.name);
     if (mode & DISTILL_GRAD) {
         if (!std::isfinite(a.scale)) return fail(EASGD_EINVAL, "%s: scale must be finite", q.name);
@@ -720,7 +727,7 @@ template <int DT, bool GRAD> static void launch_rows(const DistillArgs &a, int s
 }
 
 // Rows that a wavefront holds
-static constexpr int SHORT_V = 1024;
+static constexpr int SHORT_V = DISTILL_SHORT_V;
 
 template <int DT, int NQ, int MODE> static void launch_short_nq(const DistillArgs &a, hipStream_t s)
 {
@@ -732,6 +739,14 @@ template <int DT, int MODE> static void launch_short(const DistillArgs &a, hipSt
 {
     if (a.V <= 128) launch_short_nq<DT, 2, MODE>(a, s);
     else launch_short_nq<DT, SHORT_V / 64, MODE>(a, s);
+}
+
+void distill_logits(const float *logits, int parts, size_t part_stride, size_t rows, int classes, const TeacherGiven &t, float scale,
+                    float *row_loss, float *dlogits, void *stream)
+{
+    const DistillArgs a = {logits, (size_t)classes, classes, t.k, t.indices, t.values, t.lse, t.labels, t.temperature, t.hard, row_loss, nullptr, nullptr,
+                           scale, dlogits, (size_t)classes, rows, parts, part_stride, nullptr, 1, 0};
+    launch_short<EASGD_F32, DISTILL_BOTH>(a, static_cast<hipStream_t>(stream));
 }
 
 // Rows cut into parts: a workspace for the parts' sums, then for the states of the rows.

@@ -22,6 +22,7 @@
 // Eq. (5),(6) to the layer's slice of every replica in its epilogue.
 #include "gemm_chain.h"
 #include "gemm_split.h"
+#include "distill.h"
 #include "shared_launches.h"
 #include "mlp_head.h"
 #include "persistent_round.h"
@@ -620,7 +621,7 @@ struct ElasticStep {
 
 static int grad_impl(const char *name, const int *dims, int n_layers, const float *W, size_t ld, const float *X,
                      const int32_t *y, int P, int b, float *G, float *loss, void *workspace, size_t workspace_bytes,
-                     void *stream, const ElasticStep *step, unsigned short *G16 = nullptr);
+                     void *stream, const ElasticStep *step, unsigned short *G16 = nullptr, const TeacherGiven *teacher = nullptr);
 
 // A second stream per device (default priority) with the two events that order it against the caller's
 // stream: `fork` is recorded on the caller's stream when the round starts, `join` on the second stream when
@@ -732,6 +733,17 @@ int easgd_grad_bf16(const int *dims, int n_layers, const float *W, size_t ld, co
                             workspace_bytes, stream, nullptr, G);
 }
 
+int easgd_grad_distill(const int *dims, int n_layers, const float *W, size_t ld, const float *X, const int32_t *indices, const float *values,
+                       const float *teacher_lse, int k, const int32_t *labels, int P, int b, float temperature, float hard,
+                       float *G, float *loss, void *workspace, size_t workspace_bytes, void *stream)
+{
+    static_assert(easgd::MAX_CLASSES <= easgd::DISTILL_SHORT_V, "every network's logits are short rows");
+    const easgd::TeacherGiven teacher = {indices, values, teacher_lse, k, labels, temperature, hard};
+    if (int rc = easgd::check_teacher("easgd_grad_distill", teacher, true)) return rc;
+    return easgd::grad_impl("easgd_grad_distill", dims, n_layers, W, ld, X, labels, P, b, G, loss, workspace, workspace_bytes,
+                            stream, nullptr, nullptr, &teacher);
+}
+
 int easgd_mlp_round(const int *dims, int n_layers, float *W, float *V, float *Wc, size_t ld,
                     const float *X, const int32_t *y, int P, int b, float *G, float *loss,
                     float eta, float rho, float delta, void *workspace, size_t workspace_bytes, void *stream)
@@ -759,11 +771,11 @@ namespace easgd {
 
 static int grad_impl(const char *name, const int *dims, int n_layers, const float *W, size_t ld, const float *X,
                      const int32_t *y, int P, int b, float *G, float *loss, void *workspace, size_t workspace_bytes,
-                     void *stream, const ElasticStep *step, unsigned short *G16)
+                     void *stream, const ElasticStep *step, unsigned short *G16, const TeacherGiven *teacher)
 {
     const int L = n_layers;
     GradPlan pl;
-    if (!W || !X || !y || (!G && !G16 && !step)) return fail(EASGD_EINVAL, "%s: NULL pointer", name);
+    if (!W || !X || (!y && !teacher) || (!G && !G16 && !step)) return fail(EASGD_EINVAL, "%s: NULL pointer", name);
     if (!make_plan(dims, L, P, b, pl))
         return fail(EASGD_EINVAL, "%s: need 1 <= n_layers <= %d, all dims >= 1, P >= 1, b >= 1", name, MAX_LAYERS);
     if (dims[L] > MAX_CLASSES) return fail(EASGD_EINVAL, "%s: at most %d classes, got %d", name, MAX_CLASSES, dims[L]);
@@ -797,7 +809,7 @@ static int grad_impl(const char *name, const int *dims, int n_layers, const floa
     const Form by_size = fp32 ? FORM_FP32 : FORM_BY_SIZE;
 
     // a narrow last layer goes through mlp_head_kernel together with the softmax and its own input gradient
-    const bool head = options().mlp_head != 0 && head_fits(dims, L);
+    const bool head = !teacher && options().mlp_head != 0 && head_fits(dims, L);
     if (head && (size_t)P * ((b + HEAD_ROWS - 1) / HEAD_ROWS) > 0x3fffffffull) return fail(EASGD_ERANGE, "%s: P*b too large", name);
 
     // ---- a single-layer network small enough to be bound by launch boundaries: the whole call in one launch ----
@@ -900,6 +912,8 @@ static int grad_impl(const char *name, const int *dims, int n_layers, const floa
         h.d_in = dims[L - 1]; h.C = dims[L]; h.b = b; h.P = P;
         if (L == 1) h.ctr = center_job;
         launch_head(h, s);
+    } else if (teacher) {
+        distill_logits(logits, pl.splits, (size_t)rows * dims[L], (size_t)rows, dims[L], *teacher, 1.f / (float)b, row_loss, dz[(L - 1) % 3], stream);
     } else {
         EASGD_LAUNCH(softmax_xent_kernel, dim3((rows + 3) / 4), dim3(256), 0, s, logits, y, dz[(L - 1) % 3], row_loss,
                            rows, b, dims[L], pl.splits, (size_t)rows * dims[L]);

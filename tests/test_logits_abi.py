@@ -22,7 +22,7 @@ def hip():
 
 def test_declared_and_exported(hip):
     text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "easgd.h")).read(), flags=re.S)
-    for name in ("easgd_top_logits", "easgd_distill_loss", "easgd_distill_grad", "easgd_distill", "easgd_sample_tokens"):
+    for name in ("easgd_top_logits", "easgd_distill_loss", "easgd_distill_grad", "easgd_distill", "easgd_sample_tokens", "easgd_grad_distill"):
         assert re.search(rf"\b{name}\s*\(", text) and hasattr(hip.lib(), name) and callable(getattr(hip, name))
     assert re.search(r"EASGD_MAX_TOP\s+256\b", text) and hip.MAX_TOP == 256
 
@@ -120,3 +120,17 @@ def test_the_binding_refuses_tensors_that_are_not_on_a_gpu(hip):
         hip.easgd_distill(z, idx, val)
     with pytest.raises(TypeError, match="logits must be a CUDA/HIP tensor"):
         hip.easgd_sample_tokens(z, torch.rand(3))
+
+
+def test_the_network_call_refuses_too(hip):
+    lib = hip.lib()
+    dims = (ctypes.c_int * 2)(784, 10)
+    good = dict(dims=dims, n_layers=1, W=FAKE, ld=7852, X=FAKE, indices=FAKE, values=FAKE, teacher_lse=None, k=3, labels=None, P=1, b=1,
+                temperature=1.0, hard=0.0, G=FAKE, loss=None, workspace=FAKE, workspace_bytes=1 << 30)
+    call = lambda **changes: lib.easgd_grad_distill(*{**good, **changes}.values(), None)
+    for changes in (dict(W=None), dict(X=None), dict(G=None), dict(indices=None), dict(values=None), dict(k=0), dict(k=257), dict(temperature=0.0),
+                    dict(hard=0.5), dict(hard=2.0, labels=FAKE), dict(n_layers=0), dict(P=0), dict(b=0), dict(ld=7000), dict(indices=FAKE + 2), dict(X=FAKE + 4),
+                    dict(dims=(ctypes.c_int * 2)(784, 1025), ld=1 << 20)):
+        assert call(**changes) == EINVAL, changes
+        assert lib.easgd_last_error().decode().startswith("easgd_grad_distill:"), changes
+    assert call(workspace=None) == EWORKSPACE and call(workspace_bytes=16) == EWORKSPACE
