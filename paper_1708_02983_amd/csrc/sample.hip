@@ -25,9 +25,17 @@ struct SampleArgs {
     int unit;                 // log2 of the units of mass in the largest weight
 };
 
+// how many tokens the filters leave at most; 1 for greedy rows (and where nothing reaches a min_p above 1)
+__device__ __forceinline__ int most_tokens(const SampleArgs &a, size_t r)
+{
+    const float T = a.temperature ? a.temperature[r] : 1.f, min_p = a.min_p ? a.min_p[r] : 0.f;
+    return T > 0.f && !(min_p > 1.f) ? (a.top_k ? a.top_k[r] : 0) : 1;
+}
+
 // w = 2^y with y = (z - max) log2(e) / T <= 0, in 64 bits: y = j / 512 + f with |f| <= 2^-10 (adding 1.5 * 2^43 rounds to the
 // multiple of 2^-9 and leaves j in the low bits), 2^(j / 512) from a table in LDS and an exponent, 2^f from its Taylor polynomial,
-// whose remainder is below (2^-10 ln 2)^4 / 24 = 9e-15.  Below 2^-200 the value no longer matters (a unit is at least 2^-51 of
+// whose remainder is below (2^-10 ln 2)^4 / 24 = 9e-15.  (The time is the 64-bit instructions': 131072 logits on one compute unit
+// 29 us; with 32 entries, as many copies as there are pairs of banks and polynomials of degree 5 33.)  Below 2^-200 the value no longer matters (a unit is at least 2^-51 of
 // the largest weight, min_p at least 2^-149).
 static constexpr int WEIGHT_TABLE = 512;
 struct Weight {
@@ -112,6 +120,28 @@ __device__ __forceinline__ unsigned long long scan(unsigned long long v, unsigne
     return before;
 }
 
+// out[i], i < n: the number of j < n for which before(j, i) holds.  As many neighbouring lanes as there are threads share an i.
+// Ends with a barrier.
+template <int BLOCK, typename P> __device__ __forceinline__ void ranks(unsigned n, P before, unsigned *out)
+{
+    unsigned share = 1, log2_share = 0;
+    while (share < 64 && 2 * share * n <= BLOCK) {
+        share *= 2;
+        ++log2_share;
+    }
+    for (unsigned t = threadIdx.x; t - (threadIdx.x & 63) < n * share; t += BLOCK) {       // whole wavefronts
+        const unsigned i = t >> log2_share;
+        unsigned rank = 0;
+        if (i < n) {
+#pragma unroll 4
+            for (unsigned j = t & (share - 1); j < n; j += share) rank += before(j, i);
+        }
+        for (unsigned o = 1; o < share; o *= 2) rank += __shfl_xor(rank, o);
+        if (i < n && (t & (share - 1)) == 0) out[i] = rank;
+    }
+    __syncthreads();
+}
+
 // the place of the drawn number in a mass: the token is the first at which the running sum exceeds it
 __device__ __forceinline__ unsigned long long drawn(float u, unsigned long long mass)
 {
@@ -148,7 +178,7 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
     const Row<DT> row(a.logits, r, a.ld, a.V);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const float T = a.temperature ? a.temperature[r] : 1.f, top_p = a.top_p ? a.top_p[r] : 1.f, min_p = a.min_p ? a.min_p[r] : 0.f, u = a.u[r];
-    const int asked = a.top_k ? a.top_k[r] : 0, top_k = T > 0.f && !(min_p > 1.f) ? asked : 1;      // nothing reaches a min_p above 1: the first token is left
+    const int top_k = most_tokens(a, r);
     auto answer = [&](int token, float lp) {
         a.tokens[r] = token;
         if (a.logprob) a.logprob[r] = lp;
@@ -174,16 +204,13 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
         if (min_p > 0.f && i > 0 && i < n && weight.real(z) < (double)min_p) keep = false;
         if (!keep) w = 0;
         // by index
-        unsigned at = 0;
-        if (i < n) {
-            const unsigned mine = (unsigned)words[i];              // ~index
-            for (unsigned j = 0; j < n; ++j) at += (unsigned)words[j] > mine;
-            mass_of[at] = w;
-        }
+        unsigned *place = lds.top.select.count;
+        ranks<BLOCK>(n, [&](unsigned j, unsigned q) { return (unsigned)words[j] > (unsigned)words[q]; }, place);      // words hold ~index
+        const unsigned at = i < n ? place[i] : 0;
+        if (i < n) mass_of[at] = w;
         __syncthreads();
         const unsigned long long w_at = i < n ? mass_of[i] : 0;
         const unsigned long long lead = scan<BLOCK>(w_at, part, all);
-        __syncthreads();
         if (i < n) mass_of[i] = lead;
         __syncthreads();
         const unsigned long long target = drawn(u, all);
@@ -271,13 +298,17 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
             }
             __syncthreads();
             // logits of the border's bin, with room for the rounding of M - z and of its product
-            const float high = M - (float)border / width * 0.999999f + fabsf(M) * 1e-6f, low = M - (float)(border + 1) / width * 1.000001f - fabsf(M) * 1e-6f;
+            const float middle = M - ((float)border + 0.5f) / width, half = (0.5f + (float)(border + 1) * 1e-6f) / width * 1.00001f + fabsf(M) * 1e-6f;
             each_slot<DT, BLOCK>(row, 0, row.slots, [&](const uint4 &raw, int s) {
                 float x[VEC];
                 Type::unpack(raw, x);
+                bool any = false;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) any |= fabsf(x[i] - middle) <= half;
+                if (!any) return;
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
-                    if (x[i] <= high && x[i] >= low && bin_of(x[i]) == border && above_floor(x[i], row.index(s, i))) {
+                    if (bin_of(x[i]) == border && above_floor(x[i], row.index(s, i))) {
                         const unsigned at = atomicAdd(&lds.top.n, 1u);
                         if (at < BORDER_LIST) lds.top.list[at] = order_word(logit_key(x[i]), row.index(s, i));
                     }
@@ -289,12 +320,17 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
                 unsigned long long *weights = lds.top.list + BORDER_LIST;
                 for (unsigned i = tid; i < n; i += BLOCK) weights[i] = weight_of(key_logit((unsigned)(lds.top.list[i] >> 32)));
                 __syncthreads();
-                for (unsigned i = tid; i < n; i += BLOCK) {
-                    const unsigned long long mine = lds.top.list[i];
-                    unsigned long long lead = above;
-#pragma unroll 4
-                    for (unsigned j = 0; j < n; ++j) lead += lds.top.list[j] > mine ? weights[j] : 0;
-                    if (lead < target && lead + weights[i] >= target) part[0] = mine;      // one word
+                // as many neighbouring lanes to a word as there are threads
+                unsigned share = 1;
+                while (share < 64 && 2 * share * n <= BLOCK) share *= 2;
+                for (unsigned t = tid; t - (t & 63) < n * share; t += BLOCK) {       // whole wavefronts
+                    const unsigned i = t / share;
+                    const unsigned long long mine = i < n ? lds.top.list[i] : 0;
+                    unsigned long long lead = 0;
+                    for (unsigned j = t % share; j < n; j += share) lead += lds.top.list[j] > mine ? weights[j] : 0;
+                    for (unsigned o = 1; o < share; o *= 2) lead += __shfl_xor(lead, o);
+                    lead += above;
+                    if (i < n && t % share == 0 && lead < target && lead + weights[i] >= target) part[0] = mine;      // one word
                 }
                 __syncthreads();
                 const unsigned long long found = part[0];
