@@ -364,7 +364,7 @@ int easgd_layer_product(int kind, int d_in, int d_out, int P, int b,
  *
  *   logits  DEVICE in  [rows][ld], row-major; a row's first V entries are its logits, entries [V, ld) are never read
  *   dtype   EASGD_F32, EASGD_BF16 or EASGD_F16: the elements of logits (and of dlogits).  Arithmetic is fp32 or wider.
- *   1 <= V <= 2^20, ld >= V, rows < 2^30; rows == 0 is a call that does nothing.
+ *   1 <= V <= 2^20, ld >= V, rows < 2^22; rows == 0 is a call that does nothing.
  * Rows may start at any element's address; every alignment takes 128-bit accesses.
  *
  * The order of a row's logits, wherever one is meant: larger logits first, equal ones (0 and -0 among them) by

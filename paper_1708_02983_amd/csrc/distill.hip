@@ -399,9 +399,20 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a)
     if (!padding) {
         if (place >= 0) z_place = row.load_one(place);
         if (threadIdx.x == 0) z_label = row.load_one(label);
-        sums.x = -INFINITY;
-        for (int i = 0; i < a.segments; ++i) sums.x = fmaxf(sums.x, a.partial[r * a.segments + i].x);
-        for (int i = 0; i < a.segments; ++i) RowSums<4, TAIL, HARD_EXP>::join(sums, a.partial[r * a.segments + i], q);
+        // a part per thread, in a fixed order
+        float4 own = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+        for (int i = threadIdx.x; i < a.segments; i += 256) {
+            const float4 p = a.partial[r * a.segments + i];
+            const float4 w = own;
+            own = make_float4(fmaxf(w.x, p.x), 0.f, 0.f, 0.f);
+            RowSums<4, TAIL, HARD_EXP>::join(own, w, q);
+            RowSums<4, TAIL, HARD_EXP>::join(own, p, q);
+        }
+        sums.x = block_max<256>(own.x, lds.fpart);
+        RowSums<4, TAIL, HARD_EXP>::join(sums, own, q);
+        sums.y = block_sum<256>(sums.y, lds.fpart);
+        sums.z = block_sum<256>(sums.z, lds.fpart);
+        sums.w = block_sum<256>(sums.w, lds.fpart);
     }
     write_loss<256>(a, r, place, z_place, z_label, padding, sums, lds);
 }
@@ -787,7 +798,7 @@ extern "C" {
 size_t easgd_distill_workspace_bytes(size_t rows, int V, int)
 {
     using namespace easgd;
-    if (rows == 0 || rows > 0x3fffffffull || V < 1 || V > LOGITS_MAX_V) return 0;
+    if (rows == 0 || rows > LOGITS_MAX_ROWS || V < 1 || V > LOGITS_MAX_V) return 0;
     const int most = segments_of(rows, most_slots(EASGD_F32, V)), least = segments_of(rows, most_slots(EASGD_BF16, V));
     return split_bytes(rows, most > least ? most : least);
 }

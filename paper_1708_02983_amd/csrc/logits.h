@@ -9,6 +9,7 @@
 namespace easgd {
 
 static constexpr int LOGITS_MAX_V = 1 << 20;      // an index fits 20 bits of an order word
+static constexpr size_t LOGITS_MAX_ROWS = ((size_t)1 << 22) - 1;
 static constexpr int LOGITS_MAX_TOP = EASGD_MAX_TOP;
 
 // one of four words by number, without an indexed register
@@ -259,7 +260,7 @@ static inline int check_logits(const char *name, const void *logits, int dtype, 
     if (V < 1) return fail(EASGD_EINVAL, "%s: V (%d) < 1", name, V);
     if (V > LOGITS_MAX_V) return fail(EASGD_ERANGE, "%s: V (%d) above %d", name, V, LOGITS_MAX_V);
     if (ld < (size_t)V) return fail(EASGD_EINVAL, "%s: ld (%zu) < V (%d)", name, ld, V);
-    if (rows > 0x3fffffffull) return fail(EASGD_ERANGE, "%s: more than 2^30-1 rows", name);
+    if (rows > LOGITS_MAX_ROWS) return fail(EASGD_ERANGE, "%s: more than %zu rows", name, LOGITS_MAX_ROWS);       // a grid has fewer than 2^32 threads
     if (rows > 1 && ld > ((size_t)1 << 60) / rows) return fail(EASGD_ERANGE, "%s: rows * ld too large", name);
     if (rows > 0 && !logits) return fail(EASGD_EINVAL, "%s: NULL pointer", name);
     if (!aligned_to(logits, dtype_bytes(dtype))) return fail(EASGD_EINVAL, "%s: logits must be aligned to their elements (%zu bytes)", name, dtype_bytes(dtype));

@@ -68,14 +68,21 @@ __global__ __launch_bounds__(BLOCK) void top_join_kernel(TopArgs a)
     __shared__ TopLds lds;
     const size_t r = blockIdx.x;
     const unsigned all = (unsigned)(a.segments * a.k);             // <= TOP_LIST
-    if (threadIdx.x == 0) {
+    if (threadIdx.x < 64) {                             // the parts' sums, a part per lane (and every 64th after it), in a fixed order
         const Scales q(a.temperature);
-        float4 s = make_float4(-INFINITY, 0.f, 0.f, 0.f);
-        for (int i = 0; i < a.segments; ++i) s.x = fmaxf(s.x, a.partial[r * a.segments + i].x);
-        for (int i = 0; i < a.segments; ++i) RowSums<4, false, HARD_PLAIN>::join(s, a.partial[r * a.segments + i], q);
-        write_lse(a, r, s);
-        lds.n = all;
+        float4 own = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+        for (int i = threadIdx.x; i < a.segments; i += 64) {
+            const float4 p = a.partial[r * a.segments + i], w = own;
+            own = make_float4(fmaxf(w.x, p.x), 0.f, 0.f, 0.f);
+            RowSums<4, false, HARD_PLAIN>::join(own, w, q);
+            RowSums<4, false, HARD_PLAIN>::join(own, p, q);
+        }
+        float4 s = make_float4(wave_max(own.x), 0.f, 0.f, 0.f);
+        RowSums<4, false, HARD_PLAIN>::join(s, own, q);
+        s.y = wave_sum(s.y);
+        if (threadIdx.x == 0) write_lse(a, r, s);
     }
+    if (threadIdx.x == 0) lds.n = all;
     for (unsigned i = threadIdx.x; i < all; i += BLOCK) lds.list[i] = a.words[r * all + i];
     __syncthreads();
     unsigned n = keep_from<BLOCK>(lds, all, FIRST_WORD);           // the words that are there
@@ -187,7 +194,7 @@ extern "C" {
 size_t easgd_top_logits_workspace_bytes(size_t rows, int V, int k)
 {
     using namespace easgd;
-    if (rows == 0 || rows > 0x3fffffffull || V < 1 || V > LOGITS_MAX_V || k < 1 || k > LOGITS_MAX_TOP) return 0;
+    if (rows == 0 || rows > LOGITS_MAX_ROWS || V < 1 || V > LOGITS_MAX_V || k < 1 || k > LOGITS_MAX_TOP) return 0;
     return top_bytes(rows, top_segments(rows, most_slots(EASGD_F32, V), k), k);     // fp32 rows have the most slots
 }
 

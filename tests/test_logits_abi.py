@@ -79,7 +79,7 @@ def test_refusals(hip, name):
     for changes in bad:
         assert call(**changes) == EINVAL, changes
         assert last().startswith(name + ":"), (changes, last())
-    far = [dict(V=(1 << 20) + 1, ld=1 << 21), dict(rows=1 << 30), dict(ld=1 << 60)]
+    far = [dict(V=(1 << 20) + 1, ld=1 << 21), dict(rows=1 << 22), dict(ld=1 << 60)]
     if call.has("dld"):
         far += [dict(V=(1 << 20) + 1, ld=1 << 21, dld=1 << 21), dict(dld=1 << 60)]
     for changes in far:
