@@ -730,10 +730,15 @@ template <int DT, int BLOCK, int NV, bool GRAD> static void launch_block(const D
 }
 
 // The block's size goes by the row's length alone, so that the forward pass adds in the same order with and without the gradient.
+// Loss and gradient in us, blocks of 256 threads that hold 4 slots a thread / 256 that hold 12 / 512 that hold 8:
+//   4096 x 8192 bf16 54 / 60 / 62      4096 x 32000 bf16 122 / 116 / 117      777 x 50001 fp16 47 / 46.5 / 53
+//   2048 x 65536 bf16 140 / 123 / 123  2048 x 131072 bf16 279 / 254 / 241
+// Short rows want many blocks a compute unit (six against four); long ones few, whose rows the last-level cache (256 MB) holds
+// between the two passes: 1024 rows under way of 256 KB are too many.
 template <int DT, bool GRAD> static void launch_rows(const DistillArgs &a, int slots, hipStream_t s)
 {
-    if (slots <= 256 * 4) launch_block<DT, 256, 4, GRAD>(a, s);
-    else if (slots <= 256 * 16) launch_block<DT, 256, 12, GRAD>(a, s);
+    if (slots <= 2048) launch_block<DT, 256, 4, GRAD>(a, s);
+    else if (slots <= 8192 + 2) launch_block<DT, 256, 12, GRAD>(a, s);
     else launch_block<DT, 512, 8, GRAD>(a, s);
 }
 
