@@ -36,7 +36,7 @@ enum { DISTILL_LOSS = 1, DISTILL_GRAD = 2, DISTILL_BOTH = 3 };
 // ---- the teacher ---------------------------------------------------------------------------------------------------
 // What a row's teacher asks for.  Its 64-bit numbers live in LDS: the registers hold the row.
 struct TeacherLds {
-    int index[LOGITS_MAX_TOP];             // -1: slot not used
+    __attribute__((aligned(16))) int index[LOGITS_MAX_TOP];       // -1: slot not used
     double log_p[LOGITS_MAX_TOP], p[LOGITS_MAX_TOP];
     double mass, rest;                     // sum of p; what it leaves over (0 without a teacher's log-sum-exp)
     double part[16];
@@ -66,7 +66,7 @@ __device__ __forceinline__ int read_teacher(const DistillArgs &a, size_t r, cons
     const double T = (double)a.temperature;
     const int place = (unsigned)slot.place < (unsigned)a.V ? slot.place : -1;
     const double logit = place >= 0 ? (double)slot.value / T : -(double)INFINITY;
-    if (tid < a.k) lds.index[tid] = place;
+    if (tid < LOGITS_MAX_TOP) lds.index[tid] = place;
     double lse;
     if constexpr (TAIL) lse = (double)a.teacher_lse[r];
     else {
@@ -87,6 +87,18 @@ __device__ __forceinline__ int read_teacher(const DistillArgs &a, size_t r, cons
     }
     __syncthreads();
     return place;
+}
+
+// how many of the first k slots name the place (index: 16-byte aligned, -1 behind the last slot up to a multiple of four)
+__device__ __forceinline__ int slots_of(const int *index, int k, int place)
+{
+    int n = 0;
+#pragma unroll 4
+    for (int i = 0; i < k; i += 4) {
+        const int4 q = *reinterpret_cast<const int4 *>(index + i);
+        n += (q.x == place) + (q.y == place) + (q.z == place) + (q.w == place);
+    }
+    return n;
 }
 
 // A bit per element of the places [first, first + 32 * words) on the row's 16-byte grid: the teacher's places.
@@ -217,10 +229,14 @@ __device__ __forceinline__ void name_places(const DistillArgs &a, size_t r, cons
     double target = 0.0;
     if (place >= max(j0, 0) && place < j1) {
         at = place;
-        for (int i = 0; i < a.k; ++i) {
-            if (lds.index[i] != place) continue;
-            if (i < (int)threadIdx.x) at = -1;
-            target += lds.p[i];
+        target = lds.p[threadIdx.x];
+        if (slots_of(lds.index, a.k, place) > 1) {      // named again: the first slot adds all up
+            target = 0.0;
+            for (int i = 0; i < a.k; ++i) {
+                if (lds.index[i] != place) continue;
+                if (i < (int)threadIdx.x) at = -1;
+                target += lds.p[i];
+            }
         }
     }
     const Factors f(a, r, lds, s);
@@ -230,9 +246,7 @@ __device__ __forceinline__ void name_places(const DistillArgs &a, size_t r, cons
         if (f.up_hard != 0.0) d += f.up_hard * (exp(x) / (double)s.z - (labelled && j == label ? 1.0 : 0.0));
         out.put(j, (float)d);
     };
-    bool alone = labelled && threadIdx.x == blockDim.x - 1 && label >= j0 && label < j1;    // a label that no slot names
-    if (alone)
-        for (int i = 0; i < a.k; ++i) alone = alone && lds.index[i] != label;
+    const bool alone = labelled && threadIdx.x == blockDim.x - 1 && label >= j0 && label < j1 && slots_of(lds.index, a.k, label) == 0;    // a label that no slot names
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {
         const int j = turn == 0 ? at : alone ? label : -1;
@@ -471,7 +485,7 @@ __global__ __launch_bounds__(256) void distill_short_kernel(DistillArgs a)
 {
     using Type = LogitType<DT>;
     constexpr int SLOTS = LOGITS_MAX_TOP / 64;
-    __shared__ int all_index[4][LOGITS_MAX_TOP];
+    __shared__ __attribute__((aligned(16))) int all_index[4][LOGITS_MAX_TOP];
     __shared__ double all_p[4][LOGITS_MAX_TOP];
     __shared__ float all_target[4][NQ * 64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -537,10 +551,8 @@ __global__ __launch_bounds__(256) void distill_short_kernel(DistillArgs a)
         p[j] = 0.0;
         if (64 * j < a.k) {
             p[j] = place[j] >= 0 ? exp(logit[j] - lse) : 0.0;
-            if (i < a.k) {
-                index[i] = place[j];
-                probability[i] = p[j];
-            }
+            index[i] = place[j];
+            probability[i] = p[j];
         }
         mass += p[j];
     }
@@ -552,12 +564,15 @@ __global__ __launch_bounds__(256) void distill_short_kernel(DistillArgs a)
 #pragma unroll
     for (int j = 0; j < SLOTS; ++j) {
         if (64 * j >= a.k) break;                       // uniform
-        double sum = 0.0;
+        double sum = p[j];
         bool first = place[j] >= 0;
-        for (int i = 0; i < a.k; ++i) {
-            if (index[i] != place[j]) continue;
-            if (i < lane + 64 * j) first = false;
-            sum += probability[i];
+        if (first && slots_of(index, a.k, place[j]) > 1) {      // named again: the first slot adds all up
+            sum = 0.0;
+            for (int i = 0; i < a.k; ++i) {
+                if (index[i] != place[j]) continue;
+                if (i < lane + 64 * j) first = false;
+                sum += probability[i];
+            }
         }
         if (first) target[place[j]] = (float)sum;
     }
