@@ -35,8 +35,8 @@ __device__ __forceinline__ int most_tokens(const SampleArgs &a, size_t r)
 // w = 2^y with y = (z - max) log2(e) / T <= 0, in 64 bits: y = j / 512 + f with |f| <= 2^-10 (adding 1.5 * 2^43 rounds to the
 // multiple of 2^-9 and leaves j in the low bits), 2^(j / 512) from a table in LDS and an exponent, 2^f from its Taylor polynomial,
 // whose remainder is below (2^-10 ln 2)^4 / 24 = 9e-15.  (The time is the 64-bit instructions': 131072 logits on one compute unit
-// 29 us; with 32 entries, as many copies as there are pairs of banks and polynomials of degree 5 33.)  Below 2^-200 the value no longer matters (a unit is at least 2^-51 of
-// the largest weight, min_p at least 2^-149).
+// 29 us; with 32 entries, as many copies as there are pairs of banks and polynomials of degree 5 33.)  Below 2^-200 the value no
+// longer matters (a unit is at least 2^-51 of the largest weight, min_p at least 2^-149).
 static constexpr int WEIGHT_TABLE = 512;
 struct Weight {
     double scale, max;        // log2(e) / T
@@ -53,40 +53,48 @@ struct Weight {
         __syncthreads();
     }
     static __device__ __forceinline__ double power(int n) { return __builtin_bit_cast(double, (unsigned long long)(n + 1023) << 52); }
-    // 2^y units as factors that are still to be multiplied
-    __device__ __forceinline__ void split(float z, double &a, double &b) const
+    // 2^y units, not yet whole; no branch, so that the elements of a slot are computed side by side (256 rows of 131072 with one
+    // top_p: 112 us, 125 us with each element's own branches).  Product and sum stay two roundings wherever a logit's units are
+    // asked for: joined in some places and not in others, two passes could disagree by a unit.
+    __device__ __forceinline__ double scaled(float z) const
     {
+#pragma clang fp contract(off)
         const double y = fmax(((double)z - max) * scale, -200.0), t = y + 0x1.8p43, f = y - (t - 0x1.8p43);
         const int j = (int)(unsigned)__builtin_bit_cast(unsigned long long, t);
         const unsigned long long e = __builtin_bit_cast(unsigned long long, table[j & (WEIGHT_TABLE - 1)]);
-        a = __builtin_bit_cast(double, e + ((unsigned long long)(unsigned)((j >> 9) << 20) << 32));
-        b = fma(fma(fma(5.5504108664821576e-02, f, 2.4022650695910069e-01), f, 6.9314718055994529e-01), f, 1.0);
+        const double a = __builtin_bit_cast(double, e + ((unsigned long long)(unsigned)((j >> 9) << 20) << 32));
+        return a * fma(fma(fma(5.5504108664821576e-02, f, 2.4022650695910069e-01), f, 6.9314718055994529e-01), f, 1.0);
+    }
+    template <int VEC> __device__ __forceinline__ void scaled(const float (&z)[VEC], double (&w)[VEC]) const
+    {
+        if (infinite) {                                 // uniform: logits are in or out
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) w[i] = z[i] == top ? power(unit) : 0.0;
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) w[i] = scaled(z[i]);
+        }
     }
     // adding 2^52 rounds to the nearest whole number and leaves it in the low bits of the sum (units <= 2^51)
     static constexpr unsigned long long BIAS = 0x4330000000000000ull;
-    __device__ __forceinline__ unsigned long long biased_units(float z) const
+    static __device__ __forceinline__ unsigned long long biased(double w)
     {
-        if (infinite) return BIAS + (z == top ? 1ull << unit : 0ull);        // uniform
-        double a, b;
-        split(z, a, b);
-        return __builtin_bit_cast(unsigned long long, fma(a, b, 0x1p52));
+#pragma clang fp contract(off)
+        return __builtin_bit_cast(unsigned long long, w + 0x1p52);
     }
-    __device__ __forceinline__ unsigned long long units(float z) const { return biased_units(z) - BIAS; }
+    __device__ __forceinline__ unsigned long long units(float z) const
+    {
+        const float one[1] = {z};
+        double w[1];
+        scaled<1>(one, w);
+        return biased(w[0]) - BIAS;
+    }
     __device__ __forceinline__ double real(float z) const
     {
-        if (infinite) return z == top ? 1.0 : 0.0;
-        double a, b;
-        split(z, a, b);
-        return a * b * power(-unit);
-    }
-    // units, or 0 where there is a limit (in units, not whole) and w is below it
-    __device__ __forceinline__ unsigned long long units_from(float z, bool limited, double limit) const
-    {
-        if (infinite) return units(z);                  // w is 0 or 1
-        double a, b;
-        split(z, a, b);
-        if (limited && a * b < limit) return 0;
-        return __builtin_bit_cast(unsigned long long, fma(a, b, 0x1p52)) - BIAS;
+        const float one[1] = {z};
+        double w[1];
+        scaled<1>(one, w);
+        return w[0] * power(-unit);
     }
     // log of w over a mass
     __device__ __forceinline__ float log_share(float z, unsigned long long mass) const
@@ -255,13 +263,16 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
         unsigned long long far = 0;
         each_slot<DT, BLOCK>(row, 0, row.slots, [&](const uint4 &raw, int s) {
             float x[VEC];
+            double w[VEC];
             Type::unpack(raw, x);
+            if constexpr (BY_MASS) weight.template scaled<VEC>(x, w);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
                 if (!above_floor(x[i], row.index(s, i))) continue;
+                const unsigned long long weight_here = BY_MASS ? Weight::biased(w[i]) - Weight::BIAS : 1ull;
                 const int b = bin_of(x[i]);
-                if (b < MASS_BINS - 1) atomicAdd(&lds.mass.mass[b], weight_of(x[i]));
-                else far += weight_of(x[i]);
+                if (b < MASS_BINS - 1) atomicAdd(&lds.mass.mass[b], weight_here);
+                else far += weight_here;
             }
         });
         __syncthreads();
@@ -361,25 +372,36 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
     const float floor_logit = key_logit(max((unsigned)(floor >> 32), 0x00800000u));
     const unsigned floor_index = ~(unsigned)floor;     // the last of the floor's value that is kept
     const double least_mass = (double)min_p * Weight::power(a.unit);
-    auto kept_units = [&](float x, int index) -> unsigned long long {
-        if (!(x >= least) || (x == floor_logit && (unsigned)index > floor_index)) return 0;
-        return weight.units_from(x, filtered, least_mass);
+    // units of a slot's elements, 0 for those that are not kept
+    auto kept_units = [&](const float (&x)[VEC], int s, unsigned long long (&u)[VEC]) {
+        double w[VEC];
+        weight.template scaled<VEC>(x, w);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const bool out = !(x[i] >= least) | ((x[i] == floor_logit) & ((unsigned)row.index(s, i) > floor_index)) |
+                             (filtered & (w[i] < least_mass));
+            u[i] = out ? 0 : Weight::biased(w[i]) - Weight::BIAS;
+        }
     };
     auto slot_units = [&](const uint4 &raw, int s) {
         unsigned long long sum = 0;
         float x[VEC];
         Type::unpack(raw, x);
         if (whole) {                                    // uniform: masked logits (-inf and NaN) are all that is not kept
+            double w[VEC];
+            weight.template scaled<VEC>(x, w);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) sum += x[i] >= -FLT_MAX ? weight.biased_units(x[i]) : Weight::BIAS;
+            for (int i = 0; i < VEC; ++i) sum += x[i] >= -FLT_MAX ? Weight::biased(w[i]) : Weight::BIAS;
             return sum - VEC * Weight::BIAS;
         }
         float t = x[0];
 #pragma unroll
         for (int i = 1; i < VEC; ++i) t = fmaxf(t, x[i]);
         if (t >= least) {
+            unsigned long long u[VEC];
+            kept_units(x, s, u);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) sum += kept_units(x[i], row.index(s, i));
+            for (int i = 0; i < VEC; ++i) sum += u[i];
         }
         return sum;
     };
@@ -415,12 +437,13 @@ __global__ __launch_bounds__(BLOCK) void sample_kernel(SampleArgs a)
         unsigned long long at = before + scan<BLOCK>(mine, part, all);
         if (at <= target && target - at < mine) {
             float x[VEC];
+            unsigned long long w[VEC];
             Type::unpack(raw, x);
+            kept_units(x, s, w);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                const unsigned long long w = kept_units(x[i], row.index(s, i));
-                if (at <= target && target - at < w) answer(row.index(s, i), weight.log_share(x[i], total));
-                at += w;
+                if (at <= target && target - at < w[i]) answer(row.index(s, i), weight.log_share(x[i], total));
+                at += w[i];
             }
         }
         before += all;
