@@ -14,6 +14,8 @@ Only ``tests/``, ``__graft_entry__.smoke()`` and the ``cpu_baseline`` leg of
   (an extension; numpy; the stored 16-bit code is decided in fp32, the rest in double)
 * ``oracle.mlp_grad`` -- per-worker minibatch gradient of a dense ReLU MLP with
   softmax cross-entropy (numpy, double arithmetic)
+* ``oracle.logits``  -- rows of logits: top logits, distillation and its gradient, sampled tokens, and the gradient of a
+  network under the distillation loss (numpy, double arithmetic)
 """
 from .elastic import (async_easgd, build, easgd_round, measgd_round, num_threads, set_num_threads,  # noqa: F401
                       sync_sgd_round)

@@ -217,6 +217,12 @@ template <int BLOCK> __device__ __forceinline__ float floor_of(float t, unsigned
 // The order words of the first k (<= LOGITS_MAX_TOP) elements of slots [s0, s1), in the order, at the front of lds.list; returns
 // how many there are (fewer than k where fewer are above -inf).  seen(x, slot) is called for every slot by whole wavefronts
 // (an empty slot where a lane has none).  Ends with a barrier.
+//
+// One pass.  The maxima of BLOCK threads over their first slots are logits of the row, so the k-th largest of them is at most
+// the k-th largest logit: a floor that leaves a few hundred of 131072 logits, found with one pass over bins in LDS.  What
+// reaches the floor goes to a list in LDS, and the floor rises to the list's k-th word whenever the list has grown.  A row that
+// overruns the list (ascending logits, many equal ones) is walked digit by digit instead.  (2048 x 131072 bf16, k = 64: 826 us
+// with that walk for every row, five passes; 167 this way.)
 template <int DT, int BLOCK, typename F>
 __device__ __forceinline__ unsigned first_of(const Row<DT> &row, int s0, int s1, unsigned k, TopLds &lds, F seen)
 {

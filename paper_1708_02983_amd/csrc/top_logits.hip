@@ -38,6 +38,9 @@ __device__ __forceinline__ void write_list(const TopArgs &a, size_t r, const uns
 }
 
 // ---- a block per row, or per part of a row ------------------------------------------------------------------------------
+// Measured: 2048 x 131072 bf16, k = 64, 167 us = 3.2 TB/s: the vector ALUs are busy 70 to 80 % of it (141 instructions a
+// wavefront for 64 slots: unpacking, an exponential, sum and comparison for each of eight logits), the rest is barriers between
+// the four loads in flight.
 template <int DT, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void top_rows_kernel(TopArgs a)
 {
@@ -62,6 +65,7 @@ __global__ __launch_bounds__(BLOCK) void top_rows_kernel(TopArgs a)
 }
 
 // ---- the parts of a row together ------------------------------------------------------------------------------------------
+// Bound: latency.  8 x 50001 fp16, k = 20: parts 12.3 us, this kernel 4.6; a block per row took 79 us with the digits' walk.
 template <int BLOCK>
 __global__ __launch_bounds__(BLOCK) void top_join_kernel(TopArgs a)
 {
@@ -93,7 +97,7 @@ __global__ __launch_bounds__(BLOCK) void top_join_kernel(TopArgs a)
 
 // ---- short rows: a wavefront each ---------------------------------------------------------------------------------------------
 // Element lane + 64 q sits in register q.  The k-th largest key is found bit by bit with votes; equal keys are taken by
-// ascending index, which is the order of registers, then lanes.
+// ascending index, which is the order of registers, then lanes.  Bound: the votes' latency.  2048 x 1000 fp32, k = 10: 10.8 us.
 template <int DT, int NQ>
 __global__ __launch_bounds__(256) void top_short_kernel(TopArgs a)
 {
