@@ -101,6 +101,22 @@ __device__ __forceinline__ int slots_of(const int *index, int k, int place)
     return n;
 }
 
+// The probabilities of the slots that name a place, added in their order; `first` becomes the first of them.  Every slot is read, named
+// or not, so that the reads run ahead (one trip to LDS after the other takes 50 us for 200 slots).
+__device__ __forceinline__ double mass_of(const int *index, const double *p, int k, int place, int &first)
+{
+    double sum = 0.0;
+    first = k;
+#pragma unroll 8
+    for (int i = 0; i < k; ++i) {
+        const bool named = index[i] == place;
+        const double here = p[i];
+        sum += named ? here : 0.0;
+        first = min(first, named ? i : k);
+    }
+    return sum;
+}
+
 // A bit per element of the places [first, first + 32 * words) on the row's 16-byte grid: the teacher's places.
 __device__ __forceinline__ void mark_places(unsigned *bits, int words, int first, int place, int shift, int block)
 {
@@ -231,12 +247,9 @@ __device__ __forceinline__ void name_places(const DistillArgs &a, size_t r, cons
         at = place;
         target = lds.p[threadIdx.x];
         if (slots_of(lds.index, a.k, place) > 1) {      // named again: the first slot adds all up
-            target = 0.0;
-            for (int i = 0; i < a.k; ++i) {
-                if (lds.index[i] != place) continue;
-                if (i < (int)threadIdx.x) at = -1;
-                target += lds.p[i];
-            }
+            int first;
+            target = mass_of(lds.index, lds.p, a.k, place, first);
+            if (first < (int)threadIdx.x) at = -1;
         }
     }
     const Factors f(a, r, lds, s);
@@ -489,7 +502,8 @@ __global__ __launch_bounds__(BLOCK) void distill_grad_kernel(DistillArgs a)
 // Rows of at most 64 * NQ logits sit in a wavefront's registers, element lane + 64 q in x[q]; maximum and sums are shuffles,
 // and nothing waits for other wavefronts.  LDS holds the teacher's slots and, for every element, its target (-1: not one
 // of the teacher's places).  Bound: latency (one trip to memory, two chains of 64-bit exponentials and logarithms).
-// Measured: 2048 x 100 fp32 7.4 us, of which a launch that does nothing is some 2.
+// Measured: 2048 x 100 fp32 7.4 us, of which a launch that does nothing is some 2.  Beyond 1024 logits a block a row is faster
+// (16384 x 2040 bf16: 136 us, 202 with 32 registers a lane here).
 template <int DT, int NQ, bool TAIL, int MODE>
 __global__ __launch_bounds__(256) void distill_short_kernel(DistillArgs a)
 {
@@ -571,21 +585,40 @@ __global__ __launch_bounds__(256) void distill_short_kernel(DistillArgs a)
 #pragma unroll
     for (int c = 0; c < NQ; ++c) target[lane + 64 * c] = -1.f;
     in_order();
+    // a place that is named again: its first slot adds all up, in their order.  A lane's slots go through the teacher's together.
+    int named[SLOTS] = {}, first[SLOTS];
+    double sum[SLOTS];
+#pragma unroll 2
+    for (int i = 0; i < a.k; i += 4) {
+        const int4 q = *reinterpret_cast<const int4 *>(index + i);
+#pragma unroll
+        for (int j = 0; j < SLOTS; ++j) named[j] += (q.x == place[j]) + (q.y == place[j]) + (q.z == place[j]) + (q.w == place[j]);
+    }
+    bool again = false;
 #pragma unroll
     for (int j = 0; j < SLOTS; ++j) {
-        if (64 * j >= a.k) break;                       // uniform
-        double sum = p[j];
-        bool first = place[j] >= 0;
-        if (first && slots_of(index, a.k, place[j]) > 1) {      // named again: the first slot adds all up
-            sum = 0.0;
-            for (int i = 0; i < a.k; ++i) {
-                if (index[i] != place[j]) continue;
-                if (i < lane + 64 * j) first = false;
-                sum += probability[i];
+        again |= place[j] >= 0 && named[j] > 1;
+        first[j] = lane + 64 * j;
+        sum[j] = p[j];
+    }
+    if (__any(again)) {
+#pragma unroll
+        for (int j = 0; j < SLOTS; ++j) sum[j] = 0.0;
+#pragma unroll 4
+        for (int i = 0; i < a.k; ++i) {
+            const int here = index[i];
+            const double mass_here = probability[i];
+#pragma unroll
+            for (int j = 0; j < SLOTS; ++j) {
+                const bool is = here == place[j];
+                sum[j] += is ? mass_here : 0.0;
+                first[j] = min(first[j], is ? i : LOGITS_MAX_TOP);
             }
         }
-        if (first) target[place[j]] = (float)sum;
     }
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j)
+        if (place[j] >= 0 && first[j] == lane + 64 * j) target[place[j]] = (float)sum[j];
     in_order();
 
     // maximum and sums
