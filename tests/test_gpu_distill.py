@@ -120,6 +120,27 @@ def test_sizes(dtype, rows, V, k):
               dloss=rng.uniform(0.5, 2.0, rows).astype(F), dpad=(0, 3, 0, 1, 0)[n], doffset=(0, 1, 2, 0, 5)[n])
 
 
+@pytest.mark.parametrize("V, k", [(10, 256), (100, 256), (900, 200), (1024, 65), (1500, 256), (40000, 130)])
+def test_places_named_many_times(V, k):
+    """Places drawn with repetition from few and from all; one place in every slot; between slots that are not used."""
+    rng = np.random.default_rng(V + k)
+    rows, T = 6, 2.0
+    z = rng.normal(0, 2.0, (rows, V))
+    idx = rng.integers(0, V, (rows, k)).astype(np.int32)
+    idx[1] = rng.integers(0, min(V, 7), k)
+    idx[2] = V - 1
+    idx[3, ::2] = -1
+    idx[4] = np.where(np.arange(k) % 64 == 63, 3, V)
+    idx[5] = idx[5, ::-1] // 2
+    val = rng.normal(0.0, 2.0, (rows, k)).astype(F)
+    used = (idx >= 0) & (idx < V)
+    lse = (np.log(np.where(used, np.exp(val.astype(np.float64) / T), 0.0).sum(axis=1)) + 0.25).astype(F)
+    labels = rng.integers(0, V, rows).astype(np.int32)
+    labels[2] = V - 1
+    for tail, hard in ((False, 0.0), (True, 0.3)):
+        check(z, idx, val, lse if tail else None, labels if hard else None, T, hard, "fp32", scale=4.0)
+
+
 @pytest.mark.parametrize("V, rows", [(262144, 2), (1048576, 1)])
 def test_longest_rows(V, rows):
     rng = np.random.default_rng(1)
