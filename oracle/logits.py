@@ -14,18 +14,20 @@ def order(z):
     return there[np.lexsort((there, -z[there]))]
 
 
-def logsumexp(z):
+def logsumexp(z, T=1.0):
+    """Differences are taken before they are divided: quotients of large logits would round away what they differ by."""
     z = np.asarray(z, np.float64)
     m = z.max() if z.size else -np.inf
     if not np.isfinite(m):
         return m
-    return m + np.log(np.exp(z - m).sum())
+    return m / T + np.log(np.exp((z - m) / T).sum())
 
 
-def log_softmax(z):
+def log_softmax(z, T=1.0):
     """The maximum is taken off first: logits near the ends of a type's range would absorb the logarithm of the sum."""
     z = np.asarray(z, np.float64)
-    return (z - z.max()) - np.log(np.exp(z - z.max()).sum())
+    t = (z - z.max()) / T
+    return t - np.log(np.exp(t).sum())
 
 
 def top_logits(z, k, temperature=1.0):
@@ -34,7 +36,7 @@ def top_logits(z, k, temperature=1.0):
     first = order(z)[:k]
     values, indices = np.full(k, -np.inf), np.full(k, -1, np.int64)
     values[:len(first)], indices[:len(first)] = z[first], first
-    lse = np.inf if (z == np.inf).any() else np.nan if np.isnan(z).any() else logsumexp(z / temperature)
+    lse = np.inf if (z == np.inf).any() else np.nan if np.isnan(z).any() else logsumexp(z, temperature)
     return values, indices, lse
 
 
@@ -63,7 +65,7 @@ def distill(z, indices, values, teacher_lse=None, label=None, temperature=1.0, h
     if not (z > -np.inf).any() and not np.isnan(z).any():
         return zero
     used, p, log_p, target = _teacher(V, indices, values, teacher_lse, T)
-    log_q = log_softmax(z / T)
+    log_q = log_softmax(z, T)
     q = np.exp(log_q)
     places = np.unique(np.asarray(indices)[used])
     outside = np.ones(V, bool)

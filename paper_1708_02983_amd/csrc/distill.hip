@@ -170,10 +170,11 @@ struct Factors {
         outside = rest > 0.0 ? cover - rest * (double)s.y / (double)s.w : cover;
     }
 };
-struct Slope {
+template <int VEC> struct Slope {
     float fq, f1;
-    Reference at;
+    Reference<VEC> at;
     bool none;                 // nothing to learn: the gradient is 0
+    bool apart;                // a row of large logits: its elements go through of_apart()
     __device__ __forceinline__ Slope(const DistillArgs &a, size_t r, const TeacherLds &teacher, bool padding, const float4 &s, const Scales &q)
         : at(uniform(s.x), q)
     {
@@ -181,8 +182,17 @@ struct Slope {
         const Factors f(a, r, teacher, s);
         fq = uniform((float)(f.soft * f.outside / (double)s.y) * exp2_fast(-at.lost));
         f1 = a.hard > 0.f ? uniform((float)(f.up_hard / (double)s.z) * exp2_fast(-at.lost1)) : 0.f;
+        apart = at.by_difference();
     }
-    template <int HARD, int VEC> __device__ __forceinline__ void of(float (&x)[VEC]) const
+    __device__ __forceinline__ void of_apart(float (&x)[VEC], const Scales &q) const
+    {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const float d = x[i] - at.ref;
+            x[i] = fmaf(f1, exp2_fast(d * q.c1), fq * exp2_fast(d * q.c));
+        }
+    }
+    template <int HARD> __device__ __forceinline__ void of(float (&x)[VEC]) const
     {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
@@ -233,6 +243,28 @@ template <int DT> struct GradRow {
         for (int s = first + threadIdx.x; s < last; s += block) store(s, zero, s * VEC >= shift && (s + 1) * VEC <= shift + V);
     }
 };
+
+// The gradient of slots [s0, s1) where Slope asks for the careful way.
+template <int DT, int BLOCK>
+__device__ __forceinline__ void put_apart(const Row<DT> &row, const GradRow<DT> &out, const Slope<Row<DT>::VEC> &g, const Scales &q, int s0, int s1)
+{
+    constexpr int VEC = Row<DT>::VEC, DEEP = 2;
+#pragma unroll 1
+    for (int s = s0 + (int)threadIdx.x; s < s1; s += DEEP * BLOCK) {
+        uint4 v[DEEP];
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i)
+            if (s + i * BLOCK < s1) v[i] = row.load(s + i * BLOCK);
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) {
+            if (s + i * BLOCK >= s1) break;
+            float x[VEC];
+            Row<DT>::Type::unpack(v[i], x);
+            g.of_apart(x, q);
+            out.store(s + i * BLOCK, x, row.full(s + i * BLOCK));
+        }
+    }
+}
 
 // The places that the teacher or the label names, within elements [j0, j1) (j0 may lie before the row): each once, by the
 // first slot that names it, after a barrier behind the stores of all others.
@@ -286,7 +318,7 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
     const size_t r = blockIdx.x;
     const Row<DT> row(a.logits, r, a.ld, a.V);
     const int tid = threadIdx.x;
-    const Scales q(a.temperature);
+    const Scales q(a.temperature, a.hard > 0.f);
     const int label = a.labels ? a.labels[r] : 0;
     const bool padding = (unsigned)label >= (unsigned)a.V;
     Slot slot;
@@ -340,15 +372,17 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
     }
     if constexpr (GRAD) {
         const GradRow<DT> out(a, r, row);
-        const Slope g(a, r, lds, padding, sums, q);
+        const Slope<VEC> g(a, r, lds, padding, sums, q);
         auto put = [&](const uint4 &raw, int s, bool full) {
             float x[VEC];
             Type::unpack(raw, x);
-            g.template of<HARD, VEC>(x);
+            g.template of<HARD>(x);
             out.store(s, x, full);
         };
         if (g.none) {                                   // uniform
             out.clear(row.slots, BLOCK);
+        } else if (g.apart) {                           // uniform, and rare: the row is read again
+            put_apart<DT, BLOCK>(row, out, g, q, 0, row.slots);
         } else {
             for (int s0 = f0 + tid + NV * BLOCK; s0 < f1; s0 += DEEP * BLOCK) {
                 uint4 w[DEEP];
@@ -386,7 +420,7 @@ __global__ __launch_bounds__(BLOCK) void distill_sums_kernel(DistillArgs a)
     const int seg = blockIdx.x % a.segments;
     const Row<DT> row(a.logits, r, a.ld, a.V);
     const int tid = threadIdx.x;
-    const Scales q(a.temperature);
+    const Scales q(a.temperature, a.hard > 0.f);
     if (a.labels && (unsigned)a.labels[r] >= (unsigned)a.V) return;
     const int s0 = seg * a.seg_slots, s1 = min(s0 + a.seg_slots, row.slots);
     if constexpr (TAIL) {
@@ -422,7 +456,7 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a)
     __shared__ TeacherLds lds;
     const size_t r = blockIdx.x;
     const Row<DT> row(a.logits, r, a.ld, a.V);
-    const Scales q(a.temperature);
+    const Scales q(a.temperature, a.hard > 0.f);
     const int label = a.labels ? a.labels[r] : 0;
     const bool padding = (unsigned)label >= (unsigned)a.V;
     Slot slot;
@@ -464,7 +498,7 @@ __global__ __launch_bounds__(BLOCK) void distill_grad_kernel(DistillArgs a)
     const int seg = blockIdx.x % a.segments;
     const Row<DT> row(a.logits, r, a.ld, a.V);
     const int tid = threadIdx.x;
-    const Scales q(a.temperature);
+    const Scales q(a.temperature, a.hard > 0.f);
     const int label = a.labels ? a.labels[r] : 0;
     const bool padding = (unsigned)label >= (unsigned)a.V;
     const int s0 = seg * a.seg_slots, s1 = min(s0 + a.seg_slots, row.slots);
@@ -472,12 +506,12 @@ __global__ __launch_bounds__(BLOCK) void distill_grad_kernel(DistillArgs a)
     slot.load(a, r);
     const int place = read_teacher<BLOCK, TAIL>(a, r, slot, lds);
     const float4 sums = reinterpret_cast<const float4 *>(a.state)[r];
-    const Slope g(a, r, lds, padding, sums, q);
+    const Slope<VEC> g(a, r, lds, padding, sums, q);
     const GradRow<DT> out(a, r, row);
     auto put = [&](const uint4 &raw, int s) {
         float x[VEC];
         Type::unpack(raw, x);
-        g.template of<HARD, VEC>(x);
+        g.template of<HARD>(x);
         out.store(s, x, row.full(s));
     };
     int s = s0 + tid;
@@ -486,6 +520,10 @@ __global__ __launch_bounds__(BLOCK) void distill_grad_kernel(DistillArgs a)
         return;
     }
     const float z_place = place >= 0 ? row.load_one(place) : 0.f, z_label = row.load_one(label);
+    if (g.apart) {                                      // uniform, and rare
+        put_apart<DT, BLOCK>(row, out, g, q, s0, s1);
+        s = s1;
+    }
     for (; s - tid + DEEP * BLOCK <= s1; s += DEEP * BLOCK) {
         uint4 v[DEEP];
 #pragma unroll
@@ -522,7 +560,7 @@ __global__ __launch_bounds__(256) void distill_short_kernel(DistillArgs a)
     auto in_order = []() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); };
 
     const Row<DT> row(a.logits, r, a.ld, a.V);
-    const Scales q(a.temperature);
+    const Scales q(a.temperature, a.hard > 0.f);
     const double T = (double)a.temperature;
     const int label = a.labels ? a.labels[r] : 0;
     const bool padding = (unsigned)label >= (unsigned)a.V, hard = a.hard > 0.f;

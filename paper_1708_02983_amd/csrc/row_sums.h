@@ -11,29 +11,37 @@ enum { HARD_PLAIN = 0, HARD_SQUARE = 1, HARD_EXP = 2 };
 __device__ __forceinline__ float uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
 
 struct Scales {
-    float c, c1;              // log2(e) / T, log2(e)
-    __device__ __forceinline__ explicit Scales(float temperature) : c((float)(LOG2E / (double)temperature)), c1((float)LOG2E) {}
+    float c, c1;              // log2(e) / T, and log2(e) where a cross-entropy asks for it
+    __device__ __forceinline__ explicit Scales(float temperature, bool hard = false) : c((float)(LOG2E / (double)temperature)), c1(hard ? (float)LOG2E : c) {}
 };
 
 // Exponentials relative to a logit `ref`: 2^((x - ref) c) in one fused multiply-add and one exponential, as 2^(x c - rc) with
 // rc = ref * c rounded once for all; what that rounding takes from every exponent alike, `lost`, is known exactly and goes
-// into the row's factors.  Where ref is so large that ref * c might overflow (rows of fp32's lowest value), every
-// other logit is at least one unit of 2^-23 ref away and its exponential 0 or infinite at any scale: a power of two, exact, does.
-struct Reference {
+// into the row's factors.  That holds as long as `lost` is small, at most half a unit for |ref| c < 2^24.  Beyond:
+//   * where even the type's next value is more than 2^8 units of the exponent away (2^-24 of ref for fp32, 2^-12 for fp16, more for
+//     bfloat16), every other logit's exponential is 0 or infinite at any such scale, and a power of two, which multiplies exactly, does;
+//   * between the two (fp32 logits from 2^24 T to 2^32 T, and some mixed temperatures) the difference comes first and is scaled then: an
+//     instruction more a logit.  c is NaN there, so that the loops that do not know of it (one comparison a slot) find their sum to
+//     be no number and look closer.
+template <int VEC> struct Reference {
     float ref, c, c1, rc, rc1, lost, lost1;
     __device__ __forceinline__ Reference(const Scales &q) : ref(-INFINITY), c(q.c), c1(q.c1), rc(0.f), rc1(0.f), lost(0.f), lost1(0.f) {}
     __device__ __forceinline__ Reference(float r, const Scales &q) { set(r, q); }
     __device__ __forceinline__ void set(float r, const Scales &q)
     {
-        const bool huge = fabsf(r) * fmaxf(q.c, q.c1) >= 0x1p100f;
+        constexpr float APART = VEC == 4 ? 0x1p32f : 0x1p20f;
+        const float most = fabsf(r) * fmaxf(q.c, q.c1), least = fabsf(r) * fminf(q.c, q.c1);
         ref = r;
-        c = huge ? 0x1p-40f : q.c;
-        c1 = huge ? 0x1p-40f : q.c1;
+        c = q.c;
+        c1 = q.c1;
+        if (least >= APART) c = c1 = __uint_as_float((294u - (__float_as_uint(r) >> 23 & 255u)) << 23);      // |r| c in [2^40, 2^41)
+        else if (most >= 0x1p24f) c = c1 = NAN;
         rc = r * c;
         rc1 = r * c1;
-        lost = fmaf(r, c, -rc);                        // the exponents are this much too large
-        lost1 = fmaf(r, c1, -rc1);
+        lost = by_difference() ? 0.f : fmaf(r, c, -rc);               // the exponents are this much too large
+        lost1 = by_difference() ? 0.f : fmaf(r, c1, -rc1);
     }
+    __device__ __forceinline__ bool by_difference() const { return isnan(c); }
     __device__ __forceinline__ float soft(float x) const { return exp2_fast(fmaf(x, c, -rc)); }
     __device__ __forceinline__ float hard(float x) const { return exp2_fast(fmaf(x, c1, -rc1)); }
 };
@@ -43,7 +51,7 @@ struct Reference {
 // so that the loop over a row needs neither a maximum nor a rescaling, only a comparison per 128 bits.
 template <int VEC, bool TAIL, int HARD> struct RowSums {
     const Scales &q;
-    Reference at;
+    Reference<VEC> at;
     float st = 0.f, s1 = 0.f, so = 0.f;
 
     __device__ __forceinline__ RowSums(const Scales &q) : q(q), at(q) {}
@@ -66,12 +74,27 @@ template <int VEC, bool TAIL, int HARD> struct RowSums {
                 high = high || !(h <= 0x1p24f);
             }
             if (at.ref > -INFINITY && !__any(high)) break;      // uniform for the wavefront, and nearly always
+            if (at.by_difference()) {                   // uniform
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) e[i] = exp2_fast((x[i] - at.ref) * q.c);
+                sum = e[0];
+#pragma unroll
+                for (int i = 1; i < VEC; ++i) sum += e[i];
+                high = !(sum <= 0x1p24f);
+                if constexpr (HARD == HARD_EXP) {
+                    h = exp2_fast((x[0] - at.ref) * q.c1);
+#pragma unroll
+                    for (int i = 1; i < VEC; ++i) h += exp2_fast((x[i] - at.ref) * q.c1);
+                    high = high || !(h <= 0x1p24f);
+                }
+                if (!__any(high)) break;
+            }
             float t = x[0];
 #pragma unroll
             for (int i = 1; i < VEC; ++i) t = fmaxf(t, x[i]);
             t = uniform(wave_max(t));
             if (!(t > at.ref)) break;
-            const Reference old = at;
+            const Reference<VEC> old = at;
             at.set(t, q);
             const float f = change(old, at, q.c, old.lost, at.lost), f1 = change(old, at, q.c1, old.lost1, at.lost1);
             st *= f;
@@ -92,7 +115,7 @@ template <int VEC, bool TAIL, int HARD> struct RowSums {
         }
     }
     // what sums relative to `old` are multiplied with to be relative to `now`
-    __device__ static __forceinline__ float change(const Reference &old, const Reference &now, float c, float old_lost, float now_lost)
+    __device__ static __forceinline__ float change(const Reference<VEC> &old, const Reference<VEC> &now, float c, float old_lost, float now_lost)
     {
         return old.ref == -INFINITY ? 1.f : exp2_fast((old.ref - now.ref) * c - old_lost + now_lost);
     }
