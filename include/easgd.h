@@ -401,7 +401,8 @@ int easgd_top_logits(const void *logits, int dtype, size_t rows, int V, size_t l
  *   teacher_lse == NULL:  p_i = exp(a_i/T) / sum_i exp(a_i/T)         the teacher's probabilities, renormalised over S
  *   teacher_lse != NULL:  p_i = exp(a_i/T - teacher_lse)              the teacher's probabilities; what they leave over,
  *                         r = max(0, 1 - sum_i p_i), R = sum of q outside S   is the probability of "any other place"
- *   KL   = sum_i p_i (log p_i - log q[t_i])  (+ r (log r - log R); left out where r == 0 or no place outside S has mass)
+ *   KL   = sum_i p_i (log p_i - log q[t_i])  (+ r (log r - log R); left out where r == 0 or no logit outside S is above -inf.
+ *                                             log R is right however small R is, also where R itself is beyond fp32.)
  *   loss = (1 - hard) T^2 KL + hard (log sum_j exp(z[j]) - z[y])
  *   d loss / d z[j] = (1 - hard) T (c q[j] - sum of p_i with t_i == j - (j outside S: r q[j] / R)) + hard (softmax(z)[j] - (j == y))
  *                     with c = sum_i p_i (+ r where its term counts)
@@ -414,7 +415,8 @@ int easgd_top_logits(const void *logits, int dtype, size_t rows, int V, size_t l
  *                                            logits are not read, its loss and gradient are 0.
  *   loss         DEVICE out [rows] fp32
  *   state        DEVICE out [rows][4] fp32, 16-byte aligned   for the backward pass: m (the largest logit, or one near it), sum exp((z-m)/T), sum exp(z-m) (unused
- *                                            where hard is 0), the first sum over the places outside S (0 without teacher_lse)
+ *                                            where hard is 0), the first sum over the places outside S (0 without teacher_lse; where it
+ *                                            is below 2^-64 the backward pass sums the row's logits again)
  *   scale, dloss     the gradient is that of scale * sum over the rows of dloss[row] * loss[row]; dloss DEVICE in [rows] fp32, or
  *                    NULL: all 1.  (Mean losses of b samples: scale = 1/b.)
  *   dlogits      DEVICE out [rows][dld], element type of logits; entries [V, dld) of a row are not written; aligned like

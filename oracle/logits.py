@@ -70,19 +70,19 @@ def distill(z, indices, values, teacher_lse=None, label=None, temperature=1.0, h
     places = np.unique(np.asarray(indices)[used])
     outside = np.ones(V, bool)
     outside[places] = False
-    R = q[outside].sum()
+    log_R = logsumexp(log_q[outside])        # R itself may be too small for 64 bits
     r = max(0.0, 1.0 - p.sum()) if teacher_lse is not None else 0.0
-    if R == 0.0:
+    if log_R == -np.inf:
         r = 0.0
     kl = 0.0
     for i in np.flatnonzero(p > 0):
         kl += p[i] * (log_p[i] - log_q[indices[i]])
     if r > 0.0:
-        kl += r * (np.log(r) - np.log(R))
+        kl += r * (np.log(r) - log_R)
     c = p.sum() + r
     soft = c * q - target
     if r > 0.0:
-        soft[outside] -= r * q[outside] / R
+        soft[outside] -= r * np.exp(log_q[outside] - log_R)
     loss, grad = 0.0, np.zeros(V)
     if hard < 1.0:
         loss += (1.0 - hard) * T * T * kl

@@ -131,10 +131,65 @@ template <int VEC> __device__ __forceinline__ unsigned marks_of(const unsigned *
     return (bits[slot * VEC >> 5] >> (slot * VEC & 31)) & ((1u << VEC) - 1);
 }
 
+// The student's mass outside the teacher's places, against which the rest of the teacher's probability is held.  SO has it relative to
+// the row's largest logit; where less than OUTSIDE_FAR is left of that, its terms leave fp32 one after the other (up to 2^20 of them below
+// 2^-126) while its logarithm is an ordinary number, so it is summed again relative to the largest logit outside.
+static constexpr float OUTSIDE_FAR = 0x1p-64f;
+static constexpr int OUTSIDE_WORDS = 512;      // marks of 16384 places, for the kernels that have no marks of the whole row
+struct Outside {
+    bool apart = false;        // summed again: sum of exp((z - top)/T) over the places outside (0: all of them masked)
+    float top = 0.f, sum = 0.f;
+};
+__device__ __forceinline__ bool outside_far(const float4 &s, double rest) { return rest > 0.0 && s.w < OUTSIDE_FAR && s.y > 0.f; }
+
+// Two passes over the row, which is in the caches; every thread of the block calls it.  bits: marks of the teacher's places, `words` of
+// them at a time.  Rare (students that put next to nothing outside, vocabularies masked with finite numbers): loss and gradient of 2048 rows
+// of 131072 bf16, all of them such, 446 us against 239; of 16 rows of 262144 fp32, which a block each walks alone, 400 against 25.
+template <int DT, int BLOCK>
+__device__ __forceinline__ Outside outside_of(const Row<DT> &row, int place, const Scales &q, unsigned *bits, int words, float *fpart)
+{
+    constexpr int VEC = Row<DT>::VEC, DEEP = 4;
+    const int tid = threadIdx.x, chunk = words * 32 / VEC;
+    Outside o;
+    o.apart = true;
+    o.top = -INFINITY;
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+        float run = pass == 0 ? -INFINITY : 0.f;
+#pragma unroll 1
+        for (int s0 = 0; s0 < row.slots; s0 += chunk) {
+            const int s1 = min(s0 + chunk, row.slots);
+            __syncthreads();                            // everyone is done with the marks before these
+            mark_places(bits, words, s0 * VEC, place, row.shift, BLOCK);
+#pragma unroll 1
+            for (int s = s0 + tid; s < s1; s += DEEP * BLOCK) {
+                uint4 v[DEEP];
+#pragma unroll
+                for (int i = 0; i < DEEP; ++i) v[i] = s + i * BLOCK < s1 ? row.load(s + i * BLOCK) : Row<DT>::empty();
+#pragma unroll
+                for (int i = 0; i < DEEP; ++i) {
+                    const unsigned skip = s + i * BLOCK < s1 ? marks_of<VEC>(bits, s + i * BLOCK - s0) : 0u;
+                    float x[VEC];
+                    Row<DT>::Type::unpack(v[i], x);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        const float here = skip >> j & 1 ? -INFINITY : x[j];
+                        run = pass == 0 ? fmaxf(run, here) : run + exp2_fast((here - o.top) * q.c);
+                    }
+                }
+            }
+        }
+        if (pass == 0) o.top = block_max<BLOCK>(run, fpart);
+        else o.sum = block_sum<BLOCK>(run, fpart);
+        if (o.top == -INFINITY) break;                  // uniform
+    }
+    return o;
+}
+
 // The row's loss from its sums (M, ST, S1, SO); every thread of the block calls it.
 template <int BLOCK>
 __device__ __forceinline__ void write_loss(const DistillArgs &a, size_t r, int place, float z_place, float z_label, bool padding,
-                                           const float4 &s, TeacherLds &lds)
+                                           const float4 &s, const Outside &out, TeacherLds &lds)
 {
     const double T = (double)a.temperature;
     const bool none = padding || s.y == 0.f;           // padding, or every logit masked
@@ -145,7 +200,10 @@ __device__ __forceinline__ void write_loss(const DistillArgs &a, size_t r, int p
     if (isnan(p)) term = p;
     double kl = block_sum<BLOCK>(term, lds.part);
     if (threadIdx.x != 0) return;
-    if (lds.rest > 0.0 && s.w > 0.f) kl += lds.rest * (log(lds.rest) - log((double)s.w) + log_st);
+    if (lds.rest > 0.0) {
+        if (!out.apart && s.w > 0.f) kl += lds.rest * (log(lds.rest) - log((double)s.w) + log_st);
+        if (out.apart && out.sum > 0.f) kl += lds.rest * (log(lds.rest) - (((double)out.top - (double)s.x) / T + log((double)out.sum)) + log_st);
+    }
     double loss = 0.0;
     if (!none) {
         if (a.hard < 1.f) loss = (1.0 - (double)a.hard) * T * T * kl;
@@ -157,39 +215,44 @@ __device__ __forceinline__ void write_loss(const DistillArgs &a, size_t r, int p
 }
 
 // ---- the gradient ----------------------------------------------------------------------------------------------------
-// The factors of a row's gradient: outside the places that the teacher or the label names it is fq e_j + f1 h_j.
+// The factors of a row's gradient: outside the places that the teacher or the label names it is fq e_j + f1 h_j, less
+// far exp((z_j - top)/T) where the mass outside has a sum of its own.
 struct Factors {
-    double soft, up_hard, cover, outside;
-    __device__ __forceinline__ Factors(const DistillArgs &a, size_t r, const TeacherLds &teacher, const float4 &s)
+    double soft, up_hard, cover, outside, far;
+    __device__ __forceinline__ Factors(const DistillArgs &a, size_t r, const TeacherLds &teacher, const float4 &s, const Outside &out)
     {
         const double up = (double)a.scale * (a.dloss ? (double)a.dloss[r] : 1.0);
-        const double rest = s.w > 0.f ? teacher.rest : 0.0;
+        const double rest = (out.apart ? out.sum : s.w) > 0.f ? teacher.rest : 0.0;
         soft = up * (1.0 - (double)a.hard) * (double)a.temperature;
         up_hard = up * (double)a.hard;
         cover = teacher.mass + rest;
-        outside = rest > 0.0 ? cover - rest * (double)s.y / (double)s.w : cover;
+        outside = rest > 0.0 && !out.apart ? cover - rest * (double)s.y / (double)s.w : cover;
+        far = rest > 0.0 && out.apart ? soft * rest / (double)out.sum : 0.0;
     }
 };
 template <int VEC> struct Slope {
-    float fq, f1;
+    float fq, f1, far, top;
     Reference<VEC> at;
     bool none;                 // nothing to learn: the gradient is 0
-    bool apart;                // a row of large logits: its elements go through of_apart()
-    __device__ __forceinline__ Slope(const DistillArgs &a, size_t r, const TeacherLds &teacher, bool padding, const float4 &s, const Scales &q)
+    bool apart;                // a row of large logits, or a mass outside with a sum of its own: its elements go through of_apart()
+    __device__ __forceinline__ Slope(const DistillArgs &a, size_t r, const TeacherLds &teacher, bool padding, const float4 &s, const Outside &out, const Scales &q)
         : at(uniform(s.x), q)
     {
         none = padding || uniform(s.y) == 0.f;
-        const Factors f(a, r, teacher, s);
-        fq = uniform((float)(f.soft * f.outside / (double)s.y) * exp2_fast(-at.lost));
-        f1 = a.hard > 0.f ? uniform((float)(f.up_hard / (double)s.z) * exp2_fast(-at.lost1)) : 0.f;
-        apart = at.by_difference();
+        apart = at.by_difference() || out.apart;
+        const Factors f(a, r, teacher, s, out);
+        fq = uniform((float)(f.soft * f.outside / (double)s.y) * exp2_fast(apart ? 0.f : -at.lost));
+        f1 = a.hard > 0.f ? uniform((float)(f.up_hard / (double)s.z) * exp2_fast(apart ? 0.f : -at.lost1)) : 0.f;
+        far = uniform((float)f.far);
+        top = uniform(out.top);
     }
     __device__ __forceinline__ void of_apart(float (&x)[VEC], const Scales &q) const
     {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
             const float d = x[i] - at.ref;
-            x[i] = fmaf(f1, exp2_fast(d * q.c1), fq * exp2_fast(d * q.c));
+            const float beyond = far != 0.f ? far * exp2_fast((x[i] - top) * q.c) : 0.f;       // the teacher's own places are stored anew
+            x[i] = fmaf(f1, exp2_fast(d * q.c1), fq * exp2_fast(d * q.c)) - beyond;
         }
     }
     template <int HARD> __device__ __forceinline__ void of(float (&x)[VEC]) const
@@ -270,7 +333,7 @@ __device__ __forceinline__ void put_apart(const Row<DT> &row, const GradRow<DT> 
 // first slot that names it, after a barrier behind the stores of all others.
 template <int DT>
 __device__ __forceinline__ void name_places(const DistillArgs &a, size_t r, const GradRow<DT> &out, int place, float z_place, int label,
-                                            float z_label, const float4 &s, const TeacherLds &lds, int j0, int j1)
+                                            float z_label, const float4 &s, const Outside &outside, const TeacherLds &lds, int j0, int j1)
 {
     const bool labelled = a.hard > 0.f;
     int at = -1;
@@ -284,10 +347,11 @@ __device__ __forceinline__ void name_places(const DistillArgs &a, size_t r, cons
             if (first < (int)threadIdx.x) at = -1;
         }
     }
-    const Factors f(a, r, lds, s);
+    const Factors f(a, r, lds, s, outside);
     auto name = [&](int j, float z, bool top, double goal) {
         const double x = (double)z - (double)s.x;
         double d = f.soft * ((top ? f.cover : f.outside) * exp(x / (double)a.temperature) / (double)s.y - goal);
+        if (!top && f.far != 0.0) d -= f.far * exp(((double)z - (double)outside.top) / (double)a.temperature);
         if (f.up_hard != 0.0) d += f.up_hard * (exp(x) / (double)s.z - (labelled && j == label ? 1.0 : 0.0));
         out.put(j, (float)d);
     };
@@ -370,9 +434,12 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
         }
         sums = acc.template combine<BLOCK>(part);
     }
+    Outside outside;
+    if constexpr (TAIL)
+        if (!padding && outside_far(sums, lds.rest)) outside = outside_of<DT, BLOCK>(row, place, q, in_top, (row.slots * VEC + 31) / 32, lds.fpart);
     if constexpr (GRAD) {
         const GradRow<DT> out(a, r, row);
-        const Slope<VEC> g(a, r, lds, padding, sums, q);
+        const Slope<VEC> g(a, r, lds, padding, sums, outside, q);
         auto put = [&](const uint4 &raw, int s, bool full) {
             float x[VEC];
             Type::unpack(raw, x);
@@ -398,10 +465,10 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
             for (int i = 0; i < NV; ++i)
                 if (f0 + tid + i * BLOCK < f1) put(v[i], f0 + tid + i * BLOCK, true);
         }
-        write_loss<BLOCK>(a, r, place, z_place, z_label, padding, sums, lds);       // its barriers stand between the stores above and below
-        if (!g.none) name_places<DT>(a, r, out, place, z_place, label, z_label, sums, lds, 0, a.V);
+        write_loss<BLOCK>(a, r, place, z_place, z_label, padding, sums, outside, lds);       // its barriers stand between the stores above and below
+        if (!g.none) name_places<DT>(a, r, out, place, z_place, label, z_label, sums, outside, lds, 0, a.V);
     } else {
-        write_loss<BLOCK>(a, r, place, z_place, z_label, padding, sums, lds);
+        write_loss<BLOCK>(a, r, place, z_place, z_label, padding, sums, outside, lds);
     }
 }
 
@@ -482,7 +549,12 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a)
         sums.z = block_sum<256>(sums.z, lds.fpart);
         sums.w = block_sum<256>(sums.w, lds.fpart);
     }
-    write_loss<256>(a, r, place, z_place, z_label, padding, sums, lds);
+    Outside outside;
+    if constexpr (TAIL) {
+        __shared__ unsigned bits[OUTSIDE_WORDS];
+        if (!padding && outside_far(sums, lds.rest)) outside = outside_of<DT, 256>(row, place, q, bits, OUTSIDE_WORDS, lds.fpart);
+    }
+    write_loss<256>(a, r, place, z_place, z_label, padding, sums, outside, lds);
 }
 
 // ---- backward: gradients of parts of rows ----------------------------------------------------------------------------
@@ -506,7 +578,12 @@ __global__ __launch_bounds__(BLOCK) void distill_grad_kernel(DistillArgs a)
     slot.load(a, r);
     const int place = read_teacher<BLOCK, TAIL>(a, r, slot, lds);
     const float4 sums = reinterpret_cast<const float4 *>(a.state)[r];
-    const Slope<VEC> g(a, r, lds, padding, sums, q);
+    Outside outside;
+    if constexpr (TAIL) {
+        __shared__ unsigned bits[OUTSIDE_WORDS];
+        if (!padding && outside_far(sums, lds.rest)) outside = outside_of<DT, BLOCK>(row, place, q, bits, OUTSIDE_WORDS, lds.fpart);
+    }
+    const Slope<VEC> g(a, r, lds, padding, sums, outside, q);
     const GradRow<DT> out(a, r, row);
     auto put = [&](const uint4 &raw, int s) {
         float x[VEC];
@@ -533,7 +610,7 @@ __global__ __launch_bounds__(BLOCK) void distill_grad_kernel(DistillArgs a)
     }
     for (; s < s1; s += BLOCK) put(row.load(s), s);
     __syncthreads();
-    name_places<DT>(a, r, out, place, z_place, label, z_label, sums, lds, s0 * VEC - row.shift, s1 * VEC - row.shift);
+    name_places<DT>(a, r, out, place, z_place, label, z_label, sums, outside, lds, s0 * VEC - row.shift, s1 * VEC - row.shift);
 }
 
 // ---- short rows: a wavefront each, all three calls --------------------------------------------------------------------
@@ -543,7 +620,7 @@ __global__ __launch_bounds__(BLOCK) void distill_grad_kernel(DistillArgs a)
 // Measured: 2048 x 100 fp32 7.4 us, of which a launch that does nothing is some 2.  Beyond 1024 logits a block a row is faster
 // (16384 x 2040 bf16: 136 us, 202 with 32 registers a lane here).
 template <int DT, int NQ, bool TAIL, int MODE>
-__global__ __launch_bounds__(256) void distill_short_kernel(DistillArgs a)
+__global__ __launch_bounds__(256, 4) void distill_short_kernel(DistillArgs a)
 {
     using Type = LogitType<DT>;
     constexpr int SLOTS = LOGITS_MAX_TOP / 64;
@@ -573,16 +650,14 @@ __global__ __launch_bounds__(256) void distill_short_kernel(DistillArgs a)
         value[j] = i < a.k ? a.values[r * a.k + i] : 0.f;
     }
     const float lse_given = TAIL ? a.teacher_lse[r] : 0.f;
+    auto logit_at = [&](int j) {
+        float z = row.load_one(j);
+        if constexpr (DT == EASGD_F32)                  // logits that come as partial sums: added in ascending order
+            for (int s = 1; s < a.parts; ++s) z += row.base[row.shift + j + s * a.part_stride];
+        return z;
+    };
 #pragma unroll
-    for (int c = 0; c < NQ; ++c) {
-        const int j = lane + 64 * c;
-        x[c] = -INFINITY;
-        if (j < a.V && !padding) {
-            x[c] = row.load_one(j);
-            if constexpr (DT == EASGD_F32)              // logits that come as partial sums: added in ascending order
-                for (int s = 1; s < a.parts; ++s) x[c] += row.base[row.shift + j + s * a.part_stride];
-        }
-    }
+    for (int c = 0; c < NQ; ++c) x[c] = lane + 64 * c < a.V && !padding ? logit_at(lane + 64 * c) : -INFINITY;
     float z_label = 0.f;
 #pragma unroll
     for (int c = 0; c < NQ; ++c) z_label = lane + 64 * c == label ? x[c] : z_label;
@@ -685,7 +760,23 @@ __global__ __launch_bounds__(256) void distill_short_kernel(DistillArgs a)
         s.w = TAIL ? wave_sum(so) : 0.f;
     }
     const bool none = padding || s.y == 0.f;
-    if (!(s.w > 0.f)) rest = 0.0;
+    Outside outside;
+    if constexpr (TAIL) {
+        if (__any(!padding && outside_far(s, rest))) {  // uniform; the row is read again: registers would cost every row
+            float top = -INFINITY, sum = 0.f;
+#pragma unroll 1
+            for (int j = lane; j < a.V; j += 64) top = fmaxf(top, target[j] >= 0.f ? -INFINITY : logit_at(j));
+            top = wave_max(top);
+            if (top > -INFINITY) {
+#pragma unroll 1
+                for (int j = lane; j < a.V; j += 64) sum += target[j] >= 0.f ? 0.f : exp2_fast((logit_at(j) - top) * q.c);
+            }
+            outside.apart = true;
+            outside.top = top;
+            outside.sum = wave_sum(sum);
+        }
+    }
+    if (!((outside.apart ? outside.sum : s.w) > 0.f)) rest = 0.0;
 
     if constexpr (MODE & DISTILL_LOSS) {
         const double log_st = log((double)s.y);
@@ -694,17 +785,16 @@ __global__ __launch_bounds__(256) void distill_short_kernel(DistillArgs a)
         for (int j = 0; j < SLOTS; ++j) {
             if (64 * j >= a.k) break;
             z_place[j] = 0.f;
-            if (!none && place[j] >= 0) {
-                z_place[j] = row.load_one(place[j]);
-                if constexpr (DT == EASGD_F32)
-                    for (int u = 1; u < a.parts; ++u) z_place[j] += row.base[row.shift + place[j] + u * a.part_stride];
-            }
+            if (!none && place[j] >= 0) z_place[j] = logit_at(place[j]);
             if (!none && p[j] > 0.0) kl += p[j] * (logit[j] - lse - (((double)z_place[j] - (double)s.x) / T - log_st));
             if (isnan(p[j])) kl += p[j];
         }
         kl = wave_sum(kl);
         if (lane == 0) {
-            if (rest > 0.0) kl += rest * (log(rest) - log((double)s.w) + log_st);
+            if (rest > 0.0) {
+                const double log_so = outside.apart ? ((double)outside.top - (double)s.x) / T + log((double)outside.sum) : log((double)s.w);
+                kl += rest * (log(rest) - log_so + log_st);
+            }
             double loss = 0.0;
             if (!none) {
                 if (a.hard < 1.f) loss = (1.0 - (double)a.hard) * T * T * kl;
@@ -717,19 +807,30 @@ __global__ __launch_bounds__(256) void distill_short_kernel(DistillArgs a)
     }
     if constexpr (MODE & DISTILL_GRAD) {
         const double up = (double)a.scale * (a.dloss ? (double)a.dloss[r] : 1.0), soft = up * (1.0 - (double)a.hard) * T;
-        const double cover = mass + rest, outside = rest > 0.0 ? cover - rest * (double)s.y / (double)s.w : cover;
-        const float f_in = (float)(soft * cover / (double)s.y), f_out = (float)(soft * outside / (double)s.y), f_t = (float)soft;
+        const double cover = mass + rest, all_out = rest > 0.0 && !outside.apart ? cover - rest * (double)s.y / (double)s.w : cover;
+        const float f_in = (float)(soft * cover / (double)s.y), f_out = (float)(soft * all_out / (double)s.y), f_t = (float)soft;
+        const float far = rest > 0.0 && outside.apart ? (float)(soft * rest / (double)outside.sum) : 0.f;
         const float f1 = hard ? (float)(up * (double)a.hard / (double)s.z) : 0.f, f_y = (float)(up * (double)a.hard);
         const Row<DT> out(a.dlogits, r, a.dld, a.V);
-#pragma unroll
-        for (int c = 0; c < NQ; ++c) {
-            const int j = lane + 64 * c;
-            const bool in = t[c] >= 0.f;
-            float d = fmaf(f1, h[c], (in ? f_in : f_out) * e[c]);
-            if (in) d = fmaf(-f_t, t[c], d);
+        auto put = [&](int j, float target_j, float e_j, float h_j, float beyond) {
+            const bool in = target_j >= 0.f;
+            float d = fmaf(f1, h_j, (in ? f_in : f_out) * e_j);
+            if (in) d = fmaf(-f_t, target_j, d);
+            else d -= beyond;
             if (hard && j == label) d -= f_y;
-            if (j < a.V) out.base[out.shift + j] = Type::narrow(none ? 0.f : d);
+            out.base[out.shift + j] = Type::narrow(none ? 0.f : d);
+        };
+        if (TAIL && __any(far != 0.f)) {                // uniform, and rare: the row is read again
+#pragma unroll 1
+            for (int j = lane; j < a.V; j += 64) {
+                const float z = logit_at(j), e_j = exp2_fast((z - m) * q.c);
+                put(j, target[j], e_j, a.temperature == 1.f ? e_j : exp2_fast((z - m) * q.c1), far * exp2_fast((z - outside.top) * q.c));
+            }
+            return;
         }
+#pragma unroll
+        for (int c = 0; c < NQ; ++c)
+            if (lane + 64 * c < a.V) put(lane + 64 * c, t[c], e[c], h[c], 0.f);
     }
 }
 

@@ -15,3 +15,25 @@ def test_differences_of_large_logits():
     loss, grad = oracle.distill(z, [0], [0.0], temperature=T)
     assert loss == pytest.approx(-T * T * np.log(w[0] / w.sum()), abs=1e-13)
     assert np.allclose(grad, T * (w / w.sum() - [1, 0, 0]), rtol=0, atol=1e-14)
+
+
+@pytest.mark.parametrize("gap", [10.0, 100.0, 600.0, 1e4, 1e9])
+def test_rest_of_the_teacher_against_a_confident_student(gap):
+    """One place at the gap, 999 others at 0, p = 0.9: 0.9 log(0.9 / q) + 0.1 log(0.1 / R), where R (1e-4342 at a gap of 1e4) is no 64-bit number."""
+    z = np.zeros(1000)
+    z[5] = gap
+    log_all = gap + np.log1p(999 * np.exp(-gap))
+    loss, grad = oracle.distill(z, [5], [np.log(0.9)], 0.0)
+    assert loss == pytest.approx(0.9 * (np.log(0.9) - gap + log_all) + 0.1 * (np.log(0.1) - np.log(999) + log_all), rel=1e-12)
+    q = np.exp(gap - log_all)
+    want = np.full(1000, (1 - q) / 999 - 0.1 / 999)
+    want[5] = q - 0.9
+    assert np.allclose(grad, want, rtol=0, atol=1e-14)
+
+
+def test_a_rest_without_a_place_counts_for_nothing():
+    z = np.array([1.0, -np.inf, 2.0, -np.inf])
+    loss, grad = oracle.distill(z, [0, 2], np.log([0.3, 0.4]), 0.0)
+    lq = z[[0, 2]] - np.logaddexp(1.0, 2.0)
+    assert loss == pytest.approx(0.3 * (np.log(0.3) - lq[0]) + 0.4 * (np.log(0.4) - lq[1]), abs=1e-15)
+    assert np.allclose(grad, [0.7 * np.exp(lq[0]) - 0.3, 0, 0.7 * np.exp(lq[1]) - 0.4, 0], rtol=0, atol=1e-15)
