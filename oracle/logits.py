@@ -82,7 +82,7 @@ def distill(z, indices, values, teacher_lse=None, label=None, temperature=1.0, h
     c = p.sum() + r
     soft = c * q - target
     if r > 0.0:
-        soft[outside] -= r * np.exp(log_q[outside] - log_R)
+        soft[outside] -= r * np.exp(log_softmax(z[outside], T))      # every place's share of R
     loss, grad = 0.0, np.zeros(V)
     if hard < 1.0:
         loss += (1.0 - hard) * T * T * kl
