@@ -410,7 +410,8 @@ int easgd_top_logits(const void *logits, int dtype, size_t rows, int V, size_t l
  *   indices      DEVICE in [rows][k] int32   t_i; an index outside [0, V) marks a slot that is not used (its value is ignored).  An
  *                                            index that comes up twice counts with both probabilities.
  *   values       DEVICE in [rows][k] fp32    a_i (-inf: probability 0), as easgd_top_logits writes them
- *   teacher_lse  DEVICE in [rows] fp32, or NULL   at the same temperature, as easgd_top_logits writes it
+ *   teacher_lse  DEVICE in [rows] fp32, or NULL   at the same temperature, as easgd_top_logits writes it (-inf: the teacher's row is
+ *                                            masked, every p_i is 0)
  *   labels       DEVICE in [rows] int32, or NULL (then hard == 0).  A row whose label is outside [0, V) is padding: its
  *                                            logits are not read, its loss and gradient are 0.
  *   loss         DEVICE out [rows] fp32

@@ -45,10 +45,12 @@ def _teacher(V, indices, values, teacher_lse, T):
     indices = np.asarray(indices)
     used = (indices >= 0) & (indices < V)
     a = np.where(used, np.where(used, values, 0.0).astype(np.float64) / T, -np.inf)
-    norm = teacher_lse if teacher_lse is not None else logsumexp(a) if used.any() else 0.0
-    if norm == -np.inf:
-        norm = 0.0                       # every used slot is masked: no probability anywhere
-    log_p = a - norm
+    live = a != -np.inf                  # the others have probability 0, whatever the log-sum-exp is
+    if teacher_lse == -np.inf:
+        live[:] = False                  # the teacher's row is masked
+    log_p = np.full(len(a), -np.inf)
+    if live.any():
+        log_p[live] = a[live] - teacher_lse if teacher_lse is not None else a[live] - logsumexp(a[live])
     p = np.where(used, np.exp(log_p), 0.0)
     target = np.zeros(V)
     np.add.at(target, indices[used], p[used])

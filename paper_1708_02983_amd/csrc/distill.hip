@@ -65,17 +65,20 @@ __device__ __forceinline__ int read_teacher(const DistillArgs &a, size_t r, cons
     const int tid = threadIdx.x;
     const double T = (double)a.temperature;
     const int place = (unsigned)slot.place < (unsigned)a.V ? slot.place : -1;
-    const double logit = place >= 0 ? (double)slot.value / T : -(double)INFINITY;
     if (tid < LOGITS_MAX_TOP) lds.index[tid] = place;
-    double lse;
-    if constexpr (TAIL) lse = (double)a.teacher_lse[r];
-    else {
-        const float top = block_max<BLOCK>((float)logit, lds.fpart);
-        const double total = block_sum<BLOCK>(place >= 0 && top > -INFINITY ? exp(logit - (double)top) : 0.0, lds.part);
-        lse = (double)top + log(total);
-        if (!(top > -INFINITY)) lse = isnan(total) ? (double)NAN : 0.0;      // no used slot, or all masked: no probability anywhere
+    // A masked value has probability 0 whatever the others are; so have all of a row that the teacher masks.
+    double log_p = -(double)INFINITY;
+    if constexpr (TAIL) {
+        const float lse = a.teacher_lse[r];
+        if (place >= 0 && slot.value != -INFINITY && lse != -INFINITY) log_p = (double)slot.value / T - (double)lse;
+    } else {
+        const bool live = place >= 0 && slot.value != -INFINITY;
+        const double logit = (double)slot.value / T;
+        const float top = block_max<BLOCK>(live ? (float)logit : -INFINITY, lds.fpart);
+        const double total = block_sum<BLOCK>(live ? exp(logit - (double)top) : 0.0, lds.part);
+        if (live) log_p = logit - ((double)top + log(total));
     }
-    const double log_p = logit - lse, p = place >= 0 ? exp(log_p) : 0.0;
+    const double p = place >= 0 ? exp(log_p) : 0.0;
     if (tid < a.k) {
         lds.log_p[tid] = log_p;
         lds.p[tid] = p;
@@ -664,30 +667,41 @@ __global__ __launch_bounds__(256, 4) void distill_short_kernel(DistillArgs a)
     z_label = wave_only(z_label);
 
     // the teacher
-    double logit[SLOTS], p[SLOTS], lse = (double)lse_given, mass = 0.0;
+    double log_p[SLOTS], p[SLOTS], mass = 0.0;
     float top = -INFINITY;
+    bool live[SLOTS];
 #pragma unroll
     for (int j = 0; j < SLOTS; ++j) {
         if ((unsigned)place[j] >= (unsigned)a.V) place[j] = -1;
-        logit[j] = place[j] >= 0 ? (double)value[j] / T : -(double)INFINITY;
-        top = fmaxf(top, (float)logit[j]);
+        live[j] = place[j] >= 0 && value[j] != -INFINITY && !(TAIL && lse_given == -INFINITY);       // as in read_teacher
+        log_p[j] = -(double)INFINITY;
+        if (live[j]) top = fmaxf(top, (float)((double)value[j] / T));
     }
-    if constexpr (!TAIL) {
+    if constexpr (TAIL) {
+#pragma unroll
+        for (int j = 0; j < SLOTS; ++j)
+            if (live[j]) log_p[j] = (double)value[j] / T - (double)lse_given;
+    } else {
         top = wave_max(top);
         double total = 0.0;
 #pragma unroll
+        for (int j = 0; j < SLOTS; ++j) {
+            if (live[j]) {
+                log_p[j] = (double)value[j] / T;
+                total += exp(log_p[j] - (double)top);
+            }
+        }
+        const double lse = (double)top + log(wave_sum(total));
+#pragma unroll
         for (int j = 0; j < SLOTS; ++j)
-            if (64 * j < a.k && place[j] >= 0 && top > -INFINITY) total += exp(logit[j] - (double)top);
-        total = wave_sum(total);
-        lse = (double)top + log(total);
-        if (!(top > -INFINITY)) lse = isnan(total) ? (double)NAN : 0.0;
+            if (live[j]) log_p[j] -= lse;
     }
 #pragma unroll
     for (int j = 0; j < SLOTS; ++j) {
         const int i = lane + 64 * j;
         p[j] = 0.0;
         if (64 * j < a.k) {
-            p[j] = place[j] >= 0 ? exp(logit[j] - lse) : 0.0;
+            p[j] = place[j] >= 0 ? exp(log_p[j]) : 0.0;
             index[i] = place[j];
             probability[i] = p[j];
         }
@@ -786,7 +800,7 @@ __global__ __launch_bounds__(256, 4) void distill_short_kernel(DistillArgs a)
             if (64 * j >= a.k) break;
             z_place[j] = 0.f;
             if (!none && place[j] >= 0) z_place[j] = logit_at(place[j]);
-            if (!none && p[j] > 0.0) kl += p[j] * (logit[j] - lse - (((double)z_place[j] - (double)s.x) / T - log_st));
+            if (!none && p[j] > 0.0) kl += p[j] * (log_p[j] - (((double)z_place[j] - (double)s.x) / T - log_st));
             if (isnan(p[j])) kl += p[j];
         }
         kl = wave_sum(kl);

@@ -37,3 +37,14 @@ def test_a_rest_without_a_place_counts_for_nothing():
     lq = z[[0, 2]] - np.logaddexp(1.0, 2.0)
     assert loss == pytest.approx(0.3 * (np.log(0.3) - lq[0]) + 0.4 * (np.log(0.4) - lq[1]), abs=1e-15)
     assert np.allclose(grad, [0.7 * np.exp(lq[0]) - 0.3, 0, 0.7 * np.exp(lq[1]) - 0.4, 0], rtol=0, atol=1e-15)
+
+
+def test_a_teacher_without_probability():
+    """Masked values count for nothing, also against a log-sum-exp of -inf: the rest is 1, and the loss is -log R."""
+    z = np.log([0.5, 0.25, 0.125, 0.125])
+    with np.errstate(invalid="ignore"):
+        for lse in (-np.inf, 0.3):
+            loss, grad = oracle.distill(z, [0, 1], [-np.inf, -np.inf], lse)
+            assert loss == pytest.approx(np.log(4)) and np.allclose(grad, [0.5, 0.25, 0.125 - 0.5, 0.125 - 0.5])
+        loss, grad = oracle.distill(z, [0, 1], [-np.inf, -np.inf])
+        assert loss == 0.0 and not grad.any()
