@@ -50,7 +50,7 @@ def _teacher(V, indices, values, teacher_lse, T):
         live[:] = False                  # the teacher's row is masked
     log_p = np.full(len(a), -np.inf)
     if live.any():
-        log_p[live] = a[live] - teacher_lse if teacher_lse is not None else a[live] - logsumexp(a[live])
+        log_p[live] = a[live] - teacher_lse if teacher_lse is not None else log_softmax(a[live])
     p = np.where(used, np.exp(log_p), 0.0)
     target = np.zeros(V)
     np.add.at(target, indices[used], p[used])

@@ -66,17 +66,18 @@ __device__ __forceinline__ int read_teacher(const DistillArgs &a, size_t r, cons
     const double T = (double)a.temperature;
     const int place = (unsigned)slot.place < (unsigned)a.V ? slot.place : -1;
     if (tid < LOGITS_MAX_TOP) lds.index[tid] = place;
-    // A masked value has probability 0 whatever the others are; so have all of a row that the teacher masks.
+    // A masked value has probability 0 whatever the others are; so have all of a row that the teacher masks.  Logits are taken relative to the
+    // largest before they are divided and before the logarithm of their sum comes to them: near fp32's ends it would be lost.
     double log_p = -(double)INFINITY;
     if constexpr (TAIL) {
         const float lse = a.teacher_lse[r];
         if (place >= 0 && slot.value != -INFINITY && lse != -INFINITY) log_p = (double)slot.value / T - (double)lse;
     } else {
         const bool live = place >= 0 && slot.value != -INFINITY;
-        const double logit = (double)slot.value / T;
-        const float top = block_max<BLOCK>(live ? (float)logit : -INFINITY, lds.fpart);
-        const double total = block_sum<BLOCK>(live ? exp(logit - (double)top) : 0.0, lds.part);
-        if (live) log_p = logit - ((double)top + log(total));
+        const float top = block_max<BLOCK>(live ? slot.value : -INFINITY, lds.fpart);
+        if (live) log_p = ((double)slot.value - (double)top) / T;
+        const double total = block_sum<BLOCK>(live ? exp(log_p) : 0.0, lds.part);
+        if (live) log_p -= log(total);
     }
     const double p = place >= 0 ? exp(log_p) : 0.0;
     if (tid < a.k) {
@@ -675,7 +676,7 @@ __global__ __launch_bounds__(256, 4) void distill_short_kernel(DistillArgs a)
         if ((unsigned)place[j] >= (unsigned)a.V) place[j] = -1;
         live[j] = place[j] >= 0 && value[j] != -INFINITY && !(TAIL && lse_given == -INFINITY);       // as in read_teacher
         log_p[j] = -(double)INFINITY;
-        if (live[j]) top = fmaxf(top, (float)((double)value[j] / T));
+        if (live[j]) top = fmaxf(top, value[j]);
     }
     if constexpr (TAIL) {
 #pragma unroll
@@ -687,14 +688,14 @@ __global__ __launch_bounds__(256, 4) void distill_short_kernel(DistillArgs a)
 #pragma unroll
         for (int j = 0; j < SLOTS; ++j) {
             if (live[j]) {
-                log_p[j] = (double)value[j] / T;
-                total += exp(log_p[j] - (double)top);
+                log_p[j] = ((double)value[j] - (double)top) / T;
+                total += exp(log_p[j]);
             }
         }
-        const double lse = (double)top + log(wave_sum(total));
+        const double log_total = log(wave_sum(total));
 #pragma unroll
         for (int j = 0; j < SLOTS; ++j)
-            if (live[j]) log_p[j] -= lse;
+            if (live[j]) log_p[j] -= log_total;
     }
 #pragma unroll
     for (int j = 0; j < SLOTS; ++j) {

@@ -1,4 +1,4 @@
-"""A teacher's numbers at their ends: rows that the teacher masks as a whole."""
+"""A teacher's numbers at their ends: rows that the teacher masks as a whole, logits near the ends of fp32 at small temperatures."""
 import numpy as np
 import pytest
 import torch
@@ -60,3 +60,22 @@ def test_the_log_sum_exp_of_a_masked_row_goes_on():
     for idx in (indices, indices.clamp(min=0)):
         loss, grad = hip.easgd_distill(z, idx, values, teacher_lse=lse)
         assert torch.isfinite(loss).all() and torch.isfinite(grad).all()
+
+
+@pytest.mark.parametrize("V", LENGTHS)
+@pytest.mark.parametrize("T", [0.5, 1e-3, 1e-6, 1.0])
+def test_logits_at_the_ends_of_fp32(V, T):
+    """Their quotients by a small temperature leave fp32; their differences count."""
+    rng = np.random.default_rng(V + 1)
+    rows, k = 6, 40
+    z = (rng.normal(0, 2.0, (rows, V)) * T).astype(F)
+    idx = np.stack([rng.permutation(V)[:k] for _ in range(rows)]).astype(np.int32)
+    low = np.finfo(F).min
+    val = np.full((rows, k), low, F)
+    val[1] = -low
+    val[2, 1:] = -low * F(0.5)
+    val[3, 7] = 1.0
+    val[4, :] = rng.normal(0, 1, k) * T
+    val[4, 3] = low
+    val[5, 10:] = -np.inf
+    check(z, idx, val, None, T)

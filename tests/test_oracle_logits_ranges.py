@@ -48,3 +48,8 @@ def test_a_teacher_without_probability():
             assert loss == pytest.approx(np.log(4)) and np.allclose(grad, [0.5, 0.25, 0.125 - 0.5, 0.125 - 0.5])
         loss, grad = oracle.distill(z, [0, 1], [-np.inf, -np.inf])
         assert loss == 0.0 and not grad.any()
+        # values that differ by nothing at the end of fp32, and one that is all
+        low = float(np.finfo(np.float32).min)
+        loss, _ = oracle.distill(z, [0, 1], [low, low], temperature=1e-6)
+        even, _ = oracle.distill(z, [0, 1], [0.0, 0.0], temperature=1e-6)
+        assert loss == pytest.approx(even)
