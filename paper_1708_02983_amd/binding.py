@@ -157,6 +157,24 @@ def _dev(name: str, t: torch.Tensor, dtype, min_numel: int) -> int:
     return t.data_ptr()
 
 
+def _stream_object(stream):
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream)
+
+
+def _new(shape, dtype, like, stream):
+    """A tensor for a result or for scratch, from the memory of the stream that works on it first: what the current stream's
+    memory holds free may still be in use by that stream's work, which another stream does not wait for.  The current
+    stream, whose program gets the tensor, is noted as a user: the memory goes back to `stream` after its work, too."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    stream, caller = _stream_object(stream), torch.cuda.current_stream(like.device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=like.device)
+    if stream != caller:
+        t.record_stream(caller)
+    return t
+
+
 def _replica_shape(W: torch.Tensor, N: Optional[int]):
     if W.dim() != 2:
         raise ValueError("replica matrices must be [P][ld]")
@@ -296,7 +314,7 @@ def easgd_grad(dims: Sequence[int], W, X, y, G, loss=None, workspace=None, strea
     need = (P - 1) * ld + N
     nbytes = easgd_grad_workspace_bytes(dims, P, b)
     if workspace is None:
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=W.device)
+        workspace = _new(nbytes, torch.uint8, W, stream)
     g16 = G.dtype == torch.bfloat16
     entry = _lib.easgd_grad_bf16 if g16 else _lib.easgd_grad
     _check(entry(arr, L, _dev("W", W, torch.float32, need), ld,
@@ -370,7 +388,7 @@ def easgd_mlp_round(dims: Sequence[int], W, Wc, X, y, eta: float, rho: float, V=
     need = (P - 1) * ld + N
     nbytes = easgd_mlp_round_workspace_bytes(dims, P, b)
     if workspace is None:
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=W.device)
+        workspace = _new(nbytes, torch.uint8, W, stream)
     v16 = V is not None and V.dtype == torch.bfloat16
     entry = _lib.easgd_mlp_round_bf16v if v16 else _lib.easgd_mlp_round
     _check(entry(arr, L, _dev("W", W, torch.float32, need),
@@ -429,14 +447,6 @@ def _given(name: str, t, dtype, shape: tuple, device: int):
     if t.get_device() != device:
         raise ValueError(f"{name} must be on cuda:{device}, is on {t.device}")
     return t.data_ptr()
-
-
-def _new(shape, dtype, like, stream):
-    """A tensor for a result or for scratch; one that another stream than the current one works on is kept from reuse."""
-    t = torch.empty(shape, dtype=dtype, device=like.device)
-    if stream is not None:
-        t.record_stream(stream)
-    return t
 
 
 def _scratch(nbytes: int, workspace, like, stream):
