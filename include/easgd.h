@@ -421,7 +421,8 @@ int easgd_top_logits(const void *logits, int dtype, size_t rows, int V, size_t l
  *   scale, dloss     the gradient is that of scale * sum over the rows of dloss[row] * loss[row]; dloss DEVICE in [rows] fp32, or
  *                    NULL: all 1.  (Mean losses of b samples: scale = 1/b.)
  *   dlogits      DEVICE out [rows][dld], element type of logits; entries [V, dld) of a row are not written; aligned like
- *                                            logits, but need not share their alignment or stride
+ *                                            logits, but need not share their alignment or stride.  Its rows must not overlap those of
+ *                                            logits (EASGD_EINVAL): not in place.  At one stride rows may alternate
  *   1 <= k <= EASGD_MAX_TOP; temperature in [1e-6, 1e6]; hard in [0, 1]; scale finite.
  * A student's row whose logits are all -inf has loss and gradient 0, as has a row without a used slot as far as KL goes; a
  * teacher's place where the student's logit is -inf gives an infinite loss and a finite gradient; a NaN or +inf among

@@ -889,6 +889,18 @@ static int check_distill(const DistillCall &q, int mode)
     return EASGD_OK;
 }
 
+// Whether a row of logits and one of dlogits share memory: blocks read a row, or parts of others, while they store.  Rows that
+// alternate (the two halves of wider rows, say) share none; at two strides the whole ranges have to be apart.
+static bool rows_overlap(const DistillArgs &a, size_t rows, size_t size)
+{
+    const uintptr_t in = reinterpret_cast<uintptr_t>(a.logits), out = reinterpret_cast<uintptr_t>(a.dlogits);
+    const size_t row = (size_t)a.V * size;
+    if (in + (rows - 1) * a.ld * size + row <= out || out + (rows - 1) * a.dld * size + row <= in) return false;
+    if (rows == 1 || a.ld != a.dld) return true;
+    const size_t pitch = a.ld * size, apart = in < out ? (out - in) % pitch : (in - out) % pitch;
+    return apart < row || pitch - apart < row;
+}
+
 // Into how many parts rows are cut: enough blocks to fill the chip, and at least 1024 slots (four per thread) a part.
 static constexpr int SPLIT_ROWS = 256, SPLIT_BLOCKS = 1024, SPLIT_SLOTS = 1024;
 static int segments_of(size_t rows, int slots)
@@ -990,6 +1002,7 @@ template <int MODE> static int launch_distill(const DistillCall &q, void *stream
         const size_t need = easgd_distill_workspace_bytes(q.rows, a.V, a.k);
         if (int rc = check_workspace(q.name, q.workspace, q.workspace_bytes, need)) return rc;
     }
+    if ((MODE & DISTILL_GRAD) && q.rows && rows_overlap(a, q.rows, dtype_bytes(q.dtype))) return fail(EASGD_EINVAL, "%s: dlogits must not overlap logits", q.name);
     clear_error();
     if (q.rows == 0) return EASGD_OK;
     const hipStream_t s = static_cast<hipStream_t>(stream);
