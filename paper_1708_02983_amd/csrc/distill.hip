@@ -137,14 +137,15 @@ template <int VEC> __device__ __forceinline__ unsigned marks_of(const unsigned *
 
 // The student's mass outside the teacher's places, against which the rest of the teacher's probability is held.  SO has it relative to
 // the row's largest logit; where less than OUTSIDE_FAR is left of that, its terms leave fp32 one after the other (up to 2^20 of them below
-// 2^-126) while its logarithm is an ordinary number, so it is summed again relative to the largest logit outside.
+// 2^-126) while its logarithm is an ordinary number, so it is summed again relative to the largest logit outside.  (0: all of them are masked,
+// nothing to sum.)
 static constexpr float OUTSIDE_FAR = 0x1p-64f;
 static constexpr int OUTSIDE_WORDS = 512;      // marks of 16384 places, for the kernels that have no marks of the whole row
 struct Outside {
-    bool apart = false;        // summed again: sum of exp((z - top)/T) over the places outside (0: all of them masked)
+    bool apart = false;        // summed again: sum of exp((z - top)/T) over the places outside
     float top = 0.f, sum = 0.f;
 };
-__device__ __forceinline__ bool outside_far(const float4 &s, double rest) { return rest > 0.0 && s.w < OUTSIDE_FAR && s.y > 0.f; }
+__device__ __forceinline__ bool outside_far(const float4 &s, double rest) { return rest > 0.0 && s.w > 0.f && s.w < OUTSIDE_FAR && s.y > 0.f; }
 
 // Two passes over the row, which is in the caches; every thread of the block calls it.  bits: marks of the teacher's places, `words` of
 // them at a time.  Rare (students that put next to nothing outside, vocabularies masked with finite numbers): loss and gradient of 2048 rows
@@ -188,6 +189,21 @@ __device__ __forceinline__ Outside outside_of(const Row<DT> &row, int place, con
         if (o.top == -INFINITY) break;                  // uniform
     }
     return o;
+}
+
+// Whether a slot holds anything but -inf outside the teacher's places, which `skip` marks
+template <int DT> __device__ __forceinline__ bool unmasked(const uint4 &raw, unsigned skip)
+{
+    const uint4 masked = Row<DT>::empty();
+    unsigned d[4] = {raw.x ^ masked.x, raw.y ^ masked.y, raw.z ^ masked.z, raw.w ^ masked.w};
+    if (skip) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (Row<DT>::VEC == 4) d[i] = skip >> i & 1 ? 0 : d[i];
+            else d[i] &= (skip >> 2 * i & 1 ? 0 : 0xffffu) | (skip >> (2 * i + 1) & 1 ? 0 : 0xffff0000u);
+        }
+    }
+    return (d[0] | d[1] | d[2] | d[3]) != 0;
 }
 
 // The row's loss from its sums (M, ST, S1, SO); every thread of the block calls it.
@@ -379,6 +395,7 @@ template <int DT, int BLOCK, int NV, bool TAIL, int HARD, bool GRAD>
 __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
 {
     constexpr int VEC = Row<DT>::VEC, DEEP = 4;
+    static_assert(NV % DEEP == 0, "slots are looked at in groups");
     using Type = LogitType<DT>;
     extern __shared__ unsigned in_top[];
     __shared__ TeacherLds lds;
@@ -421,10 +438,22 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
             Type::unpack(raw, x);
             acc.add(x, TAIL ? marks_of<VEC>(in_top, s) : 0u);
         };
-        if (tid < 64) add(edge, max(edge_slot, 0));
+        auto look = [&](const uint4 &raw, int s) { acc.some = acc.some || unmasked<DT>(raw, marks_of<VEC>(in_top, s)); };
+        if (tid < 64) {
+            add(edge, max(edge_slot, 0));
+            acc.until_settled([&] { look(edge, max(edge_slot, 0)); });
+        }
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (first + i * BLOCK < f1) add(v[i], min(f0 + tid + i * BLOCK, f1 - 1));
+        for (int i0 = 0; i0 < NV; i0 += DEEP) {
+#pragma unroll
+            for (int i = i0; i < i0 + DEEP; ++i)
+                if (first + i * BLOCK < f1) add(v[i], min(f0 + tid + i * BLOCK, f1 - 1));
+            acc.until_settled([&] {
+#pragma unroll
+                for (int i = i0; i < i0 + DEEP; ++i)
+                    if (first + i * BLOCK < f1) look(v[i], min(f0 + tid + i * BLOCK, f1 - 1));
+            });
+        }
         for (int i0 = NV; first + i0 * BLOCK < f1; i0 += DEEP) {
             uint4 w[DEEP];
 #pragma unroll
@@ -435,6 +464,11 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
 #pragma unroll
             for (int i = 0; i < DEEP; ++i)
                 if (first + (i0 + i) * BLOCK < f1) add(w[i], min(f0 + tid + (i0 + i) * BLOCK, f1 - 1));
+            acc.until_settled([&] {
+#pragma unroll
+                for (int i = 0; i < DEEP; ++i)
+                    if (first + (i0 + i) * BLOCK < f1) look(w[i], min(f0 + tid + (i0 + i) * BLOCK, f1 - 1));
+            });
         }
         sums = acc.template combine<BLOCK>(part);
     }
@@ -506,6 +540,7 @@ __global__ __launch_bounds__(BLOCK) void distill_sums_kernel(DistillArgs a)
         Type::unpack(raw, x);
         acc.add(x, TAIL ? marks_of<VEC>(in_top, s - s0) : 0u);
     };
+    auto look = [&](const uint4 &raw, int s) { acc.some = acc.some || unmasked<DT>(raw, marks_of<VEC>(in_top, s - s0)); };
     const int lead = __builtin_amdgcn_readfirstlane(tid & ~63);
     int s = s0 + tid;
     for (; s - tid + DEEP * BLOCK <= s1; s += DEEP * BLOCK) {      // uniform
@@ -514,8 +549,16 @@ __global__ __launch_bounds__(BLOCK) void distill_sums_kernel(DistillArgs a)
         for (int i = 0; i < DEEP; ++i) v[i] = row.load(s + i * BLOCK);
 #pragma unroll
         for (int i = 0; i < DEEP; ++i) add(v[i], s + i * BLOCK);
+        acc.until_settled([&] {
+#pragma unroll
+            for (int i = 0; i < DEEP; ++i) look(v[i], s + i * BLOCK);
+        });
     }
-    for (; s - tid + lead < s1; s += BLOCK) add(s < s1 ? row.load(s) : Row<DT>::empty(), min(s, s1 - 1));      // whole wavefronts
+    for (; s - tid + lead < s1; s += BLOCK) {           // whole wavefronts
+        const uint4 v = s < s1 ? row.load(s) : Row<DT>::empty();
+        add(v, min(s, s1 - 1));
+        acc.until_settled([&] { look(v, min(s, s1 - 1)); });
+    }
     const float4 sums = acc.template combine<BLOCK>(part);
     if (tid == 0) a.partial[r * a.segments + seg] = sums;
 }
@@ -760,9 +803,11 @@ __global__ __launch_bounds__(256, 4) void distill_short_kernel(DistillArgs a)
     } else s = reinterpret_cast<const float4 *>(a.state)[r];
     const float m = s.x == -INFINITY ? 0.f : s.x;
     float st = 0.f, s1 = 0.f, so = 0.f;
+    bool some = false;
 #pragma unroll
     for (int c = 0; c < NQ; ++c) {
         t[c] = target[lane + 64 * c];
+        if constexpr (TAIL && (MODE & DISTILL_LOSS)) some = some || (!(t[c] >= 0.f) && x[c] > -INFINITY);
         e[c] = exp2_fast((x[c] - m) * q.c);
         h[c] = !hard ? 0.f : a.temperature == 1.f ? e[c] : exp2_fast((x[c] - m) * q.c1);
         st += e[c];
@@ -773,6 +818,7 @@ __global__ __launch_bounds__(256, 4) void distill_short_kernel(DistillArgs a)
         s.y = wave_sum(st);
         s.z = hard ? wave_sum(s1) : 0.f;
         s.w = TAIL ? wave_sum(so) : 0.f;
+        if (TAIL && s.w == 0.f && __any(some)) s.w = OUTSIDE_TINY;
     }
     const bool none = padding || s.y == 0.f;
     Outside outside;

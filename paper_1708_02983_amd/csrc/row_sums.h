@@ -49,10 +49,16 @@ template <int VEC> struct Reference {
 // Running sums of a thread, relative to a reference that its wavefront shares: the largest logit of the first slots that
 // hold any, moved only when a slot's exponentials sum up to more than 2^24 (sums of 2^20 such terms are far from fp32's end),
 // so that the loop over a row needs neither a maximum nor a rescaling, only a comparison per 128 bits.
+//
+// The sum outside the teacher's places is 0 if and only if every logit there is masked: where its terms are all below fp32, OUTSIDE_TINY
+// stands for them.
+static constexpr float OUTSIDE_TINY = 0x1p-100f;
 template <int VEC, bool TAIL, int HARD> struct RowSums {
     const Scales &q;
     Reference<VEC> at;
     float st = 0.f, s1 = 0.f, so = 0.f;
+    bool some = false;        // a logit above -inf outside the teacher's places: noted where nothing else tells of it
+    bool settled = false;     // uniform: some lane has one, or a sum above 0
 
     __device__ __forceinline__ RowSums(const Scales &q) : q(q), at(q) {}
     // Whole wavefronts call it (lanes without a slot with an empty one).  skip: a bit for every element that is one of the
@@ -98,6 +104,7 @@ template <int VEC, bool TAIL, int HARD> struct RowSums {
             at.set(t, q);
             const float f = change(old, at, q.c, old.lost, at.lost), f1 = change(old, at, q.c1, old.lost1, at.lost1);
             st *= f;
+            if constexpr (TAIL) some = some || so > 0.f;
             so *= f;
             s1 *= f1;
         }
@@ -114,6 +121,14 @@ template <int VEC, bool TAIL, int HARD> struct RowSums {
             } else so += sum;
         }
     }
+    // For whole wavefronts, after some slots: calls look() as long as no exponential outside the teacher's places has been above 0 and no look at
+    // the slots has found a logit there that is not masked.  In all but masked rows that ends with the first slots.
+    template <typename L> __device__ __forceinline__ void until_settled(L look)
+    {
+        if (!TAIL || settled) return;
+        if (!__any(so > 0.f)) look();
+        settled = __any(some || so > 0.f);
+    }
     // what sums relative to `old` are multiplied with to be relative to `now`
     __device__ static __forceinline__ float change(const Reference<VEC> &old, const Reference<VEC> &now, float c, float old_lost, float now_lost)
     {
@@ -124,6 +139,7 @@ template <int VEC, bool TAIL, int HARD> struct RowSums {
     {
         constexpr int WAVES = BLOCK / 64;
         const float f = exp2_fast(-at.lost), f1 = exp2_fast(-at.lost1);
+        if constexpr (TAIL) so = some && so == 0.f ? OUTSIDE_TINY : so;
         float4 w = make_float4(at.ref, wave_sum(st) * f, wave_sum(s1) * f1, wave_sum(so) * f);
         static_assert(WAVES > 1, "part is used");
         if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = w;
@@ -150,7 +166,7 @@ template <int VEC, bool TAIL, int HARD> struct RowSums {
         const float f = exp2_fast(d * q.c);
         w.y += p.y * f;
         w.z += p.z * exp2_fast(d * q.c1);
-        w.w += p.w * f;
+        if constexpr (TAIL) w.w = fmaxf(w.w + p.w * f, p.w > 0.f ? OUTSIDE_TINY : 0.f);
     }
 };
 

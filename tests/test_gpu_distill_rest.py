@@ -105,6 +105,29 @@ def test_finite_masks(V):
     check(z, idx, val, 0.5, 0.0, "fp32", 25 if V > 3000 else 1, 8.0)
 
 
+@pytest.mark.parametrize("V, many", SHAPES)
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_few_places_in_masked_rows(dtype, V, many):
+    """Nearly all of a row is masked with -inf: one logit outside the teacher's places far below them (beside one of them, at either end, or
+    none at all), and outside logits that come before the ones that dwarf them."""
+    rows = len(GAPS)
+    rng = np.random.default_rng(V)
+    z = np.full((rows, V), -np.inf)
+    idx = np.full((rows, 4), -1, np.int32)
+    val = rng.normal(2.0, 1.0, (rows, 4)).astype(F)
+    for r in range(rows):
+        idx[r, :3] = V - 1 - rng.permutation(min(V, 40) - 1)[:3] if r % 2 else 1 + rng.permutation(min(V, 40) - 1)[:3]
+        free = np.setdiff1d(np.arange(V), idx[r, :3])
+        where = (free[0], free[-1], free[np.argmin(np.abs(free - idx[r, 0]))], None)[r % 4]
+        z[r, idx[r, :3]] = rng.normal(0, 1, 3)
+        if where is not None:
+            z[r, where] = -500.0 if r < 8 else -90.0
+        if r >= 9:
+            z[r, free[:max(1, V // 3)]] = -400.0 + rng.normal(0, 1, max(1, V // 3))
+    check(torch.from_numpy(z).to(DTYPES[dtype]), idx, val, 1.0, 0.0, dtype, many, 16.0)
+    check(torch.from_numpy(z).to(DTYPES[dtype]), idx, val, 0.5, 0.0, dtype, many, 16.0)
+
+
 def test_the_place_that_is_all():
     """One place at 100, the others at 0: loss 0.9 log 0.9 + 0.1 log(0.1 / 999) + 0.1 * 100, as worked out by hand."""
     import paper_1708_02983_amd as hip
