@@ -142,6 +142,9 @@ def _stream(stream) -> ctypes.c_void_p:
         if _raw_current_stream is not None:
             return ctypes.c_void_p(_raw_current_stream(torch.cuda.current_device()))
         stream = torch.cuda.current_stream()
+    device = getattr(stream, "device", None)
+    if isinstance(device, torch.device) and device.index not in (None, torch.cuda.current_device()):
+        raise ValueError(f"stream is on {device}, the current device is cuda:{torch.cuda.current_device()}")
     return ctypes.c_void_p(stream.cuda_stream)
 
 
@@ -571,11 +574,15 @@ def easgd_grad_distill(dims: Sequence[int], W, X, indices, values, G, loss=None,
         raise ValueError(f"invalid layer widths {list(dims)}")
     need = (P - 1) * ld + N
     nbytes = easgd_grad_workspace_bytes(dims, P, b)
+    for name, t in (("W", W), ("G", G)):
+        _dev(name, t, _F32, need)
+        if t.get_device() != on:
+            raise ValueError(f"{name} must be on cuda:{on}, is on {t.device}")
     workspace, ws, size = _scratch(nbytes, workspace, W, stream)
-    _check(_lib.easgd_grad_distill(arr, L, _dev("W", W, _F32, need), ld, _given("X", X, _F32, (P, b, dims[0]), on),
+    _check(_lib.easgd_grad_distill(arr, L, W.data_ptr(), ld, _given("X", X, _F32, (P, b, dims[0]), on),
                                    _given("indices", indices, _I32, (P, b, k), on), _given("values", values, _F32, (P, b, k), on),
                                    _given("teacher_lse", teacher_lse, _F32, (P, b), on), k, _given("labels", labels, _I32, (P, b), on),
-                                   P, b, temperature, hard, _dev("G", G, _F32, need), _given("loss", loss, _F32, (P,), on), ws, size, _stream(stream)))
+                                   P, b, temperature, hard, G.data_ptr(), _given("loss", loss, _F32, (P,), on), ws, size, _stream(stream)))
     return workspace
 
 

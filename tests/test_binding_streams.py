@@ -72,3 +72,20 @@ def test_workspaces_of_the_network_calls(monkeypatch, call):
         else:
             m.binding.easgd_mlp_round(dims, W, W, X, y, 0.1, 0.1, stream="side")
     assert [t.pool for t in m.made] == ["side"] and m.made[0].users == ["caller"]
+
+
+def test_a_stream_of_another_device(monkeypatch):
+    """Kernels on it would run on a device that does not have the tensors."""
+    from paper_1708_02983_amd import binding
+
+    class Stream:
+        cuda_stream = 5
+
+        def __init__(self, device):
+            self.device = device
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match="stream is on cuda:1, the current device is cuda:0"):
+        binding._stream(Stream(torch.device("cuda:1")))
+    assert binding._stream(Stream(torch.device("cuda:0"))).value == 5
+    assert binding._stream(Stream("anything")).value == 5

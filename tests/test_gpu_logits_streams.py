@@ -73,3 +73,16 @@ def test_streams_that_are_only_a_handle():
     tokens, _ = hip.easgd_sample_tokens(z, u, stream=Handle(side))
     side.synchronize()
     assert torch.equal(tokens, hip.easgd_sample_tokens(z, u)[0])
+
+
+def test_replicas_of_another_device_than_the_current_one(monkeypatch):
+    """Refused by name, before a workspace is made or anything is launched."""
+    import paper_1708_02983_amd as hip
+    dims, P, b, k = (20, 10), 2, 4, 3
+    W, X = torch.zeros(P, 212, device="cuda"), torch.zeros(P, b, 20, device="cuda")
+    idx, val = torch.zeros(P, b, k, dtype=torch.int32, device="cuda"), torch.zeros(P, b, k, device="cuda")
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    with pytest.raises(ValueError, match="W must be on cuda:1, is on cuda:0"):
+        hip.easgd_grad_distill(dims, W, X, idx, val, W.clone())
+    with pytest.raises(ValueError, match="logits is on cuda:0, the current device is cuda:1"):
+        hip.easgd_distill(X[0], idx[0], val[0])
