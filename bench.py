@@ -373,6 +373,7 @@ TRAFFIC_PROFILES = {
     ("grad", "cfg2"): (131_544.7 * 1024 * 2.000 + 149_337.0 * 1024 * 1.000, "profiles/easgd_grad_cfg2_hbm_traffic.md"),
 }
 TRAFFIC_PROFILED_VERSION = 512      # easgd_version() of the library the summaries above were taken with
+TRAFFIC_VERSIONS = (512, 513)       # those with the same kernels there: 513 has the calls on rows of logits besides
 
 
 def traffic_fields(hip, key):
@@ -381,12 +382,12 @@ def traffic_fields(hip, key):
     default_opts = (hip.get_option(hip.OPT_UPDATE_GROUPS) == 0 and hip.get_option(hip.OPT_UPDATE_LAYOUT) == 2
                     and hip.get_option(hip.OPT_UPDATE_NONTEMPORAL) == 2
                     and hip.get_option(hip.OPT_UPDATE_BLOCKS_PER_CU) == 0 and hip.get_option(hip.OPT_GEMM_TILE) == 0)
-    if entry is None or not default_opts or hip.version() != TRAFFIC_PROFILED_VERSION:
+    if entry is None or not default_opts or hip.version() not in TRAFFIC_VERSIONS:
         return {"traffic": None}
     return {"traffic": entry[0],
             "traffic_from": {"profile": entry[1], "library_version": TRAFFIC_PROFILED_VERSION,
-                             "note": "counter reading of an earlier rocprofv3 session with this library version, "
-                                     "not of this run"}}
+                             "note": "counter reading of an earlier rocprofv3 session with that library version, whose "
+                                     "kernels these are; not of this run"}}
 
 
 def hbm_roofline(hip, kernel, traffic_key, nbytes, update_ms, ceilings):
