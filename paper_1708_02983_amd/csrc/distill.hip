@@ -388,9 +388,9 @@ __device__ __forceinline__ void name_places(const DistillArgs &a, size_t r, cons
 // The first NV * BLOCK slots of a row are requested at once and stay in registers between the two passes over it; what is
 // longer is read again, from the last-level cache while no more rows are under way than it holds.  Gradients are stored past the
 // caches (nobody reads them here).  Measured: 2048 x 131072 bf16, loss and gradient, 232 us = 4.6 TB/s of what has to move, with
-// the vector ALUs 56 % busy (a copy of that size by the library takes 203); 777 x 50001 fp16 43 us = 3.6 TB/s (its rows start at
+// the vector ALUs 50 % busy (a copy of that size by the library takes 203); 777 x 50001 fp16 43 us = 3.6 TB/s (its rows start at
 // odd addresses; copy 31).  A row of 2048 logits costs its block more in the teacher's numbers than in the row: 16384 x 2048
-// bf16 153 us against 26 for a copy.
+// bf16, k = 64, 117 us against 20 for a copy (both on one set of inputs, which the last-level cache holds).
 template <int DT, int BLOCK, int NV, bool TAIL, int HARD, bool GRAD>
 __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
 {
@@ -606,7 +606,7 @@ __global__ __launch_bounds__(256) void distill_join_kernel(DistillArgs a)
 
 // ---- backward: gradients of parts of rows ----------------------------------------------------------------------------
 // The forward pass left a row's sums, so that this is one pass with one exponential a logit (two where hard asks for another).
-// Bound: HBM.  1024 x 32000 bf16: 32.6 us = 4.0 TB/s.
+// Bound: HBM, and one wave of blocks that ask for their first logits when the teacher's numbers are done.  1024 x 32000 bf16: 32.8 us = 4.0 TB/s.
 template <int DT, int BLOCK, bool TAIL, int HARD>
 __global__ __launch_bounds__(BLOCK) void distill_grad_kernel(DistillArgs a)
 {
@@ -664,7 +664,7 @@ __global__ __launch_bounds__(BLOCK) void distill_grad_kernel(DistillArgs a)
 // Rows of at most 64 * NQ logits sit in a wavefront's registers, element lane + 64 q in x[q]; maximum and sums are shuffles,
 // and nothing waits for other wavefronts.  LDS holds the teacher's slots and, for every element, its target (-1: not one
 // of the teacher's places).  Bound: latency (one trip to memory, two chains of 64-bit exponentials and logarithms).
-// Measured: 2048 x 100 fp32 7.4 us, of which a launch that does nothing is some 2.  Beyond 1024 logits a block a row is faster
+// Measured: 2048 x 100 fp32 7.6 us, of which a launch that does nothing is some 2.  Beyond 1024 logits a block a row is faster
 // (16384 x 2040 bf16: 136 us, 202 with 32 registers a lane here).
 template <int DT, int NQ, bool TAIL, int MODE>
 __global__ __launch_bounds__(256, 4) void distill_short_kernel(DistillArgs a)

@@ -7,12 +7,12 @@
 //   top_p:                    the mass of the row in bins of equal width below the largest logit, then the bin of the border
 //   neither:                  no border to find
 // Bound: latency of the passes over a row (which stays in the caches) and, where masses of whole rows are asked for, the vector
-// ALUs: some 25 instructions a logit for a 64-bit exponential.  A row is one block's: cut into parts over several blocks, with
-// the launches that this takes, it was not faster.  Measured (us), top_k 50:
-//   1 x 131072 bf16         none 35   top_k 26   top_p 100   min_p 18   greedy 12
-//   256 x 131072 bf16       none 48   top_k 33   top_p 120   min_p 36   greedy 17
-//   512 x 32000 fp16        none 26   top_k 21   top_p 55    min_p 22   greedy 11.5
-//   2048 x 1000 fp32        none 15   top_k 24   top_p 28    min_p 16   greedy 13.5
+// ALUs: some 25 instructions a logit for a 64-bit exponential.  A row is one block's, however few rows there are.  Measured (us a call,
+// temperature 0.9, top_k 50 or 1000, top_p 0.9, min_p 0.05):
+//   1 x 131072 bf16         none 35   top_k 27 / 74   top_p 97    min_p 18   greedy 12
+//   256 x 131072 bf16       none 47   top_k 33 / 87   top_p 119   min_p 44   greedy 17
+//   512 x 32000 fp16        none 27   top_k 21 / 44   top_p 55    min_p 21   greedy 11
+//   2048 x 1000 fp32        none 15   top_k 24 / 15   top_p 28    min_p 16   greedy 13
 #include "logits.h"
 #include "logits_select.h"
 
@@ -58,8 +58,8 @@ struct Weight {
         __syncthreads();
     }
     static __device__ __forceinline__ double power(int n) { return __builtin_bit_cast(double, (unsigned long long)(n + 1023) << 52); }
-    // 2^y units, not yet whole; no branch, so that the elements of a slot are computed side by side (256 rows of 131072 with one
-    // top_p: 112 us, 125 us with each element's own branches).  Product and sum stay two roundings wherever a logit's units are
+    // 2^y units, not yet whole; no branch, so that the elements of a slot are computed side by side (256 rows of 131072 with
+    // mixed filters: 109 us, 125 us with each element's own branches).  Product and sum stay two roundings wherever a logit's units are
     // asked for: joined in some places and not in others, two passes could disagree by a unit.
     __device__ __forceinline__ double scaled(float z) const
     {

@@ -38,9 +38,10 @@ __device__ __forceinline__ void write_list(const TopArgs &a, size_t r, const uns
 }
 
 // ---- a block per row, or per part of a row ------------------------------------------------------------------------------
-// Measured: 2048 x 131072 bf16, k = 64, 167 us = 3.2 TB/s: the vector ALUs are busy 70 to 80 % of it (141 instructions a
-// wavefront for 64 slots: unpacking, an exponential, sum and comparison for each of eight logits), the rest is barriers between
-// the four loads in flight.
+// Measured: 2048 x 131072 bf16, k = 64, 166 us a call in a row of calls = 3.2 TB/s, 179 traced by itself; the vector ALUs are busy 66 % of
+// it.  Of 127 instructions a wavefront for 64 slots some 50 to 60 are the sums' (the two passes of distill_rows_kernel, with the packing, take 118);
+// the others are selection: in the first rounds most slots hold a logit above the floor, which sends the whole wavefront through
+// mask, key and list for it, and the list is ranked at the end.
 template <int DT, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void top_rows_kernel(TopArgs a)
 {
@@ -175,7 +176,11 @@ __global__ __launch_bounds__(256) void top_short_kernel(TopArgs a)
 
 // Few long rows are cut into parts, so that there are blocks for the whole chip: each part's first k go through the workspace.
 // Many rows take blocks of 256 threads, five of which a compute unit holds (2048 x 131072 bf16, k = 64: 168 us against 180 with 512);
-// few rows, and more than 64 tokens (whose first floor wants many maxima), 512 (8 x 50001: 15.8 us against 18.5 with 256).
+// few rows, and more than 64 tokens (whose first floor wants many maxima), 512 (8 x 50001: 15.8 us against 18.5 with 256).  The change at
+// 256 rows suits a thousand rows and more better than some hundred, which leave a compute unit one to three blocks (us; 512 threads: k = 128):
+//   rows of 131072 bf16     255 (four parts each)   256    512    768    1024   2048
+//   256 threads, k = 64     49 (512 threads)        65     71     77     88     166
+//   512 threads, k = 128    65                      46     56     88     106    204
 static constexpr int TOP_BLOCK = 512, TOP_SHORT_V = 1024;
 static constexpr int TOP_SPLIT_ROWS = 256, TOP_SPLIT_SLOTS = 2048;
 static int top_segments(size_t rows, int slots, int k)
