@@ -417,7 +417,8 @@ int easgd_top_logits(const void *logits, int dtype, size_t rows, int V, size_t l
  *   loss         DEVICE out [rows] fp32
  *   state        DEVICE out [rows][4] fp32, 16-byte aligned   for the backward pass: m (the largest logit, or one near it), sum exp((z-m)/T), sum exp(z-m) (unused
  *                                            where hard is 0), the first sum over the places outside S (0 without teacher_lse, or where all
- *                                            logits there are -inf; where it is below 2^-64 both passes sum the row's logits again)
+ *                                            logits there are -inf; below 2^-64 it only says that some are not, and both passes sum the
+ *                                            row's logits again)
  *   scale, dloss     the gradient is that of scale * sum over the rows of dloss[row] * loss[row]; dloss DEVICE in [rows] fp32, or
  *                    NULL: all 1.  (Mean losses of b samples: scale = 1/b.)
  *   dlogits      DEVICE out [rows][dld], element type of logits; entries [V, dld) of a row are not written; aligned like
