@@ -373,7 +373,7 @@ TRAFFIC_PROFILES = {
     ("grad", "cfg2"): (131_544.7 * 1024 * 2.000 + 149_337.0 * 1024 * 1.000, "profiles/easgd_grad_cfg2_hbm_traffic.md"),
 }
 TRAFFIC_PROFILED_VERSION = 512      # easgd_version() of the library the summaries above were taken with
-TRAFFIC_VERSIONS = (512, 513)       # those with the same kernels there: 513 has the calls on rows of logits besides
+TRAFFIC_VERSIONS = (512, 513, 514)  # those with the same kernels there: 513 has the calls on rows of logits besides, 514 those on tokens and AdamW
 
 
 def traffic_fields(hip, key):

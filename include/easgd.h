@@ -199,6 +199,65 @@ int sync_sgd_round(float *W, float *V, const float *G,
                    float eta, float delta, void *stream);
 
 /*
+ * An AdamW step of the same replicas as the worker rule (an extension: the paper's rules are SGD and momentum), with or without the
+ * elastic exchange.  For worker i, parameter j of tensor s, in step t = 1, 2, ...:
+ *
+ *     g = clip[i] * G[i][j]
+ *     M[i][j] <- beta1*M[i][j] + (1-beta1)*g              S[i][j] <- beta2*S[i][j] + (1-beta2)*g*g
+ *     W[i][j] <- W[i][j] - eta*rate_s*( M[i][j]/(1-beta1^t) / (sqrt(S[i][j]/(1-beta2^t)) + eps) + decay_s*W[i][j] ) - eta*rho*d_i
+ *     Wc[j]   <- Wc[j] + eta*rho*(d_0 + ... + d_{P-1})     Eq. (2), d_i = W[i][j] - Wc[j] with time-t values, ascending i
+ *
+ *   W, M, S  DEVICE in/out [P][ld] fp32   replicas, first and second moments (0 before the first step)
+ *   G        DEVICE in [P][ld], never written; dtype EASGD_F32, EASGD_BF16 or EASGD_F16: its elements
+ *   Wc       DEVICE in/out [N], or NULL: every worker's own step, no exchange (then rho == 0)
+ *   ends     DEVICE in [tensors] int64    where the tensors of a replica end, ascending: tensor s is [ends[s-1], ends[s]) (equal ends: no
+ *                                         parameter).  Parameters behind the last end have rate 1 and `decay`; tensors == 0: all of them.
+ *   rates, decays  DEVICE in [tensors] fp32   every tensor's factor of eta and its decay
+ *   clip     DEVICE in [P] fp32, or NULL: 1.  A worker whose clip is 0 sits the step out: its M and S are left as they are, and its W
+ *                                         takes part in the exchange only, whatever its G holds (easgd_grad_norms gives such factors).
+ *   eta_at, step_at  DEVICE in [1] fp32 / int64, or NULL   read in the place of eta and step when the kernel runs: a captured call takes the
+ *                                         values of its replay (step_at below 1 counts as 1)
+ *   beta1, beta2 in [0, 1), eps > 0, step >= 1; N <= 2^34.
+ * The moments' arithmetic is fixed, every operation rounded on its own: fl(fl(beta1*M) + fl(fl(1-beta1)*g)), fl(fl(beta2*S) +
+ * fl(fl(fl(1-beta2)*g)*g)).  Results are the same bits from run to run.  128-bit accesses where W, Wc (and M, S) are 16-byte and G is
+ * four elements aligned and ld % 4 == 0; element by element otherwise, with the same values.
+ *
+ * adamw_round_8bit: the moments held in 8 bits between the steps, M as e4m3 and S as e5m2 (OCP), 256 consecutive parameters of a
+ * replica (the last ones fewer) with a power of two in common per moment:
+ *   M, S               DEVICE in/out [P][ld] one byte each (4-byte aligned for the fast path); entries [N, ld) are neither read nor written
+ *   M_scale, S_scale   DEVICE in/out [P][ceil(N/256)] fp32: M[i][j] stands for e4m3(M[i][j]) * M_scale[i][j/256], likewise S (all 0 before the first step)
+ * W moves by the new moments before they are rounded.  Then, with e such that the block's largest |M| is in [2^(e+7), 2^(e+8)) (its largest S in
+ * [2^(e+14), 2^(e+15)); e >= -126), 2^e becomes the block's scale and every moment times 2^-e is rounded to one of its two neighbours at
+ * random, up with its distance from the lower one as probability (16 bits of it), so that moments are exact on average; an S above 0 never becomes 0.
+ * The random bits of parameter j = 4 g + 2 w + h of worker i in step t are bits [16 h, 16 h + 16) of mix(g ^ mix(mix(seed + i*0x9E3779B1) +
+ * t*0x85157AF5 + w*0x632BE5AB)) in 32-bit arithmetic, mix(x): x ^= x >> 16, x *= 0x6C8E9CF5, x ^= x >> 15, x *= 0x2F5D7A4B, x ^= x >> 16: stored codes
+ * are the same for the same seed and step.  A block in which a new moment is infinite or NaN gets the scale NaN.
+ * Errors: EASGD_EINVAL, EASGD_ERANGE, EASGD_ELAUNCH.
+ */
+int adamw_round(float *W, float *M, float *S, const void *G, int dtype, float *Wc, int P, size_t N, size_t ld,
+                const int64_t *ends, const float *rates, const float *decays, int tensors, const float *clip,
+                float eta, const float *eta_at, float rho, float beta1, float beta2, float eps, float decay,
+                int64_t step, const int64_t *step_at, void *stream);
+int adamw_round_8bit(float *W, uint8_t *M, uint8_t *S, float *M_scale, float *S_scale, const void *G, int dtype, float *Wc, int P, size_t N, size_t ld,
+                     const int64_t *ends, const float *rates, const float *decays, int tensors, const float *clip,
+                     float eta, const float *eta_at, float rho, float beta1, float beta2, float eps, float decay,
+                     int64_t step, const int64_t *step_at, uint32_t seed, void *stream);
+
+/*
+ * The L2 norm of every worker's gradient, and the factor that brings it down to max_norm:
+ *
+ *     norm[i] = sqrt(G[i][0]^2 + ... + G[i][N-1]^2)        clip[i] = min(1, max_norm / norm[i]); 0 where norm[i] is infinite or NaN
+ *
+ *   G      DEVICE in [P][ld], dtype EASGD_F32, EASGD_BF16 or EASGD_F16
+ *   norm   DEVICE out [P] fp32;  clip  DEVICE out [P] fp32, or NULL;  max_norm > 0 (infinity: no limit)
+ *   workspace  as for the calls on rows of logits, easgd_grad_norms_workspace_bytes bytes (0 for short rows);  N <= 2^34, P <= 65535
+ * Squares are added in 64 bits, in a fixed order.  Errors: EASGD_EINVAL, EASGD_ERANGE, EASGD_EWORKSPACE, EASGD_ELAUNCH.
+ */
+size_t easgd_grad_norms_workspace_bytes(int P, size_t N);
+int easgd_grad_norms(const void *G, int dtype, int P, size_t N, size_t ld, float max_norm, float *norm, float *clip,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Step (1) of the round (Section 5.1; forward/backward propagation of Section
  * 2.2) for a dense ReLU multilayer perceptron with softmax cross-entropy loss,
  * averaged over the b samples of each worker's minibatch.  Worker i uses its
@@ -445,6 +504,60 @@ int easgd_distill(const void *logits, int dtype, size_t rows, int V, size_t ld,
                   const int32_t *indices, const float *values, const float *teacher_lse, int k, const int32_t *labels,
                   float temperature, float hard, float scale, float *loss, void *dlogits, size_t dld,
                   void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Tokens that are given: what a row of logits says about them, and learning from that.  Per row, with q = softmax(z / temperature) and
+ * the row's token t:
+ *
+ *   logprob = log q[t]        entropy = -sum_j q[j] log q[j]        rank = the number of logits before the token in the row's order
+ *
+ *   tokens       DEVICE in [rows] int32, or NULL (then logprob and rank are NULL, too).  A row whose token is outside [0, V) is padding:
+ *                                     its logits are not read, its logprob, entropy and gradient are 0, its rank is -1, and it has no alternatives.
+ *   logprob      DEVICE out [rows] fp32, or NULL
+ *   entropy      DEVICE out [rows] fp32, or NULL
+ *   rank         DEVICE out [rows] int32, or NULL (0: the token is the first of the order; a masked or NaN token comes behind all logits above -inf)
+ *   top_logprob  DEVICE out [rows][k] fp32    log q of the first k of the order
+ *   top_indices  DEVICE out [rows][k] int32   where they stand; places that are left over hold -inf and -1.  k == 0: both are NULL.
+ *   state        DEVICE out [rows][4] fp32, 16-byte aligned, or NULL   for the backward pass: m (the largest logit, or one near it),
+ *                                     sum exp((z-m)/T), the entropy, 0; all 0 for padding
+ *   0 <= k <= EASGD_MAX_TOP; temperature in [1e-6, 1e6].
+ * A masked place (-inf) has q = 0 and adds nothing to the entropy; a token there has logprob -inf.  A row whose logits are all -inf
+ * has logprob -inf, entropy 0 and gradient 0.  A NaN or +inf among the row's logits gives NaN (ranks and alternatives' places stay as defined).
+ *
+ * easgd_score_tokens_grad: the gradient of scale * sum over the rows of (dlogprob[row] * logprob[row] + dentropy[row] * entropy[row]) from what
+ * easgd_score_tokens left in state:
+ *   d / d z[j] = scale / T * (dlogprob ([j == t] - q[j]) - dentropy q[j] (log q[j] + entropy))
+ *   dlogprob, dentropy  DEVICE in [rows] fp32; one of them may be NULL (0), dlogprob is where tokens is
+ *   dlogits      DEVICE out [rows][dld] as for easgd_distill: not in place
+ * The token's own place gets its share also where its logit is -inf.
+ *
+ * easgd_token_loss: both in one call, for losses that are known beforehand:
+ *   loss[row] = -weight[row] * logprob[row] - bonus * entropy[row], dlogits = the gradient of scale * sum over the rows of loss[row]
+ *   weight       DEVICE in [rows] fp32, or NULL: all 1 (advantages, or 0 for a token that does not count: its logprob is not looked at)
+ *   loss         DEVICE out [rows] fp32;  logprob, entropy as above, or NULL;  tokens is not NULL;  bonus, scale finite
+ * The loss of a row whose logits are all -inf is 0.
+ * Errors: EASGD_EINVAL, EASGD_ERANGE, EASGD_EWORKSPACE, EASGD_ELAUNCH.
+ */
+size_t easgd_score_tokens_workspace_bytes(size_t rows, int V, int k);
+int easgd_score_tokens(const void *logits, int dtype, size_t rows, int V, size_t ld, const int32_t *tokens, float temperature,
+                       float *logprob, float *entropy, int32_t *rank, int k, float *top_logprob, int32_t *top_indices, float *state,
+                       void *workspace, size_t workspace_bytes, void *stream);
+int easgd_score_tokens_grad(const void *logits, int dtype, size_t rows, int V, size_t ld, const int32_t *tokens, float temperature,
+                            const float *state, const float *dlogprob, const float *dentropy, float scale, void *dlogits, size_t dld, void *stream);
+size_t easgd_token_loss_workspace_bytes(size_t rows, int V);
+int easgd_token_loss(const void *logits, int dtype, size_t rows, int V, size_t ld, const int32_t *tokens, const float *weight, float bonus,
+                     float temperature, float scale, float *loss, float *logprob, float *entropy, void *dlogits, size_t dld,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Step (1) of a round as easgd_grad does it, with the loss of given tokens in the place of the softmax cross-entropy: the gradients of
+ * all workers' mean losses (sums of easgd_token_loss's losses over the worker's b samples, padding among them, over b).
+ *   tokens [P][b], weight [P][b] or NULL, bonus, temperature as for easgd_token_loss; logprob, entropy DEVICE out [P][b] or NULL;
+ *   every other argument, the workspace (easgd_grad_workspace_bytes), requirements and errors as for easgd_grad.
+ */
+int easgd_grad_token_loss(const int *dims, int n_layers, const float *W, size_t ld, const float *X, const int32_t *tokens, const float *weight,
+                          int P, int b, float bonus, float temperature, float *G, float *loss, float *logprob, float *entropy,
+                          void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Step (1) of a round as easgd_grad does it, with distillation in the place of the softmax cross-entropy: the gradients of all

@@ -16,6 +16,8 @@ Only ``tests/``, ``__graft_entry__.smoke()`` and the ``cpu_baseline`` leg of
   softmax cross-entropy (numpy, double arithmetic)
 * ``oracle.logits``  -- rows of logits: top logits, distillation and its gradient, sampled tokens, and the gradient of a
   network under the distillation loss (numpy, double arithmetic)
+* ``oracle.tokens``  -- rows of logits and given tokens: log probabilities, entropy, rank, alternatives, loss and gradient (numpy, double)
+* ``oracle.adamw``   -- AdamW rounds with moments in 32 and 8 bits, norms that clip gradients (numpy; stored bits in fp32, the rest in double)
 """
 from .elastic import (async_easgd, build, easgd_round, measgd_round, num_threads, set_num_threads,  # noqa: F401
                       sync_sgd_round)

@@ -10,6 +10,8 @@ _BINDING_NAMES = (
     "measgd_round", "easgd_sync_round_bf16", "measgd_round_bf16", "measgd_round_bf16v", "sync_sgd_round", "async_easgd_round", "hogwild_easgd_round", "stream_copy", "stream_triad", "stream_mix32", "mfma_probe", "launch_count", "get_option", "set_option", "lib", "version", "LIB_PATH",
     "easgd_top_logits", "easgd_top_logits_workspace_bytes", "easgd_distill", "easgd_distill_loss", "easgd_distill_grad", "easgd_distill_workspace_bytes", "easgd_grad_distill",
     "easgd_sample_tokens", "easgd_sample_tokens_workspace_bytes", "MAX_TOP",
+    "easgd_score_tokens", "easgd_score_tokens_workspace_bytes", "easgd_score_tokens_grad", "TokenScores", "easgd_token_loss", "easgd_token_loss_workspace_bytes",
+    "easgd_grad_token_loss", "easgd_grad_norms", "easgd_grad_norms_workspace_bytes", "adamw_round", "ADAMW_BLOCK",
     "OPT_UPDATE_BLOCKS_PER_CU", "OPT_UPDATE_NONTEMPORAL", "OPT_UPDATE_GROUPS", "OPT_GEMM_TILE", "OPT_ROUND_OVERLAP", "OPT_GEMM_XCD", "OPT_GEMM_PAIR", "OPT_MLP_HEAD", "OPT_UPDATE_LAYOUT", "OPT_ROUND_SINGLE_LAUNCH", "OPT_ROUND_SPIN_LIMIT", "round_barrier_timeouts",
 )
 __all__ = list(_BINDING_NAMES) + ["BatchFeeder"]

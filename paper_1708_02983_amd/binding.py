@@ -11,7 +11,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence
 
 import torch
 
@@ -92,6 +92,27 @@ def _load() -> ctypes.CDLL:
     lib.easgd_distill.restype = i
     lib.easgd_grad_distill.argtypes = [ip, i, vp, sz, vp, vp, vp, vp, i, vp, i, i, f, f, vp, vp, vp, sz, vp]
     lib.easgd_grad_distill.restype = i
+    lib.easgd_score_tokens_workspace_bytes.argtypes = [sz, i, i]
+    lib.easgd_score_tokens_workspace_bytes.restype = sz
+    lib.easgd_score_tokens.argtypes = [vp, i, sz, i, sz, vp, f, vp, vp, vp, i, vp, vp, vp, vp, sz, vp]
+    lib.easgd_score_tokens.restype = i
+    lib.easgd_score_tokens_grad.argtypes = [vp, i, sz, i, sz, vp, f, vp, vp, vp, f, vp, sz, vp]
+    lib.easgd_score_tokens_grad.restype = i
+    lib.easgd_token_loss_workspace_bytes.argtypes = [sz, i]
+    lib.easgd_token_loss_workspace_bytes.restype = sz
+    lib.easgd_token_loss.argtypes = [vp, i, sz, i, sz, vp, vp, f, f, f, vp, vp, vp, vp, sz, vp, sz, vp]
+    lib.easgd_token_loss.restype = i
+    lib.easgd_grad_token_loss.argtypes = [ip, i, vp, sz, vp, vp, vp, i, i, f, f, vp, vp, vp, vp, vp, sz, vp]
+    lib.easgd_grad_token_loss.restype = i
+    lib.easgd_grad_norms_workspace_bytes.argtypes = [i, sz]
+    lib.easgd_grad_norms_workspace_bytes.restype = sz
+    lib.easgd_grad_norms.argtypes = [vp, i, i, sz, sz, f, vp, vp, vp, sz, vp]
+    lib.easgd_grad_norms.restype = i
+    i64 = ctypes.c_int64
+    lib.adamw_round.argtypes = [vp, vp, vp, vp, i, vp, i, sz, sz, vp, vp, vp, i, vp, f, vp, f, f, f, f, f, i64, vp, vp]
+    lib.adamw_round.restype = i
+    lib.adamw_round_8bit.argtypes = [vp, vp, vp, vp, vp, vp, i, vp, i, sz, sz, vp, vp, vp, i, vp, f, vp, f, f, f, f, f, i64, vp, ctypes.c_uint32, vp]
+    lib.adamw_round_8bit.restype = i
     lib.easgd_sample_tokens_workspace_bytes.argtypes = [sz, i]
     lib.easgd_sample_tokens_workspace_bytes.restype = sz
     lib.easgd_sample_tokens.argtypes = [vp, i, sz, i, sz, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
@@ -605,6 +626,208 @@ def easgd_sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min
                                     _given("min_p", min_p, _F32, shape, on), _given("tokens", tokens, _I32, shape, on),
                                     _given("logprob", logprob, _F32, shape, on), ws, nbytes, _stream(stream)))
     return tokens, logprob
+
+
+class TokenScores(NamedTuple):
+    """What easgd_score_tokens says about the rows; None for what was not asked for."""
+    logprob: Optional[torch.Tensor]
+    entropy: Optional[torch.Tensor]
+    rank: Optional[torch.Tensor]
+    top_logprob: Optional[torch.Tensor]
+    top_indices: Optional[torch.Tensor]
+    state: Optional[torch.Tensor]
+
+
+@functools.lru_cache(maxsize=256)
+def easgd_score_tokens_workspace_bytes(rows: int, V: int, k: int) -> int:
+    return int(_lib.easgd_score_tokens_workspace_bytes(rows, V, k))
+
+
+@functools.lru_cache(maxsize=256)
+def easgd_token_loss_workspace_bytes(rows: int, V: int) -> int:
+    return int(_lib.easgd_token_loss_workspace_bytes(rows, V))
+
+
+def _asked(what, shape, dtype, like, stream):
+    """An optional result: None or False (not asked for), True (a new tensor) or the caller's tensor."""
+    if what is None or what is False:
+        return None
+    return _new(shape, dtype, like, stream) if what is True else what
+
+
+def easgd_score_tokens(logits, tokens=None, temperature: float = 1.0, k: int = 0, logprob=None, entropy=True, rank=None,
+                       top_logprob=None, top_indices=None, state=None, workspace=None, stream=None) -> TokenScores:
+    """Log probabilities of given tokens [rows] int32 under the rows of logits [rows][V] (fp32, bf16 or fp16, rows may be strided) at a
+    temperature, the rows' entropies, the tokens' ranks, and the k first alternatives as log probabilities with their places.
+    entropy, rank and state (for easgd_score_tokens_grad) are a tensor to fill, True for a new one, or None where they are not
+    wanted.  A token outside [0, V) marks a padded row; without tokens there are no logprob and no rank."""
+    ptr, code, rows, V, ld = _logit_rows("logits", logits)
+    k, on, shape = int(k), logits.get_device(), (rows,)
+    if k < 0 or k > MAX_TOP:
+        raise ValueError(f"k must be in [0, {MAX_TOP}], got {k}")
+    if logprob is None and tokens is not None:
+        logprob = _new(shape, _F32, logits, stream)
+    entropy = _asked(entropy, shape, _F32, logits, stream)
+    rank = _asked(rank, shape, _I32, logits, stream)
+    state = _asked(state, (rows, 4), _F32, logits, stream)
+    if k == 0 and (top_logprob is not None or top_indices is not None):
+        raise ValueError("top_logprob and top_indices need k > 0")
+    if k and top_logprob is None:
+        top_logprob = _new((rows, k), _F32, logits, stream)
+    if k and top_indices is None:
+        top_indices = _new((rows, k), _I32, logits, stream)
+    keep, ws, nbytes = _scratch(easgd_score_tokens_workspace_bytes(rows, V, k), workspace, logits, stream)
+    _check(_lib.easgd_score_tokens(ptr, code, rows, V, ld, _given("tokens", tokens, _I32, shape, on), temperature,
+                                   _given("logprob", logprob, _F32, shape, on), _given("entropy", entropy, _F32, shape, on),
+                                   _given("rank", rank, _I32, shape, on), k, _given("top_logprob", top_logprob, _F32, (rows, k), on),
+                                   _given("top_indices", top_indices, _I32, (rows, k), on), _given("state", state, _F32, (rows, 4), on),
+                                   ws, nbytes, _stream(stream)))
+    return TokenScores(logprob, entropy, rank, top_logprob, top_indices, state)
+
+
+def easgd_score_tokens_grad(logits, tokens, state, temperature: float = 1.0, dlogprob=None, dentropy=None, scale: float = 1.0,
+                            dlogits=None, stream=None):
+    """Backward pass of easgd_score_tokens: the gradient of scale * sum(dlogprob * logprob + dentropy * entropy) with respect to the
+    logits, in their type; either of dlogprob and dentropy [rows] may be None."""
+    ptr, code, rows, V, ld = _logit_rows("logits", logits)
+    on, shape = logits.get_device(), (rows,)
+    dlogits, dptr, dld = _gradient_rows(logits, dlogits, rows, V, stream)
+    _check(_lib.easgd_score_tokens_grad(ptr, code, rows, V, ld, _given("tokens", tokens, _I32, shape, on), temperature,
+                                        _given("state", state, _F32, (rows, 4), on), _given("dlogprob", dlogprob, _F32, shape, on),
+                                        _given("dentropy", dentropy, _F32, shape, on), scale, dptr, dld, _stream(stream)))
+    return dlogits
+
+
+def easgd_token_loss(logits, tokens, weight=None, bonus: float = 0.0, temperature: float = 1.0, scale: float = 1.0, loss=None, logprob=None,
+                     entropy=None, dlogits=None, workspace=None, stream=None):
+    """Loss and gradient of given tokens in one call: loss = -weight * logprob - bonus * entropy of every row, and the gradient of
+    scale * sum(loss).  Returns loss, logprob, entropy (None unless it is a tensor or True) and dlogits."""
+    ptr, code, rows, V, ld = _logit_rows("logits", logits)
+    on, shape = logits.get_device(), (rows,)
+    if loss is None:
+        loss = _new(shape, _F32, logits, stream)
+    if logprob is None:
+        logprob = _new(shape, _F32, logits, stream)
+    entropy = _asked(entropy, shape, _F32, logits, stream)
+    dlogits, dptr, dld = _gradient_rows(logits, dlogits, rows, V, stream)
+    keep, ws, nbytes = _scratch(easgd_token_loss_workspace_bytes(rows, V), workspace, logits, stream)
+    _check(_lib.easgd_token_loss(ptr, code, rows, V, ld, _given("tokens", tokens, _I32, shape, on), _given("weight", weight, _F32, shape, on),
+                                 bonus, temperature, scale, _given("loss", loss, _F32, shape, on), _given("logprob", logprob, _F32, shape, on),
+                                 _given("entropy", entropy, _F32, shape, on), dptr, dld, ws, nbytes, _stream(stream)))
+    return loss, logprob, entropy, dlogits
+
+
+def easgd_grad_token_loss(dims: Sequence[int], W, X, tokens, G, loss=None, weight=None, bonus: float = 0.0, temperature: float = 1.0, logprob=None,
+                          entropy=None, workspace=None, stream=None):
+    """Step (1) with the loss of given tokens in the place of the softmax cross-entropy: gradients of all P workers into G[P][ld] from
+    tokens [P][b] and weight [P][b]; logprob and entropy [P][b] are filled where they are given.  Returns the workspace used."""
+    arr, L = _dims(dims)
+    if W.dim() != 2 or X.dim() != 3:
+        raise ValueError("expected W[P][ld], X[P][b][d_in]")
+    P, ld = W.shape
+    b, on = X.shape[1], torch.cuda.current_device()
+    N = easgd_mlp_num_params(dims)
+    if N == 0:
+        raise ValueError(f"invalid layer widths {list(dims)}")
+    need = (P - 1) * ld + N
+    for name, t in (("W", W), ("G", G)):
+        _dev(name, t, _F32, need)
+        if t.get_device() != on:
+            raise ValueError(f"{name} must be on cuda:{on}, is on {t.device}")
+    workspace, ws, size = _scratch(easgd_grad_workspace_bytes(dims, P, b), workspace, W, stream)
+    shape = (P, b)
+    _check(_lib.easgd_grad_token_loss(arr, L, W.data_ptr(), ld, _given("X", X, _F32, (P, b, dims[0]), on), _given("tokens", tokens, _I32, shape, on),
+                                      _given("weight", weight, _F32, shape, on), P, b, bonus, temperature, G.data_ptr(),
+                                      _given("loss", loss, _F32, (P,), on), _given("logprob", logprob, _F32, shape, on),
+                                      _given("entropy", entropy, _F32, shape, on), ws, size, _stream(stream)))
+    return workspace
+
+
+# ---- AdamW on the replicas ---------------------------------------------------------------------------------------
+
+def _replica_rows(name: str, t, N: Optional[int]):
+    """Address, element type, P, N and ld of a matrix of replicas or gradients on the current device."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA/HIP tensor")
+    code = _LOGIT_TYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be torch.float32, torch.bfloat16 or torch.float16, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    P, ld, N = _replica_shape(t, N)
+    if N < 1 or N > ld:
+        raise ValueError(f"N must be in [1, {ld}], got {N}")
+    here = torch.cuda.current_device()
+    if t.get_device() != here:
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{here}")
+    return t.data_ptr(), code, P, N, ld, here
+
+
+@functools.lru_cache(maxsize=256)
+def easgd_grad_norms_workspace_bytes(P: int, N: int) -> int:
+    return int(_lib.easgd_grad_norms_workspace_bytes(P, N))
+
+
+def easgd_grad_norms(G, max_norm: float = float("inf"), N: Optional[int] = None, norm=None, clip=None, workspace=None, stream=None):
+    """The L2 norm of every worker's gradient G[P][ld] (fp32, bf16 or fp16) and the factor min(1, max_norm / norm) that clips it (0 where the
+    norm is infinite or NaN).  Returns norm [P] and clip [P], which adamw_round takes."""
+    ptr, code, P, N, ld, on = _replica_rows("G", G, N)
+    if norm is None:
+        norm = _new((P,), _F32, G, stream)
+    if clip is None:
+        clip = _new((P,), _F32, G, stream)
+    keep, ws, nbytes = _scratch(easgd_grad_norms_workspace_bytes(P, N), workspace, G, stream)
+    _check(_lib.easgd_grad_norms(ptr, code, P, N, ld, max_norm, _given("norm", norm, _F32, (P,), on), _given("clip", clip, _F32, (P,), on),
+                                 ws, nbytes, _stream(stream)))
+    return norm, clip
+
+
+ADAMW_BLOCK = 256                   # parameters that share the scales of their moments in 8 bits
+
+
+def adamw_round(W, M, S, G, step, eta, Wc=None, rho: float = 0.0, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                decay: float = 0.01, tensors=None, clip=None, M_scale=None, S_scale=None, seed: int = 0, N: Optional[int] = None, stream=None) -> None:
+    """An AdamW step of all replicas, in place on W[P][ld], M, S (and Wc[N]): with a center the elastic exchange (Eq. (1) with AdamW's
+    move in the place of the gradient, Eq. (2)), without one every worker's own step.
+
+    G[P][ld] is fp32, bf16 or fp16.  tensors = (ends int64, rates fp32, decays fp32), all [n] on the GPU, gives the tensors of a replica their own rate
+    and decay.  clip [P] fp32 scales every worker's gradient (0: the worker sits the step out).  step is a whole number from 1 on, or a tensor [1] int64,
+    eta a number or a tensor [1] fp32, read when the kernel runs (for captured calls).  M of torch.float8_e4m3fn and S of torch.float8_e5m2
+    select moments in 8 bits, with M_scale and S_scale [P][ceil(N/256)] fp32 and a seed for their random rounding."""
+    wptr, _, P, N, ld, on = _replica_rows("W", W, N)
+    if W.dtype != _F32:
+        raise TypeError(f"W must be torch.float32, got {W.dtype}")
+    gptr, code, *_ = _replica_rows("G", G, N)
+    shape = (P, ld)
+    if G.shape != shape:
+        raise ValueError(f"G must be {list(shape)}, got {list(G.shape)}")
+    eight = M.dtype == torch.float8_e4m3fn
+    mptr = _given("M", M, torch.float8_e4m3fn if eight else _F32, shape, on)
+    sptr = _given("S", S, torch.float8_e5m2 if eight else _F32, shape, on)
+    n, ends, rates, decays = 0, None, None, None
+    if tensors is not None:
+        ends, rates, decays = tensors
+        n = ends.numel()
+        ends, rates, decays = _given("ends", ends, torch.int64, (n,), on), _given("rates", rates, _F32, (n,), on), _given("decays", decays, _F32, (n,), on)
+    step_at = eta_at = None
+    if isinstance(step, torch.Tensor):
+        step, step_at = 1, _given("step", step, torch.int64, (1,), on)
+    if isinstance(eta, torch.Tensor):
+        eta, eta_at = 0.0, _given("eta", eta, _F32, (1,), on)
+    center = _given("Wc", Wc, _F32, (N,), on)
+    clip = _given("clip", clip, _F32, (P,), on)
+    if eight:
+        blocks = (P, (N + ADAMW_BLOCK - 1) // ADAMW_BLOCK)
+        if M_scale is None or S_scale is None:
+            raise ValueError("moments in 8 bits need M_scale and S_scale")
+        _check(_lib.adamw_round_8bit(wptr, mptr, sptr, _given("M_scale", M_scale, _F32, blocks, on), _given("S_scale", S_scale, _F32, blocks, on), gptr, code,
+                                     center, P, N, ld, ends, rates, decays, n, clip, eta, eta_at, rho, beta1, beta2, eps, decay, step, step_at,
+                                     seed & 0xFFFFFFFF, _stream(stream)))
+        return
+    if M_scale is not None or S_scale is not None:
+        raise ValueError("M_scale and S_scale belong to moments in 8 bits")
+    _check(_lib.adamw_round(wptr, mptr, sptr, gptr, code, center, P, N, ld, ends, rates, decays, n, clip, eta, eta_at, rho, beta1, beta2, eps, decay,
+                            step, step_at, _stream(stream)))
 
 
 def stream_copy(dst, src, stream=None) -> None:

@@ -7,6 +7,7 @@
 // so a row is read for its maximum and its sums, and once more for its gradient.  Bound: HBM (each logit once in, each
 // gradient once out), with the vector ALUs close behind (an exponential takes four issue slots, and either pass has one).
 #include "distill.h"
+#include "logits_grad.h"
 #include "row_sums.h"
 
 namespace easgd {
@@ -287,46 +288,6 @@ template <int VEC> struct Slope {
     }
 };
 
-// The rows of the gradient, which may start at another alignment than the logits': whole slots where both agree (the
-// usual case: SAME), else element by element.
-template <int DT> struct GradRow {
-    using Type = LogitType<DT>;
-    static constexpr int VEC = Type::VEC;
-    typename Type::Stored *row;         // element 0
-    int shift, V;
-    bool same;
-    __device__ __forceinline__ GradRow(const DistillArgs &a, size_t r, const Row<DT> &in)
-    {
-        const Row<DT> out(a.dlogits, r, a.dld, a.V);
-        row = out.base + out.shift;
-        same = out.shift == in.shift;
-        shift = in.shift;
-        V = a.V;
-    }
-    // the gradient of slot s of the logits' grid
-    __device__ __forceinline__ void store(int s, const float (&x)[VEC], bool full) const
-    {
-        const int j = s * VEC - shift;
-        if (same && full) {
-            typedef unsigned Four __attribute__((ext_vector_type(4)));
-            const uint4 p = Type::pack(x);
-            const Four v = {p.x, p.y, p.z, p.w};
-            __builtin_nontemporal_store(v, reinterpret_cast<Four *>(row + j));
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < VEC; ++i)
-            if ((unsigned)(j + i) < (unsigned)V) row[j + i] = Type::narrow(x[i]);
-    }
-    __device__ __forceinline__ void put(int j, float d) const { row[j] = Type::narrow(d); }
-    // 0 for slots first + thread, first + thread + block, ... below last
-    __device__ __forceinline__ void clear(int last, int block, int first = 0) const
-    {
-        const float zero[VEC] = {};
-        for (int s = first + threadIdx.x; s < last; s += block) store(s, zero, s * VEC >= shift && (s + 1) * VEC <= shift + V);
-    }
-};
-
 // The gradient of slots [s0, s1) where Slope asks for the careful way.
 template <int DT, int BLOCK>
 __device__ __forceinline__ void put_apart(const Row<DT> &row, const GradRow<DT> &out, const Slope<Row<DT>::VEC> &g, const Scales &q, int s0, int s1)
@@ -476,7 +437,7 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
     if constexpr (TAIL)
         if (!padding && outside_far(sums, lds.rest)) outside = outside_of<DT, BLOCK>(row, place, q, in_top, (row.slots * VEC + 31) / 32, lds.fpart);
     if constexpr (GRAD) {
-        const GradRow<DT> out(a, r, row);
+        const GradRow<DT> out(a.dlogits, a.dld, a.V, r, row);
         const Slope<VEC> g(a, r, lds, padding, sums, outside, q);
         auto put = [&](const uint4 &raw, int s, bool full) {
             float x[VEC];
@@ -631,7 +592,7 @@ __global__ __launch_bounds__(BLOCK) void distill_grad_kernel(DistillArgs a)
         if (!padding && outside_far(sums, lds.rest)) outside = outside_of<DT, BLOCK>(row, place, q, bits, OUTSIDE_WORDS, lds.fpart);
     }
     const Slope<VEC> g(a, r, lds, padding, sums, outside, q);
-    const GradRow<DT> out(a, r, row);
+    const GradRow<DT> out(a.dlogits, a.dld, a.V, r, row);
     auto put = [&](const uint4 &raw, int s) {
         float x[VEC];
         Type::unpack(raw, x);
@@ -927,24 +888,9 @@ static int check_distill(const DistillCall &q, int mode)
     if (!aligned_to(a.loss, 4) || !aligned_to(a.dloss, 4)) return fail(EASGD_EINVAL, "%s: loss, dloss must be 4-byte aligned", q.name);
     if (!aligned16(a.state)) return fail(EASGD_EINVAL, "%s: state must be 16-byte aligned", q.name);
     if (mode & DISTILL_GRAD) {
-        if (!std::isfinite(a.scale)) return fail(EASGD_EINVAL, "%s: scale must be finite", q.name);
-        if (a.dld < (size_t)a.V) return fail(EASGD_EINVAL, "%s: dld (%zu) < V (%d)", q.name, a.dld, a.V);
-        if (q.rows > 1 && a.dld > ((size_t)1 << 60) / q.rows) return fail(EASGD_ERANGE, "%s: rows * dld too large", q.name);
-        if (!aligned_to(a.dlogits, dtype_bytes(q.dtype))) return fail(EASGD_EINVAL, "%s: dlogits must be aligned to its elements (%zu bytes)", q.name, dtype_bytes(q.dtype));
+        if (int rc = check_gradient(q.name, a.dlogits, q.dtype, q.rows, a.V, a.dld, a.scale)) return rc;
     }
     return EASGD_OK;
-}
-
-// Whether a row of logits and one of dlogits share memory: blocks read a row, or parts of others, while they store.  Rows that
-// alternate (the two halves of wider rows, say) share none; at two strides the whole ranges have to be apart.
-static bool rows_overlap(const DistillArgs &a, size_t rows, size_t size)
-{
-    const uintptr_t in = reinterpret_cast<uintptr_t>(a.logits), out = reinterpret_cast<uintptr_t>(a.dlogits);
-    const size_t row = (size_t)a.V * size;
-    if (in + (rows - 1) * a.ld * size + row <= out || out + (rows - 1) * a.dld * size + row <= in) return false;
-    if (rows == 1 || a.ld != a.dld) return true;
-    const size_t pitch = a.ld * size, apart = in < out ? (out - in) % pitch : (in - out) % pitch;
-    return apart < row || pitch - apart < row;
 }
 
 // Into how many parts rows are cut: enough blocks to fill the chip, and at least 1024 slots (four per thread) a part.
@@ -1048,7 +994,7 @@ template <int MODE> static int launch_distill(const DistillCall &q, void *stream
         const size_t need = easgd_distill_workspace_bytes(q.rows, a.V, a.k);
         if (int rc = check_workspace(q.name, q.workspace, q.workspace_bytes, need)) return rc;
     }
-    if ((MODE & DISTILL_GRAD) && q.rows && rows_overlap(a, q.rows, dtype_bytes(q.dtype))) return fail(EASGD_EINVAL, "%s: dlogits must not overlap logits", q.name);
+    if ((MODE & DISTILL_GRAD) && q.rows && rows_overlap(a.logits, a.ld, a.dlogits, a.dld, a.V, q.rows, dtype_bytes(q.dtype))) return fail(EASGD_EINVAL, "%s: dlogits must not overlap logits", q.name);
     clear_error();
     if (q.rows == 0) return EASGD_OK;
     const hipStream_t s = static_cast<hipStream_t>(stream);

@@ -318,4 +318,72 @@ __device__ __forceinline__ unsigned first_of(const Row<DT> &row, int s0, int s1,
     return min(n, k);
 }
 
+// The order words of the first k elements of a row that a wavefront holds, element lane + 64 q in x[q] (-inf behind the row's end),
+// into words, in no order; returns how many there are.  The k-th largest key is found bit by bit with votes; equal keys are taken by
+// ascending index, which is the order of registers, then lanes.
+template <int NQ> __device__ __forceinline__ unsigned short_first(const float (&x)[NQ], unsigned k, unsigned long long *words)
+{
+    unsigned key[NQ], there = 0;
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        key[q] = logit_key(x[q]);
+        there += __popcll(__ballot(key[q] != 0));
+    }
+    k = min(k, there);
+    unsigned least = 1, above = there;                  // `above` keys are >= least
+    if (there > k) {
+        least = 0;
+        for (unsigned bit = 0x80000000u; bit && above != k; bit >>= 1) {
+            const unsigned next = least | bit;
+            unsigned n = 0;
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) n += __popcll(__ballot(key[q] >= next));
+            if (n >= k) {
+                least = next;
+                above = n;
+            }
+        }
+    }
+    // keys above `least`, then as many equal ones as are wanted
+    unsigned equal_left = k;
+    if (above != k) {
+        unsigned n = 0;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) n += __popcll(__ballot(key[q] > least));
+        equal_left = k - n;
+    }
+    unsigned n = 0;
+    const int lane = threadIdx.x & 63;
+    const unsigned long long below = (1ull << lane) - 1;
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        const unsigned long long equal = __ballot(key[q] == least && key[q] != 0);
+        const bool take = key[q] > least || (key[q] == least && key[q] != 0 && (unsigned)__popcll(equal & below) < equal_left);
+        equal_left -= min(equal_left, (unsigned)__popcll(equal));
+        const unsigned long long taken = __ballot(take);
+        if (take) words[n + __popcll(taken & below)] = order_word(key[q], lane + 64 * q);
+        n += __popcll(taken);
+    }
+    return n;
+}
+
+// ---- launch shapes of the kernels that take the first k ----
+// Few long rows are cut into parts, so that there are blocks for the whole chip: each part's first k go through the workspace.
+// Many rows take blocks of 256 threads, five of which a compute unit holds (2048 x 131072 bf16, k = 64: 168 us against 180 with 512);
+// few rows, and more than 64 tokens (whose first floor wants many maxima), 512 (8 x 50001: 15.8 us against 18.5 with 256).  The change at
+// 256 rows suits a thousand rows and more better than some hundred, which leave a compute unit one to three blocks (us; 512 threads: k = 128):
+//   rows of 131072 bf16     255 (four parts each)   256    512    768    1024   2048
+//   256 threads, k = 64     49 (512 threads)        65     71     77     88     166
+//   512 threads, k = 128    65                      46     56     88     106    204
+static constexpr int TOP_BLOCK = 512, TOP_SHORT_V = 1024;
+static constexpr int TOP_SPLIT_ROWS = 256, TOP_SPLIT_SLOTS = 2048;
+static inline int top_segments(size_t rows, int slots, int k)
+{
+    if (rows >= TOP_SPLIT_ROWS || slots < 2 * TOP_SPLIT_SLOTS) return 1;
+    int n = (int)((512 + rows - 1) / rows);
+    if (n > slots / TOP_SPLIT_SLOTS) n = slots / TOP_SPLIT_SLOTS;
+    if (n > TOP_LIST / k) n = TOP_LIST / k;
+    return n < 1 ? 1 : n;
+}
+
 }  // namespace easgd

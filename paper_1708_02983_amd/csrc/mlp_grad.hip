@@ -23,6 +23,7 @@
 #include "gemm_chain.h"
 #include "gemm_split.h"
 #include "distill.h"
+#include "score.h"
 #include "shared_launches.h"
 #include "mlp_head.h"
 #include "persistent_round.h"
@@ -621,7 +622,8 @@ struct ElasticStep {
 
 static int grad_impl(const char *name, const int *dims, int n_layers, const float *W, size_t ld, const float *X,
                      const int32_t *y, int P, int b, float *G, float *loss, void *workspace, size_t workspace_bytes,
-                     void *stream, const ElasticStep *step, unsigned short *G16 = nullptr, const TeacherGiven *teacher = nullptr);
+                     void *stream, const ElasticStep *step, unsigned short *G16 = nullptr, const TeacherGiven *teacher = nullptr,
+                     const TokensGiven *given = nullptr);
 
 // A second stream per device (default priority) with the two events that order it against the caller's
 // stream: `fork` is recorded on the caller's stream when the round starts, `join` on the second stream when
@@ -744,6 +746,17 @@ int easgd_grad_distill(const int *dims, int n_layers, const float *W, size_t ld,
                             stream, nullptr, nullptr, &teacher);
 }
 
+int easgd_grad_token_loss(const int *dims, int n_layers, const float *W, size_t ld, const float *X, const int32_t *tokens, const float *weight,
+                          int P, int b, float bonus, float temperature, float *G, float *loss, float *logprob, float *entropy,
+                          void *workspace, size_t workspace_bytes, void *stream)
+{
+    static_assert(easgd::MAX_CLASSES <= easgd::SCORE_SHORT_V, "every network's logits are short rows");
+    const easgd::TokensGiven given = {tokens, weight, bonus, temperature, logprob, entropy};
+    if (int rc = easgd::check_tokens("easgd_grad_token_loss", given, true)) return rc;
+    return easgd::grad_impl("easgd_grad_token_loss", dims, n_layers, W, ld, X, tokens, P, b, G, loss, workspace, workspace_bytes,
+                            stream, nullptr, nullptr, nullptr, &given);
+}
+
 int easgd_mlp_round(const int *dims, int n_layers, float *W, float *V, float *Wc, size_t ld,
                     const float *X, const int32_t *y, int P, int b, float *G, float *loss,
                     float eta, float rho, float delta, void *workspace, size_t workspace_bytes, void *stream)
@@ -771,11 +784,11 @@ namespace easgd {
 
 static int grad_impl(const char *name, const int *dims, int n_layers, const float *W, size_t ld, const float *X,
                      const int32_t *y, int P, int b, float *G, float *loss, void *workspace, size_t workspace_bytes,
-                     void *stream, const ElasticStep *step, unsigned short *G16, const TeacherGiven *teacher)
+                     void *stream, const ElasticStep *step, unsigned short *G16, const TeacherGiven *teacher, const TokensGiven *given)
 {
     const int L = n_layers;
     GradPlan pl;
-    if (!W || !X || (!y && !teacher) || (!G && !G16 && !step)) return fail(EASGD_EINVAL, "%s: NULL pointer", name);
+    if (!W || !X || (!y && !teacher && !given) || (!G && !G16 && !step)) return fail(EASGD_EINVAL, "%s: NULL pointer", name);
     if (!make_plan(dims, L, P, b, pl))
         return fail(EASGD_EINVAL, "%s: need 1 <= n_layers <= %d, all dims >= 1, P >= 1, b >= 1", name, MAX_LAYERS);
     if (dims[L] > MAX_CLASSES) return fail(EASGD_EINVAL, "%s: at most %d classes, got %d", name, MAX_CLASSES, dims[L]);
@@ -809,7 +822,7 @@ static int grad_impl(const char *name, const int *dims, int n_layers, const floa
     const Form by_size = fp32 ? FORM_FP32 : FORM_BY_SIZE;
 
     // a narrow last layer goes through mlp_head_kernel together with the softmax and its own input gradient
-    const bool head = !teacher && options().mlp_head != 0 && head_fits(dims, L);
+    const bool head = !teacher && !given && options().mlp_head != 0 && head_fits(dims, L);
     if (head && (size_t)P * ((b + HEAD_ROWS - 1) / HEAD_ROWS) > 0x3fffffffull) return fail(EASGD_ERANGE, "%s: P*b too large", name);
 
     // ---- a single-layer network small enough to be bound by launch boundaries: the whole call in one launch ----
@@ -914,6 +927,8 @@ static int grad_impl(const char *name, const int *dims, int n_layers, const floa
         launch_head(h, s);
     } else if (teacher) {
         distill_logits(logits, pl.splits, (size_t)rows * dims[L], (size_t)rows, dims[L], *teacher, 1.f / (float)b, row_loss, dz[(L - 1) % 3], stream);
+    } else if (given) {
+        score_logits(logits, pl.splits, (size_t)rows * dims[L], (size_t)rows, dims[L], *given, 1.f / (float)b, row_loss, dz[(L - 1) % 3], stream);
     } else {
         EASGD_LAUNCH(softmax_xent_kernel, dim3((rows + 3) / 4), dim3(256), 0, s, logits, y, dz[(L - 1) % 3], row_loss,
                            rows, b, dims[L], pl.splits, (size_t)rows * dims[L]);

@@ -1,0 +1,753 @@
+// Tokens that are given: their log probabilities, the rows' entropies, ranks and first alternatives, and the gradients of all that.
+//
+// Per row (see include/easgd.h for the definition): with a reference m near the largest logit, y_j = (z_j - m) log2(e) / T and
+// e_j = 2^y_j,
+//   s = sum e_j, u = sum e_j y_j:  logprob = (z_t - m)/T - ln s,  entropy H = ln s - ln2 u / s  (the same for any m),
+//   d/dz_j of gl logprob + gh H  =  e_j (A + B y_j) + [j = t] gl / T  with  A = (-gl - gh (H - ln s)) / (s T), B = -gh ln2 / (s T),
+// so sums and gradients are one pass each, with one exponential and a few fused multiply-adds a logit.  Bound: HBM for many long rows
+// (each logit once in, each gradient once out), latency for few or short ones.
+#include "score.h"
+#include "logits_grad.h"
+#include "logits_select.h"
+#include "row_sums.h"
+
+namespace easgd {
+
+struct ScoreArgs {
+    const void *logits;
+    size_t ld, rows;
+    int V;
+    const int *tokens;
+    float temperature;
+    float *logprob, *entropy;
+    int *rank;
+    int k;
+    float *top_logprob;
+    int *top_indices;
+    float4 *state;
+    const float *weight;           // easgd_token_loss: the loss is -weight logprob - bonus H
+    float bonus;
+    float *loss;
+    const float *dlogprob, *dentropy;
+    float scale;
+    void *dlogits;
+    size_t dld;
+    int parts;                     // logits are the sum of this many matrices (fp32, short rows)
+    size_t part_stride;
+    int segments, seg_slots;       // slots of a part of a row
+    float4 *partial;               // [rows][segments]: (m, s, u, logits before the token) of a part of a row
+    unsigned long long *words;     // [rows][segments][k]: the first k of every part (0: none left)
+};
+
+static constexpr double LN2_64 = 0.69314718055994530942;
+// the exponent that stands for any smaller one in e_j y_j, where e_j is 0: a masked place must not make it 0 times infinity
+static constexpr float LEAST = -256.f;
+
+// ---- sums ----------------------------------------------------------------------------------------------------------------
+// Running sums of a thread relative to a reference that its wavefront shares (Reference in row_sums.h): the largest logit of the
+// first slots that hold any, moved when a slot's exponentials sum up to more than 2^12, so that the usual slot needs neither a
+// maximum nor a rescaling.  u is then off by at most 12 units of rounding of s, which the entropy divides by s.
+template <int VEC, bool ENTROPY> struct TokenSums {
+    const Scales &q;
+    Reference<VEC> at;
+    float s = 0.f, u = 0.f;
+
+    __device__ __forceinline__ explicit TokenSums(const Scales &q) : q(q), at(q) {}
+    // whole wavefronts call it (lanes without a slot with an empty one)
+    __device__ __forceinline__ void add(const float (&x)[VEC])
+    {
+        float sum = 0.f, more = 0.f;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const float y = fmaf(x[i], at.c, -at.rc), e = exp2_fast(y);
+            sum += e;
+            if constexpr (ENTROPY) more = fmaf(e, y, more);
+        }
+        // NaN in either: a masked place, among others
+        const bool fine = at.ref > -INFINITY && sum <= 0x1p12f && (!ENTROPY || more <= 0x1p30f);
+        if (__any(!fine)) careful(x, sum, more);        // uniform for the wavefront
+        s += sum;
+        if constexpr (ENTROPY) u += more;
+    }
+    // a slot whose sums are not as they should be: the first one, a logit far above the reference, masked places, NaN, large logits
+    __device__ __forceinline__ void careful(const float (&x)[VEC], float &sum, float &more)
+    {
+        float t = x[0];
+        bool odd = isnan(x[0]);
+#pragma unroll
+        for (int i = 1; i < VEC; ++i) {
+            t = fmaxf(t, x[i]);
+            odd = odd || isnan(x[i]);
+        }
+        t = uniform(wave_max(t));
+        if (t > at.ref && (at.ref == -INFINITY || __any(!(sum <= 0x1p12f)))) {
+            const Reference<VEC> old = at;
+            at.set(t, q);
+            if (old.ref > -INFINITY) {                  // what the exponents of before are now
+                const float up = fmaxf((old.ref - at.ref) * q.c - old.lost + at.lost, -1e4f), f = exp2_fast(up);
+                if constexpr (ENTROPY) u = f * fmaf(up, s, u);
+                s *= f;
+            }
+        }
+        sum = odd ? NAN : 0.f;
+        more = 0.f;
+        if (at.ref == -INFINITY) return;                // masked places only, so far
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const float y = at.by_difference() ? (x[i] - at.ref) * q.c : fmaf(x[i], at.c, -at.rc), e = exp2_fast(y);
+            sum += e;
+            if constexpr (ENTROPY) more = fmaf(e, fmaxf(y, LEAST), more);
+        }
+    }
+    // sums (m, s, u, 0) of a wavefront, without what rounding rc added to the exponents
+    __device__ __forceinline__ float4 of_wave() const
+    {
+        const float f = exp2_fast(-at.lost), ws = wave_sum(s), wu = ENTROPY ? wave_sum(u) : 0.f;
+        return make_float4(at.ref, ws * f, ENTROPY ? f * fmaf(-at.lost, ws, wu) : 0.f, 0.f);
+    }
+};
+
+// a part's sums, relative to its own reference, as they are relative to m, which is at least as large
+__device__ __forceinline__ float4 rebased(const float4 &p, float m, const Scales &q)
+{
+    const float up = p.x == m || p.x == -INFINITY ? 0.f : fmaxf((p.x - m) * q.c, -1e4f), f = exp2_fast(up);
+    return make_float4(m, p.y * f, f * fmaf(up, p.y, p.z), p.w);
+}
+
+// ---- ranks -----------------------------------------------------------------------------------------------------------------
+// How many logits of the row come before the token in its order: z > z_t, or z == z_t at a lower index.  Slots before the
+// token's compare with z >= z_t, slots behind it with z >= the next larger number, and the token's own slot looks closely.
+struct RankCount {
+    float z, from;             // of the token; the next larger number
+    int slot, index;           // of the token
+    unsigned n = 0;            // uniform for the wavefront
+    template <int DT> __device__ __forceinline__ void set(const Row<DT> &row, int token)
+    {
+        slot = (token + row.shift) / Row<DT>::VEC;
+        index = token;
+        z = row.load_one(token);
+        if (!(z > -INFINITY)) z = from = -FLT_MAX;      // a masked token: behind all that are not
+        else if (z == INFINITY) from = NAN;
+        else {
+            const unsigned b = __float_as_uint(z + 0.f);
+            from = z == 0.f ? __uint_as_float(1u) : __uint_as_float(b & 0x80000000u ? b - 1 : b + 1);
+        }
+    }
+    template <int DT> __device__ __forceinline__ void add(const Row<DT> &row, const float (&x)[Row<DT>::VEC], int s)
+    {
+        const float least = s < slot ? z : from;
+        if (__any(s == slot)) {
+#pragma unroll
+            for (int i = 0; i < Row<DT>::VEC; ++i) n += __popcll(__ballot(x[i] >= (s == slot && row.index(s, i) < index ? z : least)));
+        } else {
+#pragma unroll
+            for (int i = 0; i < Row<DT>::VEC; ++i) n += __popcll(__ballot(x[i] >= least));
+        }
+    }
+};
+
+// ---- results of a row ------------------------------------------------------------------------------------------------------
+// What the sums of a row say: ln s and the entropy.
+struct RowScore {
+    double log_s, entropy;
+    bool none;                 // every logit masked
+    __device__ __forceinline__ explicit RowScore(const float4 &w)
+    {
+        none = w.y == 0.f;
+        log_s = none ? 0.0 : log((double)w.y);
+        const double h = log_s - LN2_64 * (double)w.z / (double)w.y;
+        entropy = none || h < 0.0 ? 0.0 : h;
+    }
+};
+__device__ __forceinline__ double log_probability(const RowScore &row, float m, float z, float temperature)
+{
+    return row.none ? -(double)INFINITY : ((double)z - (double)m) / (double)temperature - row.log_s;
+}
+// One thread.  token: whether the row has one.
+__device__ __forceinline__ void write_score(const ScoreArgs &a, size_t r, bool padding, bool token, const float4 &w, float z_token, unsigned before)
+{
+    const RowScore row(w);
+    const double lp = token ? log_probability(row, w.x, z_token, a.temperature) : 0.0;
+    if (a.logprob) a.logprob[r] = padding ? 0.f : (float)lp;
+    if (a.entropy) a.entropy[r] = padding ? 0.f : (float)row.entropy;
+    if (a.rank) a.rank[r] = padding ? -1 : (int)before;
+    if (a.state) a.state[r] = padding ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(w.x, w.y, (float)row.entropy, 0.f);
+    if (a.loss) {
+        const float weight = a.weight ? a.weight[r] : 1.f;
+        double loss = weight != 0.f ? -(double)weight * lp : 0.0;
+        if (a.bonus != 0.f) loss -= (double)a.bonus * row.entropy;
+        if (isnan(w.y)) loss = NAN;
+        a.loss[r] = padding || row.none ? 0.f : (float)loss;
+    }
+}
+// an alternative from its order word (0: none left)
+__device__ __forceinline__ void write_alternative(const ScoreArgs &a, size_t r, unsigned at, unsigned long long word, const RowScore &row, float m)
+{
+    a.top_logprob[r * a.k + at] = word ? (float)log_probability(row, m, key_logit((unsigned)(word >> 32)), a.temperature) : -INFINITY;
+    a.top_indices[r * a.k + at] = word ? (int)~(unsigned)word : -1;
+}
+__device__ __forceinline__ bool padded(const ScoreArgs &a, int token) { return a.tokens && (unsigned)token >= (unsigned)a.V; }
+template <int BLOCK> __device__ __forceinline__ void write_padding(const ScoreArgs &a, size_t r)
+{
+    if (threadIdx.x == 0) write_score(a, r, true, false, make_float4(0.f, 0.f, 0.f, 0.f), 0.f, 0);
+    for (int i = threadIdx.x; i < a.k; i += BLOCK) write_alternative(a, r, i, 0, RowScore(make_float4(0.f, 0.f, 0.f, 0.f)), 0.f);
+}
+
+// ---- sums of rows, or of parts of rows, a block each --------------------------------------------------------------------------
+// Every slot of [s0, s1) through whole wavefronts, DEEP loads ahead: f(raw, slot), an empty slot where a lane has none.
+template <int DT, int BLOCK, int DEEP, typename F> __device__ __forceinline__ void walk(const Row<DT> &row, int s0, int s1, F f)
+{
+    uint4 v[DEEP];
+    int s = s0 + (int)threadIdx.x;
+    const int lead = s0 + (int)__builtin_amdgcn_readfirstlane(threadIdx.x & ~63);
+#pragma unroll
+    for (int i = 0; i < DEEP; ++i) v[i] = row.load_wave(s + i * BLOCK, s1);
+    for (int first = lead; first < s1; first += DEEP * BLOCK, s += DEEP * BLOCK) {
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) {
+            if (first + i * BLOCK >= s1) break;         // uniform: the whole wavefront is behind the end
+            f(v[i], s + i * BLOCK);
+            if (first + (DEEP + i) * BLOCK < s1) v[i] = row.load_wave(s + (DEEP + i) * BLOCK, s1);
+        }
+    }
+}
+
+template <int BLOCK> struct JoinLds {
+    float4 part[BLOCK / 64];
+    unsigned before[BLOCK / 64];
+};
+// the sums of a block's wavefronts and its count, for every thread
+template <int BLOCK, typename S> __device__ __forceinline__ float4 block_sums(const S &sums, unsigned before, JoinLds<BLOCK> &lds, const Scales &q)
+{
+    constexpr int WAVES = BLOCK / 64;
+    float4 w = sums.of_wave();
+    if ((threadIdx.x & 63) == 0) {
+        w.w = __uint_as_float(before);
+        lds.part[threadIdx.x >> 6] = w;
+    }
+    __syncthreads();
+    w = lds.part[threadIdx.x & (WAVES - 1)];
+    unsigned n = __float_as_uint(w.w);
+    float m = w.x;
+#pragma unroll
+    for (int o = WAVES / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    w = rebased(w, m, q);
+#pragma unroll
+    for (int o = WAVES / 2; o > 0; o >>= 1) {
+        w.y += __shfl_xor(w.y, o);
+        w.z += __shfl_xor(w.z, o);
+        n += __shfl_xor(n, o);
+    }
+    w.w = __uint_as_float(n);
+    return w;
+}
+
+template <int DT, int BLOCK, bool ENTROPY, bool RANK>
+__global__ __launch_bounds__(BLOCK) void score_rows_kernel(ScoreArgs a)
+{
+    constexpr int VEC = Row<DT>::VEC;
+    __shared__ JoinLds<BLOCK> lds;
+    const size_t r = blockIdx.x / a.segments;
+    const int seg = blockIdx.x % a.segments;
+    const Row<DT> row(a.logits, r, a.ld, a.V);
+    const int token = a.tokens ? a.tokens[r] : 0;
+    if (padded(a, token)) {
+        if (a.segments == 1) write_padding<BLOCK>(a, r);
+        return;
+    }
+    const Scales q(a.temperature);
+    const int s0 = seg * a.seg_slots, s1 = min(s0 + a.seg_slots, row.slots);
+    TokenSums<VEC, ENTROPY> sums(q);
+    RankCount rank;
+    if constexpr (RANK) rank.set(row, token);
+    walk<DT, BLOCK, 8>(row, s0, s1, [&](const uint4 &raw, int s) {
+        float x[VEC];
+        Row<DT>::Type::unpack(raw, x);
+        sums.add(x);
+        if constexpr (RANK) rank.add(row, x, s);
+    });
+    const float4 w = block_sums<BLOCK>(sums, RANK ? rank.n : 0u, lds, q);
+    if (threadIdx.x != 0) return;
+    if (a.segments > 1) a.partial[blockIdx.x] = w;
+    else write_score(a, r, false, a.tokens, w, a.tokens ? row.load_one(token) : 0.f, __float_as_uint(w.w));
+}
+
+// the same with the first k
+template <int DT, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void score_top_kernel(ScoreArgs a)
+{
+    constexpr int VEC = Row<DT>::VEC;
+    __shared__ TopLds top;
+    __shared__ JoinLds<BLOCK> lds;
+    const size_t r = blockIdx.x / a.segments;
+    const int seg = blockIdx.x % a.segments;
+    const Row<DT> row(a.logits, r, a.ld, a.V);
+    const int token = a.tokens ? a.tokens[r] : 0;
+    if (padded(a, token)) {
+        if (a.segments == 1) write_padding<BLOCK>(a, r);
+        return;
+    }
+    const Scales q(a.temperature);
+    const int s0 = seg * a.seg_slots, s1 = min(s0 + a.seg_slots, row.slots);
+    TokenSums<VEC, true> sums(q);
+    RankCount rank;
+    rank.set(row, token);
+    const unsigned n = first_of<DT, BLOCK>(row, s0, s1, (unsigned)a.k, top, [&](const float (&x)[VEC], int s) {
+        sums.add(x);
+        rank.add(row, x, s);
+    });
+    const float4 w = block_sums<BLOCK>(sums, rank.n, lds, q);
+    const unsigned i = threadIdx.x;
+    if (a.segments > 1) {
+        if (i == 0) a.partial[blockIdx.x] = w;
+        if (i < (unsigned)a.k) a.words[(size_t)blockIdx.x * a.k + i] = i < n ? top.list[i] : 0;
+        return;
+    }
+    if (i == 0) write_score(a, r, false, a.tokens, w, a.tokens ? row.load_one(token) : 0.f, __float_as_uint(w.w));
+    if (i < (unsigned)a.k) write_alternative(a, r, i, i < n ? top.list[i] : 0, RowScore(w), w.x);
+}
+
+// ---- the parts of a row together ------------------------------------------------------------------------------------------------
+// the sums of a row's parts, a part per lane (and every 64th after it), in a fixed order, for every lane of a wavefront
+__device__ __forceinline__ float4 join_parts(const ScoreArgs &a, size_t r, const Scales &q)
+{
+    const int lane = threadIdx.x & 63;
+    float m = -INFINITY;
+    for (int i = lane; i < a.segments; i += 64) m = fmaxf(m, a.partial[r * a.segments + i].x);
+    m = wave_max(m);
+    float s = 0.f, u = 0.f;
+    unsigned before = 0;
+    for (int i = lane; i < a.segments; i += 64) {
+        const float4 p = a.partial[r * a.segments + i], w = rebased(p, m, q);
+        s += w.y;
+        u += w.z;
+        before += __float_as_uint(p.w);
+    }
+    return make_float4(m, wave_sum(s), wave_sum(u), __uint_as_float(wave_sum(before)));
+}
+
+template <int DT>
+__global__ __launch_bounds__(64) void score_join_kernel(ScoreArgs a)
+{
+    const size_t r = blockIdx.x;
+    const Row<DT> row(a.logits, r, a.ld, a.V);
+    const int token = a.tokens ? a.tokens[r] : 0;
+    if (padded(a, token)) {
+        write_padding<64>(a, r);
+        return;
+    }
+    const float z_token = a.tokens ? row.load_one(token) : 0.f;
+    const float4 w = join_parts(a, r, Scales(a.temperature));
+    if (threadIdx.x == 0) write_score(a, r, false, a.tokens, w, z_token, __float_as_uint(w.w));
+}
+
+template <int DT, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void score_top_join_kernel(ScoreArgs a)
+{
+    __shared__ TopLds top;
+    __shared__ float4 sums;
+    const size_t r = blockIdx.x;
+    const Row<DT> row(a.logits, r, a.ld, a.V);
+    const int token = a.tokens ? a.tokens[r] : 0;
+    if (padded(a, token)) {
+        write_padding<BLOCK>(a, r);
+        return;
+    }
+    const unsigned all = (unsigned)(a.segments * a.k);             // <= TOP_LIST
+    if (threadIdx.x < 64) {
+        const float4 w = join_parts(a, r, Scales(a.temperature));
+        if (threadIdx.x == 0) {
+            sums = w;
+            write_score(a, r, false, a.tokens, w, a.tokens ? row.load_one(token) : 0.f, __float_as_uint(w.w));
+        }
+    }
+    if (threadIdx.x == 0) top.n = all;
+    for (unsigned i = threadIdx.x; i < all; i += BLOCK) top.list[i] = a.words[r * all + i];
+    __syncthreads();
+    unsigned n = keep_from<BLOCK>(top, all, FIRST_WORD);           // the words that are there
+    if (n > 512) n = keep_from<BLOCK>(top, n, select_nth<BLOCK>(EachListed{top.list, n, BLOCK}, FIRST_WORD, a.k, top.select));
+    rank_list<BLOCK>(top, n, a.k);
+    const unsigned i = threadIdx.x;
+    if (i < (unsigned)a.k) write_alternative(a, r, i, i < n ? top.list[i] : 0, RowScore(sums), sums.x);
+}
+
+// ---- gradients -----------------------------------------------------------------------------------------------------------------
+// The gradient of a row from its reference, sum and entropy, as a function of the logit.
+template <int VEC> struct TokenSlope {
+    Reference<VEC> at;
+    float a, b, of_token;
+    bool none;                 // nothing to learn: the gradient is 0
+    // differences: of() is not called; exponents are those of exact differences to m
+    __device__ __forceinline__ TokenSlope(const ScoreArgs &args, size_t r, bool padding, float m, float sum, double entropy, float z_token, const Scales &q,
+                                          bool differences = false)
+        : at(uniform(m), q)
+    {
+        none = padding || sum == 0.f;
+        const double scale = (double)args.scale, T = (double)args.temperature;
+        double gl, gh;
+        if (args.loss) {
+            gl = -scale * (args.weight ? (double)args.weight[r] : 1.0);
+            gh = -scale * (double)args.bonus;
+        } else {
+            gl = args.dlogprob ? scale * (double)args.dlogprob[r] : 0.0;
+            gh = args.dentropy ? scale * (double)args.dentropy[r] : 0.0;
+        }
+        const double log_s = log((double)sum), lost = differences ? 0.0 : (double)at.lost, factor = 1.0 / ((double)sum * T);
+        const float f = differences ? 1.f : exp2_fast(-at.lost);
+        a = uniform((float)((-gl - gh * (entropy - log_s - LN2_64 * lost)) * factor) * f);
+        b = uniform((float)(-gh * LN2_64 * factor) * f);
+        const double log_q = ((double)z_token - (double)m) / T - log_s, p = exp(log_q);
+        of_token = uniform((float)((gl * (1.0 - p) - (p > 0.0 ? gh * p * (log_q + entropy) : 0.0)) / T));
+        if (isnan(sum)) of_token = NAN;
+    }
+    template <bool ENTROPY> __device__ __forceinline__ void of(float (&x)[VEC], const Scales &q) const
+    {
+        if (at.by_difference()) {                       // uniform, and rare
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float y = (x[i] - at.ref) * q.c;
+                x[i] = exp2_fast(y) * fmaf(b, fmaxf(y, LEAST), a);
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const float y = fmaf(x[i], at.c, -at.rc), e = exp2_fast(y);
+            x[i] = ENTROPY ? e * fmaf(b, fmaxf(y, LEAST), a) : e * a;
+        }
+    }
+};
+
+template <int DT, int BLOCK, bool ENTROPY>
+__global__ __launch_bounds__(BLOCK) void score_grad_kernel(ScoreArgs a)
+{
+    constexpr int VEC = Row<DT>::VEC, DEEP = 4;
+    const size_t r = blockIdx.x / a.segments;
+    const int seg = blockIdx.x % a.segments;
+    const Row<DT> row(a.logits, r, a.ld, a.V);
+    const int token = a.tokens ? a.tokens[r] : -1;
+    const bool padding = padded(a, token);
+    const int s0 = seg * a.seg_slots, s1 = min(s0 + a.seg_slots, row.slots);
+    const GradRow<DT> out(a.dlogits, a.dld, a.V, r, row);
+    if (padding) {
+        out.clear(s1, BLOCK, s0);
+        return;
+    }
+    const Scales q(a.temperature);
+    const float4 state = a.state[r];
+    const TokenSlope<VEC> g(a, r, padding, state.x, state.y, (double)state.z, a.tokens ? row.load_one(token) : 0.f, q);
+    if (g.none) {
+        out.clear(s1, BLOCK, s0);
+        return;
+    }
+    const int slot = a.tokens ? (token + row.shift) / VEC : -1;
+    auto put = [&](const uint4 &raw, int s) {
+        float x[VEC];
+        Row<DT>::Type::unpack(raw, x);
+        g.template of<ENTROPY>(x, q);
+        if (s == slot) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) x[i] = row.index(s, i) == token ? g.of_token : x[i];
+        }
+        out.store(s, x, row.full(s));
+    };
+    int s = s0 + (int)threadIdx.x;
+    for (; s - (int)threadIdx.x + DEEP * BLOCK <= s1; s += DEEP * BLOCK) {
+        uint4 v[DEEP];
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) v[i] = row.full(s + i * BLOCK) ? row.load_once(s + i * BLOCK) : row.load(s + i * BLOCK);
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i) put(v[i], s + i * BLOCK);
+    }
+    for (; s < s1; s += BLOCK) put(row.load(s), s);
+}
+
+// ---- short rows: a wavefront each, all calls --------------------------------------------------------------------------------------
+// Rows of at most 64 * NQ logits sit in a wavefront's registers, element lane + 64 i in x[i]; maximum, sums and counts are shuffles and
+// votes, and nothing waits for other wavefronts.  Bound: latency.
+enum { SCORE_SUMS = 1, SCORE_GRAD = 2, SCORE_BOTH = 3 };
+template <int DT, int NQ, int MODE, bool TOP>
+__global__ __launch_bounds__(256) void score_short_kernel(ScoreArgs a)
+{
+    __shared__ unsigned long long all_words[TOP ? 4 : 1][TOP ? LOGITS_MAX_TOP : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const size_t r = (size_t)blockIdx.x * 4 + wave;
+    if (r >= a.rows) return;                            // wavefronts of a block have nothing in common
+    const Row<DT> row(a.logits, r, a.ld, a.V);
+    const Scales q(a.temperature);
+    const int token = a.tokens ? a.tokens[r] : -1;
+    const bool padding = padded(a, token), given = a.tokens && !padding;
+    float x[NQ];
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+        const int j = lane + 64 * i;
+        x[i] = -INFINITY;
+        if (j < a.V && !padding) {
+            x[i] = row.load_one(j);
+            if constexpr (DT == EASGD_F32)              // logits that come as partial sums: added in ascending order
+                for (int p = 1; p < a.parts; ++p) x[i] += row.base[row.shift + j + p * a.part_stride];
+        }
+    }
+    float z_token = 0.f;
+    if (given) {                                        // uniform
+        float z = x[0];
+#pragma unroll
+        for (int i = 1; i < NQ; ++i) z = token >> 6 == i ? x[i] : z;
+        z_token = __shfl(z, token & 63);
+    }
+    float4 w = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+    if constexpr (MODE & SCORE_SUMS) {
+        float m = x[0];
+#pragma unroll
+        for (int i = 1; i < NQ; ++i) m = fmaxf(m, x[i]);
+        w.x = wave_max(m);
+    } else {
+        w = a.state[r];
+    }
+    const float from = w.x == -INFINITY ? 0.f : w.x;
+    float y[NQ], e[NQ], s = 0.f, u = 0.f;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+        y[i] = (x[i] - from) * q.c;
+        e[i] = exp2_fast(y[i]);
+        y[i] = fmaxf(y[i], LEAST);
+        s += e[i];
+        u = fmaf(e[i], y[i], u);
+    }
+    double entropy = (double)w.z;
+    if constexpr (MODE & SCORE_SUMS) {
+        w.y = wave_sum(s);
+        w.z = wave_sum(u);
+        unsigned before = 0;
+        if (a.rank && given) {
+            const bool masked = !(z_token > -INFINITY);
+#pragma unroll
+            for (int i = 0; i < NQ; ++i)
+                before += __popcll(__ballot(masked ? x[i] > -INFINITY : x[i] > z_token || (x[i] == z_token && lane + 64 * i < token)));
+        }
+        if (lane == 0) write_score(a, r, padding, given, w, z_token, before);
+        const RowScore score(w);
+        entropy = score.entropy;
+        if constexpr (TOP) {
+            unsigned long long *words = all_words[wave];
+            const unsigned n = short_first(x, (unsigned)a.k, words);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");         // LDS accesses of one wavefront are executed in order
+            for (unsigned i = lane; i < (unsigned)a.k; i += 64) {
+                unsigned at = i;
+                if (i < n) {
+                    at = 0;
+                    for (unsigned j = 0; j < n; ++j) at += words[j] > words[i];
+                }
+                write_alternative(a, r, at, i < n ? words[i] : 0, score, w.x);
+            }
+        }
+    }
+    if constexpr (MODE & SCORE_GRAD) {
+        const TokenSlope<4> g(a, r, padding, from, w.y, entropy, z_token, q, true);
+        const Row<DT> out(a.dlogits, r, a.dld, a.V);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+            const int j = lane + 64 * i;
+            const float d = g.none ? 0.f : j == token ? g.of_token : e[i] * fmaf(g.b, y[i], g.a);
+            if (j < a.V) out.base[out.shift + j] = LogitType<DT>::narrow(d);
+        }
+    }
+}
+
+// ---- host --------------------------------------------------------------------------------------------------------------------------
+// Into how many parts rows are cut: enough blocks to fill the chip, and at least 1024 slots (four per thread) a part.
+static constexpr int SCORE_BLOCK = 256, SCORE_SPLIT_ROWS = 256, SCORE_SPLIT_BLOCKS = 1024, SCORE_SPLIT_SLOTS = 1024;
+static int score_segments(size_t rows, int slots)
+{
+    if (rows >= SCORE_SPLIT_ROWS || slots < 2 * SCORE_SPLIT_SLOTS) return 1;
+    const int want = (int)((SCORE_SPLIT_BLOCKS + rows - 1) / rows), most = slots / SCORE_SPLIT_SLOTS;
+    return want < most ? want : most;
+}
+static void set_segments(ScoreArgs &a, int segments, int slots)
+{
+    a.segments = segments;
+    a.seg_slots = (slots + segments - 1) / segments;
+}
+static size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+template <typename F> static void by_flag(bool flag, F f)
+{
+    if (flag) f(std::true_type{});
+    else f(std::false_type{});
+}
+
+template <int DT> static void launch_sums(const ScoreArgs &a, bool entropy, hipStream_t s)
+{
+    const dim3 grid((unsigned)(a.rows * a.segments));
+    by_flag(entropy, [&](auto h) {
+        by_flag(a.rank, [&](auto rank) {
+            EASGD_LAUNCH((score_rows_kernel<DT, SCORE_BLOCK, decltype(h)::value, decltype(rank)::value>), grid, dim3(SCORE_BLOCK), 0, s, a);
+        });
+    });
+    if (a.segments > 1) EASGD_LAUNCH((score_join_kernel<DT>), dim3((unsigned)a.rows), dim3(64), 0, s, a);
+}
+template <int DT> static void launch_top(const ScoreArgs &a, hipStream_t s)
+{
+    EASGD_LAUNCH((score_top_kernel<DT, TOP_BLOCK>), dim3((unsigned)(a.rows * a.segments)), dim3(TOP_BLOCK), 0, s, a);
+    if (a.segments > 1) EASGD_LAUNCH((score_top_join_kernel<DT, TOP_BLOCK>), dim3((unsigned)a.rows), dim3(TOP_BLOCK), 0, s, a);
+}
+template <int DT> static void launch_grad(const ScoreArgs &a, bool entropy, hipStream_t s)
+{
+    by_flag(entropy, [&](auto h) {
+        EASGD_LAUNCH((score_grad_kernel<DT, SCORE_BLOCK, decltype(h)::value>), dim3((unsigned)(a.rows * a.segments)), dim3(SCORE_BLOCK), 0, s, a);
+    });
+}
+template <int DT, int MODE, bool TOP> static void launch_short(const ScoreArgs &a, hipStream_t s)
+{
+    const dim3 grid((unsigned)((a.rows + 3) / 4));
+    if (a.V <= 128) EASGD_LAUNCH((score_short_kernel<DT, 2, MODE, TOP>), grid, dim3(256), 0, s, a);
+    else EASGD_LAUNCH((score_short_kernel<DT, SCORE_SHORT_V / 64, MODE, TOP>), grid, dim3(256), 0, s, a);
+}
+
+int check_tokens(const char *name, const TokensGiven &t, bool rows)
+{
+    if (int rc = check_temperature(name, t.temperature)) return rc;
+    if (!std::isfinite(t.bonus)) return fail(EASGD_EINVAL, "%s: bonus must be finite", name);
+    if (rows && !t.tokens) return fail(EASGD_EINVAL, "%s: NULL pointer", name);
+    if (!aligned_to(t.tokens, 4) || !aligned_to(t.weight, 4) || !aligned_to(t.logprob, 4) || !aligned_to(t.entropy, 4))
+        return fail(EASGD_EINVAL, "%s: tokens, weight, logprob, entropy must be 4-byte aligned", name);
+    return EASGD_OK;
+}
+
+void score_logits(const float *logits, int parts, size_t part_stride, size_t rows, int classes, const TokensGiven &t, float scale,
+                  float *row_loss, float *dlogits, void *stream)
+{
+    ScoreArgs a = {};
+    a.logits = logits; a.ld = (size_t)classes; a.rows = rows; a.V = classes;
+    a.tokens = t.tokens; a.temperature = t.temperature; a.weight = t.weight; a.bonus = t.bonus;
+    a.logprob = t.logprob; a.entropy = t.entropy; a.loss = row_loss;
+    a.scale = scale; a.dlogits = dlogits; a.dld = (size_t)classes; a.parts = parts; a.part_stride = part_stride; a.segments = 1;
+    launch_short<EASGD_F32, SCORE_BOTH, false>(a, static_cast<hipStream_t>(stream));
+}
+
+}  // namespace easgd
+
+extern "C" {
+
+size_t easgd_score_tokens_workspace_bytes(size_t rows, int V, int k)
+{
+    using namespace easgd;
+    if (rows == 0 || rows > LOGITS_MAX_ROWS || V < 1 || V > LOGITS_MAX_V || k < 0 || k > LOGITS_MAX_TOP) return 0;
+    const int slots = most_slots(EASGD_F32, V);         // fp32 rows have the most slots, and the most parts
+    const int n = k ? top_segments(rows, slots, k) : score_segments(rows, slots);
+    return n == 1 ? 0 : rounded(rows * n * (sizeof(float4) + (size_t)k * 8));
+}
+
+int easgd_score_tokens(const void *logits, int dtype, size_t rows, int V, size_t ld, const int32_t *tokens, float temperature,
+                       float *logprob, float *entropy, int32_t *rank, int k, float *top_logprob, int32_t *top_indices, float *state,
+                       void *workspace, size_t workspace_bytes, void *stream)
+{
+    using namespace easgd;
+    const char *name = "easgd_score_tokens";
+    if (int rc = check_logits(name, logits, dtype, rows, V, ld)) return rc;
+    if (int rc = check_temperature(name, temperature)) return rc;
+    if (k < 0 || k > LOGITS_MAX_TOP) return fail(EASGD_EINVAL, "%s: k must be in [0, %d], got %d", name, LOGITS_MAX_TOP, k);
+    if (!tokens && (logprob || rank)) return fail(EASGD_EINVAL, "%s: logprob and rank need tokens", name);
+    if (rows > 0 && k > 0 && (!top_logprob || !top_indices)) return fail(EASGD_EINVAL, "%s: NULL pointer", name);
+    if (rows > 0 && k == 0 && !logprob && !entropy && !rank && !state) return fail(EASGD_EINVAL, "%s: nothing is asked for", name);
+    if (!aligned_to(tokens, 4) || !aligned_to(logprob, 4) || !aligned_to(entropy, 4) || !aligned_to(rank, 4) || !aligned_to(top_logprob, 4) || !aligned_to(top_indices, 4))
+        return fail(EASGD_EINVAL, "%s: tokens, logprob, entropy, rank, top_logprob, top_indices must be 4-byte aligned", name);
+    if (!aligned16(state)) return fail(EASGD_EINVAL, "%s: state must be 16-byte aligned", name);
+    if (int rc = check_workspace(name, workspace, workspace_bytes, easgd_score_tokens_workspace_bytes(rows, V, k))) return rc;
+    clear_error();
+    if (rows == 0) return EASGD_OK;
+    ScoreArgs a = {};
+    a.logits = logits; a.ld = ld; a.rows = rows; a.V = V;
+    a.tokens = tokens; a.temperature = temperature;
+    a.logprob = logprob; a.entropy = entropy; a.rank = rank; a.state = reinterpret_cast<float4 *>(state);
+    a.k = k; a.top_logprob = top_logprob; a.top_indices = top_indices; a.parts = 1;
+    const int slots = most_slots(dtype, V);
+    set_segments(a, k ? top_segments(rows, slots, k) : score_segments(rows, slots), slots);
+    a.partial = static_cast<float4 *>(workspace);
+    a.words = reinterpret_cast<unsigned long long *>(a.partial + rows * a.segments);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    by_dtype(dtype, [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if (V <= SCORE_SHORT_V) {
+            if (k) launch_short<DT, SCORE_SUMS, true>(a, s);
+            else launch_short<DT, SCORE_SUMS, false>(a, s);
+        } else if (k) launch_top<DT>(a, s);
+        else launch_sums<DT>(a, entropy || state, s);
+    });
+    return check_launch(name);
+}
+
+int easgd_score_tokens_grad(const void *logits, int dtype, size_t rows, int V, size_t ld, const int32_t *tokens, float temperature,
+                            const float *state, const float *dlogprob, const float *dentropy, float scale, void *dlogits, size_t dld, void *stream)
+{
+    using namespace easgd;
+    const char *name = "easgd_score_tokens_grad";
+    if (int rc = check_logits(name, logits, dtype, rows, V, ld)) return rc;
+    if (int rc = check_temperature(name, temperature)) return rc;
+    if (!tokens && dlogprob) return fail(EASGD_EINVAL, "%s: dlogprob needs tokens", name);
+    if (rows > 0 && (!state || !dlogits || (!dlogprob && !dentropy))) return fail(EASGD_EINVAL, "%s: NULL pointer", name);
+    if (!aligned_to(tokens, 4) || !aligned_to(dlogprob, 4) || !aligned_to(dentropy, 4))
+        return fail(EASGD_EINVAL, "%s: tokens, dlogprob, dentropy must be 4-byte aligned", name);
+    if (!aligned16(state)) return fail(EASGD_EINVAL, "%s: state must be 16-byte aligned", name);
+    if (int rc = check_gradient(name, dlogits, dtype, rows, V, dld, scale)) return rc;
+    if (rows && rows_overlap(logits, ld, dlogits, dld, V, rows, dtype_bytes(dtype))) return fail(EASGD_EINVAL, "%s: dlogits must not overlap logits", name);
+    clear_error();
+    if (rows == 0) return EASGD_OK;
+    ScoreArgs a = {};
+    a.logits = logits; a.ld = ld; a.rows = rows; a.V = V;
+    a.tokens = tokens; a.temperature = temperature; a.state = reinterpret_cast<float4 *>(const_cast<float *>(state));
+    a.dlogprob = dlogprob; a.dentropy = dentropy; a.scale = scale; a.dlogits = dlogits; a.dld = dld; a.parts = 1;
+    const int slots = most_slots(dtype, V);
+    set_segments(a, score_segments(rows, slots), slots);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    by_dtype(dtype, [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if (V <= SCORE_SHORT_V) launch_short<DT, SCORE_GRAD, false>(a, s);
+        else launch_grad<DT>(a, dentropy, s);
+    });
+    return check_launch(name);
+}
+
+size_t easgd_token_loss_workspace_bytes(size_t rows, int V)
+{
+    using namespace easgd;
+    if (rows == 0 || rows > LOGITS_MAX_ROWS || V <= SCORE_SHORT_V || V > LOGITS_MAX_V) return 0;
+    return rounded(rows * (score_segments(rows, most_slots(EASGD_F32, V)) + 1) * sizeof(float4));
+}
+
+int easgd_token_loss(const void *logits, int dtype, size_t rows, int V, size_t ld, const int32_t *tokens, const float *weight, float bonus,
+                     float temperature, float scale, float *loss, float *logprob, float *entropy, void *dlogits, size_t dld,
+                     void *workspace, size_t workspace_bytes, void *stream)
+{
+    using namespace easgd;
+    const char *name = "easgd_token_loss";
+    if (int rc = check_logits(name, logits, dtype, rows, V, ld)) return rc;
+    if (int rc = check_tokens(name, {tokens, weight, bonus, temperature, logprob, entropy}, rows > 0)) return rc;
+    if (rows > 0 && (!loss || !dlogits)) return fail(EASGD_EINVAL, "%s: NULL pointer", name);
+    if (!aligned_to(loss, 4)) return fail(EASGD_EINVAL, "%s: loss must be 4-byte aligned", name);
+    if (int rc = check_gradient(name, dlogits, dtype, rows, V, dld, scale)) return rc;
+    if (int rc = check_workspace(name, workspace, workspace_bytes, easgd_token_loss_workspace_bytes(rows, V))) return rc;
+    if (rows && rows_overlap(logits, ld, dlogits, dld, V, rows, dtype_bytes(dtype))) return fail(EASGD_EINVAL, "%s: dlogits must not overlap logits", name);
+    clear_error();
+    if (rows == 0) return EASGD_OK;
+    ScoreArgs a = {};
+    a.logits = logits; a.ld = ld; a.rows = rows; a.V = V;
+    a.tokens = tokens; a.temperature = temperature; a.weight = weight; a.bonus = bonus;
+    a.loss = loss; a.logprob = logprob; a.entropy = entropy; a.scale = scale; a.dlogits = dlogits; a.dld = dld; a.parts = 1;
+    const int slots = most_slots(dtype, V);
+    set_segments(a, score_segments(rows, slots), slots);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    by_dtype(dtype, [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if (V <= SCORE_SHORT_V) launch_short<DT, SCORE_BOTH, false>(a, s);
+        else {
+            a.state = static_cast<float4 *>(workspace);
+            a.partial = a.state + rows;
+            launch_sums<DT>(a, entropy || bonus != 0.f, s);
+            launch_grad<DT>(a, bonus != 0.f, s);
+        }
+    });
+    return check_launch(name);
+}
+
+}  // extern "C"

@@ -97,8 +97,7 @@ __global__ __launch_bounds__(BLOCK) void top_join_kernel(TopArgs a)
 }
 
 // ---- short rows: a wavefront each ---------------------------------------------------------------------------------------------
-// Element lane + 64 q sits in register q.  The k-th largest key is found bit by bit with votes; equal keys are taken by
-// ascending index, which is the order of registers, then lanes.  Bound: the votes' latency.  2048 x 1000 fp32, k = 10: 10.8 us.
+// Element lane + 64 q sits in register q (short_first).  Bound: the votes' latency.  2048 x 1000 fp32, k = 10: 10.8 us.
 template <int DT, int NQ>
 __global__ __launch_bounds__(256) void top_short_kernel(TopArgs a)
 {
@@ -112,15 +111,10 @@ __global__ __launch_bounds__(256) void top_short_kernel(TopArgs a)
 #pragma unroll
     for (int q = 0; q < NQ; ++q) x[q] = lane + 64 * q < a.V ? row.load_one(lane + 64 * q) : -INFINITY;
 
-    unsigned key[NQ], there = 0;
-    float m = -INFINITY;
-#pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-        key[q] = logit_key(x[q]);
-        there += __popcll(__ballot(key[q] != 0));
-        m = fmaxf(m, x[q]);
-    }
     if (a.lse) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) m = fmaxf(m, x[q]);
         m = wave_max(m);
         const float c = Scales(a.temperature).c, from = m == -INFINITY ? 0.f : m;
         float sum = 0.f;
@@ -129,40 +123,7 @@ __global__ __launch_bounds__(256) void top_short_kernel(TopArgs a)
         sum = wave_sum(sum);
         if (lane == 0) write_lse(a, r, make_float4(m, sum, 0.f, 0.f));
     }
-    const unsigned k = min((unsigned)a.k, there);
-    unsigned least = 1, above = there;                  // `above` keys are >= least
-    if (there > k) {
-        least = 0;
-        for (unsigned bit = 0x80000000u; bit && above != k; bit >>= 1) {
-            const unsigned next = least | bit;
-            unsigned n = 0;
-#pragma unroll
-            for (int q = 0; q < NQ; ++q) n += __popcll(__ballot(key[q] >= next));
-            if (n >= k) {
-                least = next;
-                above = n;
-            }
-        }
-    }
-    // keys above `least`, then as many equal ones as are wanted
-    unsigned equal_left = k;
-    if (above != k) {
-        unsigned n = 0;
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) n += __popcll(__ballot(key[q] > least));
-        equal_left = k - n;
-    }
-    unsigned n = 0;
-    const unsigned long long below = (1ull << lane) - 1;
-#pragma unroll
-    for (int q = 0; q < NQ; ++q) {
-        const unsigned long long equal = __ballot(key[q] == least && key[q] != 0);
-        const bool take = key[q] > least || (key[q] == least && key[q] != 0 && (unsigned)__popcll(equal & below) < equal_left);
-        equal_left -= min(equal_left, (unsigned)__popcll(equal));
-        const unsigned long long taken = __ballot(take);
-        if (take) words[n + __popcll(taken & below)] = order_word(key[q], lane + 64 * q);
-        n += __popcll(taken);
-    }
+    const unsigned n = short_first(x, (unsigned)a.k, words);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");         // LDS accesses of one wavefront are executed in order
     for (unsigned i = lane; i < (unsigned)a.k; i += 64) {
         unsigned rank = i;
@@ -174,23 +135,6 @@ __global__ __launch_bounds__(256) void top_short_kernel(TopArgs a)
     }
 }
 
-// Few long rows are cut into parts, so that there are blocks for the whole chip: each part's first k go through the workspace.
-// Many rows take blocks of 256 threads, five of which a compute unit holds (2048 x 131072 bf16, k = 64: 168 us against 180 with 512);
-// few rows, and more than 64 tokens (whose first floor wants many maxima), 512 (8 x 50001: 15.8 us against 18.5 with 256).  The change at
-// 256 rows suits a thousand rows and more better than some hundred, which leave a compute unit one to three blocks (us; 512 threads: k = 128):
-//   rows of 131072 bf16     255 (four parts each)   256    512    768    1024   2048
-//   256 threads, k = 64     49 (512 threads)        65     71     77     88     166
-//   512 threads, k = 128    65                      46     56     88     106    204
-static constexpr int TOP_BLOCK = 512, TOP_SHORT_V = 1024;
-static constexpr int TOP_SPLIT_ROWS = 256, TOP_SPLIT_SLOTS = 2048;
-static int top_segments(size_t rows, int slots, int k)
-{
-    if (rows >= TOP_SPLIT_ROWS || slots < 2 * TOP_SPLIT_SLOTS) return 1;
-    int n = (int)((512 + rows - 1) / rows);
-    if (n > slots / TOP_SPLIT_SLOTS) n = slots / TOP_SPLIT_SLOTS;
-    if (n > TOP_LIST / k) n = TOP_LIST / k;
-    return n < 1 ? 1 : n;
-}
 static size_t top_bytes(size_t rows, int segments, int k)
 {
     return segments == 1 ? 0 : (rows * segments * (sizeof(float4) + (size_t)k * 8) + 255) / 256 * 256;

@@ -1,0 +1,245 @@
+"""easgd_score_tokens, easgd_score_tokens_grad and easgd_token_loss against the 64-bit oracle: sizes, types, alignments, masks, ties."""
+import numpy as np
+import pytest
+import torch
+
+from logits_util import DTYPES, HALF_STEP, SMALLEST, place, sum_error
+from oracle import tokens as ot
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def hip():
+    import paper_1708_02983_amd as pkg
+    return pkg
+
+
+def exponent_error(V):
+    """Relative error of one exponential: three roundings of an exponent that counts (2^-126 is the last), two units of the function."""
+    return U * (3 * np.log(2) * 126 + 4)
+
+
+def bounds(z64, token, T):
+    """How far logprob and entropy of a row may be off.  The sum's relative error is that of sum_error; an entropy is ln s less a mean of
+    exponents weighted with the same exponentials, whose magnitudes are at most those of -log2 q and of the reference's distance (12, and 24
+    where sums of parts meet): both parts are off by the sum's error at most, the second times these magnitudes."""
+    V = len(z64)
+    e = sum_error(V)
+    return e + U, 2 * e * (1 + np.log(2) * (np.log2(max(V, 2)) + 24)) + U * 20
+
+
+def gradient_bound(z64, token, T, a, b, d, dtype):
+    """Every gradient is an exponential (exponent_error) times a factor from the sums (sum_error) and a linear function of its exponent, whose
+    terms are added in 32 bits (four roundings); the entropy's own error goes into that function."""
+    V = len(z64)
+    if not (z64 > -np.inf).any():
+        return np.zeros(V)                              # a row that is masked: 0 exactly
+    with np.errstate(invalid="ignore", divide="ignore"):
+        log_q = ot.log_softmax(z64, T)
+        q = np.exp(log_q)
+        log_q = np.where(q > 0, np.abs(log_q), 0.0)
+    _, h = bounds(z64, token, T)
+    entropy = ot.score(z64, token, T)[1]
+    size = q * (abs(a) + abs(b) * (log_q + entropy + 24)) / T
+    bound = size * (sum_error(V) + exponent_error(V) + 8 * U) + abs(b) * q * h / T
+    return bound + HALF_STEP[dtype] * np.abs(d) * 1.0001 + SMALLEST[dtype]
+
+
+def check(hip, z, tokens, T=1.0, k=0, dtype="fp32", pad=0, offset=0, a=None, b=None, without_tokens=False):
+    rows, V = z.shape
+    dz, z64 = place(z, dtype, pad, offset)
+    T = float(np.float32(T))
+    given = None if without_tokens else torch.tensor(tokens, dtype=torch.int32, device="cuda")
+    got = hip.easgd_score_tokens(dz, given, temperature=T, k=k, rank=None if without_tokens else True, state=True)
+    a = np.ones(rows, np.float32) if a is None else np.asarray(a, np.float32)
+    b = np.zeros(rows, np.float32) if b is None else np.asarray(b, np.float32)
+    out = torch.full((rows, V + 3), 7.0, dtype=DTYPES[dtype], device="cuda")
+    d = hip.easgd_score_tokens_grad(dz, given, got.state, temperature=T, dlogprob=None if without_tokens else torch.from_numpy(a).cuda(),
+                                    dentropy=torch.from_numpy(b).cuda() if b.any() or without_tokens else None, dlogits=out[:, :V])
+    assert (out[:, V:] == 7.0).all()
+    torch.cuda.synchronize()
+    host = [None if t is None else t.cpu().numpy().astype(np.float64) for t in got]
+    d = d.double().cpu().numpy()
+    for r in range(rows):
+        token = None if without_tokens else int(tokens[r])
+        lp, h, rank, top, places = ot.score(z64[r], token, T, k)
+        with np.errstate(invalid="ignore"):
+            e_lp, e_h = bounds(z64[r], token, T)
+        if not without_tokens:
+            assert close(host[0][r], lp, e_lp + U * abs(lp)), (r, host[0][r], lp, e_lp)
+            assert host[2][r] == rank, (r, host[2][r], rank)
+        assert close(host[1][r], h, e_h), (r, host[1][r], h, e_h)
+        if k:
+            assert host[4][r].tolist() == places.tolist(), r
+            for x, y in zip(host[3][r], top):
+                assert close(x, y, e_lp + U * abs(y)), (r, x, y)
+        up, up_h = (0.0 if without_tokens else float(a[r])), float(b[r])
+        want = ot.score_grad(z64[r], token, T, up, up_h)
+        if np.isnan(want).any():
+            assert np.isnan(d[r]).all(), r
+            continue
+        bound = gradient_bound(z64[r], token, T, up, up_h, want, dtype)
+        if token is not None and 0 <= token < V and (z64[r] > -np.inf).any():
+            bound[token] += abs(up) / T * sum_error(V)
+        off = np.abs(d[r] - want) - bound
+        assert (off <= 0).all(), (r, int(off.argmax()), d[r][off.argmax()], want[off.argmax()], bound[off.argmax()])
+    return got, d
+
+
+def close(x, y, tol):
+    if np.isnan(y):
+        return np.isnan(x)
+    if np.isinf(y):
+        return x == y
+    return abs(x - y) <= tol
+
+
+LENGTHS = [1, 2, 3, 63, 64, 65, 100, 127, 128, 129, 1000, 1023, 1024, 1025, 1031, 2048, 2049, 5003, 8191, 16387, 50001, 131079]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("V", LENGTHS)
+def test_lengths(hip, V, dtype):
+    rng = np.random.default_rng(V)
+    rows = 7 if V < 10000 else 3
+    z = rng.normal(size=(rows, V)) * 3
+    z[np.arange(rows), rng.integers(0, V, rows)] += 9
+    tokens = rng.integers(0, V, rows)
+    tokens[1] = z[1].argmax()
+    tokens[rows - 1] = -1 if V % 2 else V
+    check(hip, z, tokens, T=[1.0, 0.7, 2.0][V % 3], k=[0, 5, 20, 256][V % 4], dtype=dtype, pad=V % 5, offset=V % 7, a=rng.normal(size=rows), b=rng.normal(size=rows))
+
+
+@pytest.mark.parametrize("rows,V", [(300, 3000), (257, 9001), (1000, 1025), (2000, 77)])
+def test_many_rows(hip, rows, V):
+    rng = np.random.default_rng(rows)
+    z = rng.normal(size=(rows, V)) * 2
+    tokens = rng.integers(-1, V, rows)
+    check(hip, z, tokens, k=3, dtype="bf16", offset=3, a=rng.normal(size=rows), b=rng.normal(size=rows))
+    check(hip, z, tokens, k=0, dtype="fp32", offset=1, a=rng.normal(size=rows))
+
+
+@pytest.mark.parametrize("V", [5, 100, 700, 3000, 20000])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_masks_and_numbers_that_are_none(hip, V, dtype):
+    rng = np.random.default_rng(V)
+    z = rng.normal(size=(12, V)) * 2
+    ninf, inf = -np.inf, np.inf
+    z[0] = ninf                                         # nothing left
+    z[1] = ninf
+    z[1, V // 2] = 1.5                                  # one left, the token
+    z[2] = ninf
+    z[2, V // 2] = 1.5                                  # one left, another token
+    z[3, : V // 2] = ninf                               # a masked start, longer than a wavefront's first slots
+    z[4, V // 2:] = ninf
+    z[5, ::2] = ninf
+    z[6, V - 1] = inf
+    z[7, 0] = np.nan
+    z[8, :] = ninf
+    z[8, V - 1] = np.nan
+    z[9, :] = np.finfo(np.float16).min                  # masked with a large finite number
+    z[9, V // 3] = 2.0
+    z[10, :] = 3.0                                      # all equal: ranks and alternatives by index
+    z[11, : V - 1] = ninf
+    z[11, V - 1] = -1000.0
+    tokens = np.array([1, V // 2, 0, V - 1, V // 4, 2, 1, 1, 0, 1, V - 1, V - 1])
+    check(hip, z, tokens, k=4, dtype=dtype, offset=1, a=rng.normal(size=12), b=rng.normal(size=12))
+    check(hip, z, tokens, k=0, dtype=dtype, pad=1, a=rng.normal(size=12), b=rng.normal(size=12))
+
+
+@pytest.mark.parametrize("V", [90, 900, 4000])
+def test_ranks_among_equal_logits(hip, V):
+    rng = np.random.default_rng(V)
+    z = rng.integers(-2, 3, size=(40, V)).astype(np.float64)            # -0 and 0 among them
+    z[::2][z[::2] == 0] *= -1.0
+    tokens = rng.integers(0, V, 40)
+    check(hip, z, tokens, k=10, dtype="fp16", offset=5)
+    check(hip, z, tokens, k=0, dtype="fp32", offset=2)
+
+
+@pytest.mark.parametrize("V", [64, 3000, 30000])
+@pytest.mark.parametrize("size", [1e2, 1e4, 3e8, 1e30])
+def test_large_logits(hip, V, size):
+    """Logits that differ by little next to their size: exponents are of differences."""
+    rng = np.random.default_rng(V)
+    z = np.float32(size) + (rng.normal(size=(4, V)) * 2).astype(np.float32)
+    z[2] = -z[2]
+    tokens = rng.integers(0, V, 4)
+    tokens[0] = z[0].argmax()
+    got = hip.easgd_score_tokens(torch.from_numpy(z).cuda(), torch.tensor(tokens, dtype=torch.int32, device="cuda"), rank=True)
+    for r in range(4):
+        lp, h, rank, *_ = ot.score(z[r], int(tokens[r]))
+        e_lp, e_h = bounds(z[r].astype(np.float64), int(tokens[r]), 1.0)
+        assert close(got.logprob[r].item(), lp, e_lp + U * abs(lp)) and close(got.entropy[r].item(), h, e_h) and got.rank[r].item() == rank
+
+
+@pytest.mark.parametrize("V", [70, 1500, 40000])
+def test_entropy_alone(hip, V):
+    z = np.random.default_rng(V).normal(size=(5, V)) * 2
+    check(hip, z, np.zeros(5, int), k=2, without_tokens=True, b=np.ones(5))
+    check(hip, z, np.zeros(5, int), dtype="bf16", without_tokens=True, b=np.ones(5))
+
+
+@pytest.mark.parametrize("V", [40, 900, 1300, 9000, 70001])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("rows", [5, 270])
+def test_loss_and_gradient_in_one_call(hip, V, dtype, rows):
+    if rows * V > 3000000:
+        rows = 40 if dtype == "fp32" else 256
+    rng = np.random.default_rng(V + rows)
+    z = rng.normal(size=(rows, V)) * 2
+    z[1] = -np.inf
+    z[2, ::3] = -np.inf
+    tokens = rng.integers(0, V, rows)
+    tokens[3] = -1
+    tokens[2] = 1
+    weight = rng.normal(size=rows).astype(np.float32)
+    weight[4] = 0.0
+    for bonus, w in ((0.0, weight), (0.125, weight), (0.0, None)):
+        dz, z64 = place(z, dtype, pad=V % 3, offset=V % 5)
+        T, scale = 0.75, 0.5
+        given = torch.tensor(tokens, dtype=torch.int32, device="cuda")
+        loss, logprob, entropy, d = hip.easgd_token_loss(dz, given, weight=None if w is None else torch.from_numpy(w).cuda(), bonus=bonus, temperature=T,
+                                                         scale=scale, entropy=bonus != 0.0 or None)
+        again = hip.easgd_token_loss(dz, given, weight=None if w is None else torch.from_numpy(w).cuda(), bonus=bonus, temperature=T, scale=scale)
+        assert torch.equal(loss, again[0]) and torch.equal(d.view(torch.uint8), again[3].view(torch.uint8)), "not the same from run to run"
+        loss, logprob, d = loss.double().cpu().numpy(), logprob.double().cpu().numpy(), d.double().cpu().numpy()
+        for r in range(rows):
+            token, wr = int(tokens[r]), 1.0 if w is None else float(w[r])
+            want, grad = ot.token_loss(z64[r], token, wr, bonus, T)
+            lp, h, *_ = ot.score(z64[r], token, T)
+            with np.errstate(invalid="ignore"):
+                e_lp, e_h = bounds(z64[r], token, T)
+            e_lp += U * abs(lp) if np.isfinite(lp) else 0.0
+            assert close(logprob[r], lp, e_lp) and close(loss[r], want, abs(wr) * e_lp + bonus * e_h + 2 * U * abs(want)), (r, loss[r], want)
+            if entropy is not None:
+                assert close(entropy[r].item(), h, e_h)
+            bound = np.zeros(V) if not grad.any() else scale * gradient_bound(z64[r], token, T, -wr, -bonus, grad, dtype) + SMALLEST[dtype]
+            if grad.any():
+                bound[token] += scale * abs(wr) / T * sum_error(V)
+            off = np.abs(d[r] - scale * grad) - bound
+            assert (off <= 0).all(), (r, int(off.argmax()), d[r][off.argmax()], scale * grad[off.argmax()], bound[off.argmax()])
+
+
+def test_one_call_and_two_agree(hip):
+    """The one call and the two passes, and both against differences of the loss in 64 bits."""
+    rng = np.random.default_rng(2)
+    for V in (60, 3000):
+        z = rng.normal(size=(4, V)) * 2
+        dz, z64 = place(z, "fp32")
+        tokens = torch.tensor(rng.integers(0, V, 4), dtype=torch.int32, device="cuda")
+        loss, _, _, d = hip.easgd_token_loss(dz, tokens, bonus=0.5)
+        s = hip.easgd_score_tokens(dz, tokens, state=True)
+        two = hip.easgd_score_tokens_grad(dz, tokens, s.state, dlogprob=torch.full((4,), -1.0, device="cuda"), dentropy=torch.full((4,), -0.5, device="cuda"))
+        # the state's entropy is rounded to 32 bits where the one call keeps it in 64: 2^-24 H q, and each pass its own last rounding
+        assert torch.allclose(d, two, rtol=2.0 ** -20, atol=2.0 ** -21)
+        for r in range(4):
+            t = int(tokens[r])
+            for j in rng.integers(0, V, 5):
+                up, down = z64[r].copy(), z64[r].copy()
+                up[j] += 1e-4
+                down[j] -= 1e-4
+                slope = (ot.token_loss(up, t, 1.0, 0.5)[0] - ot.token_loss(down, t, 1.0, 0.5)[0]) / 2e-4
+                assert abs(d[r, j].item() - slope) <= 1e-6
