@@ -217,7 +217,7 @@ int sync_sgd_round(float *W, float *V, const float *G,
  *                                         takes part in the exchange only, whatever its G holds (easgd_grad_norms gives such factors).
  *   eta_at, step_at  DEVICE in [1] fp32 / int64, or NULL   read in the place of eta and step when the kernel runs: a captured call takes the
  *                                         values of its replay (step_at below 1 counts as 1)
- *   beta1, beta2 in [0, 1), eps > 0, step >= 1; N <= 2^34.
+ *   beta1, beta2 in [0, 1), eps in [1e-30, 1e30], step >= 1; N <= 2^34, P <= 65535.
  * The moments' arithmetic is fixed, every operation rounded on its own: fl(fl(beta1*M) + fl(fl(1-beta1)*g)), fl(fl(beta2*S) +
  * fl(fl(fl(1-beta2)*g)*g)).  Results are the same bits from run to run.  128-bit accesses where W, Wc (and M, S) are 16-byte and G is
  * four elements aligned and ld % 4 == 0; element by element otherwise, with the same values.

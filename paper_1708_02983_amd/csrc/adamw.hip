@@ -82,6 +82,48 @@ struct TensorWalk {
     __device__ __forceinline__ float decay() const { return at < a.tensors ? a.decays[at] : a.decay; }
 };
 
+// The rates (eta among them) and decays of a lane's four parameters in a block of 256; nearly always one tensor has the whole block.
+__device__ __forceinline__ bool in_one_tensor(const TensorWalk &tensor, size_t block) { return tensor.end() >= block * 256 + 256; }
+struct Pace {
+    float rate[4], decay[4];
+    __device__ __forceinline__ Pace(float r, float d)
+    {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            rate[q] = r;
+            decay[q] = d;
+        }
+    }
+    __device__ __forceinline__ Pace(const AdamwArgs &a, const StepNumbers &n, size_t block, size_t j)
+    {
+        TensorWalk tensor(a, block * 256);
+        const bool one = in_one_tensor(tensor, block);  // uniform
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (!one) tensor.to(j + q);
+            rate[q] = n.eta * tensor.rate();
+            decay[q] = tensor.decay();
+        }
+    }
+};
+// The same for the blocks of a tile: two numbers a block, and a walk anew where a tensor ends inside one.
+template <int GROUPS> struct TilePace {
+    float rate[GROUPS], decay[GROUPS];
+    bool one[GROUPS];
+    __device__ __forceinline__ void set(const AdamwArgs &a, const StepNumbers &n, int q, size_t block, size_t)
+    {
+        const TensorWalk tensor(a, block * 256);
+        one[q] = in_one_tensor(tensor, block);
+        rate[q] = n.eta * tensor.rate();
+        decay[q] = tensor.decay();
+    }
+    __device__ __forceinline__ Pace of(const AdamwArgs &a, const StepNumbers &n, int q, size_t j) const
+    {
+        if (one[q]) return Pace(rate[q], decay[q]);
+        return Pace(a, n, __builtin_amdgcn_readfirstlane((unsigned)(j >> 8)), j);
+    }
+};
+
 // ---- the rule of one parameter -------------------------------------------------------------------------------------------
 // The moments' arithmetic decides stored codes of 8 bits, so it is pinned: every operation is rounded on its own.
 __device__ __forceinline__ void adamw_moments(float &m, float &v, float g, const StepNumbers &n)
@@ -93,8 +135,11 @@ __device__ __forceinline__ void adamw_moments(float &m, float &v, float g, const
 // What a parameter moves by: eta (m' / (sqrt(v') + eps) + decay w)
 __device__ __forceinline__ float adamw_move(float w, float m, float v, float eta, float decay, const StepNumbers &n)
 {
-    const float d = fmaf(sqrtf(v), n.by2, n.eps);
-    return eta * fmaf(decay, w, m * n.by1 / d);
+    // The hardware's root and reciprocal are right to one unit; roots of what is below 2^-64 are taken of 2^64 times it, since the instruction
+    // has no subnormal numbers.  d is at least eps, so its reciprocal is a normal number.
+    const bool small = v < 0x1p-64f;
+    const float root = __builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v) * (small ? n.by2 * 0x1p-32f : n.by2);
+    return eta * fmaf(decay, w, m * (n.by1 * __builtin_amdgcn_rcpf(root + n.eps)));
 }
 
 // ---- moments in 8 bits -----------------------------------------------------------------------------------------------------
@@ -135,150 +180,256 @@ template <int BITS, int TOP> struct EightBits {
 using MomentM = EightBits<3, 7>;
 using MomentS = EightBits<2, 14>;
 
+// the largest magnitude's bits over a wavefront: within rows of 16 lanes by data-parallel moves, then the four rows as scalars
 __device__ __forceinline__ unsigned wave_max_bits(unsigned v)
 {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = max(v, (unsigned)__shfl_xor((int)v, o));
-    return v;
+    auto with = [&](unsigned other) { v = max(v, other); };
+    with((unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));        // lane ^ 1
+    with((unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));        // lane ^ 2
+    with((unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true));       // 8 lanes mirrored
+    with((unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, true));       // 16 lanes mirrored
+    const unsigned a = (unsigned)__builtin_amdgcn_readlane((int)v, 0), b = (unsigned)__builtin_amdgcn_readlane((int)v, 16);
+    const unsigned c = (unsigned)__builtin_amdgcn_readlane((int)v, 32), d = (unsigned)__builtin_amdgcn_readlane((int)v, 48);
+    return max(max(a, b), max(c, d));
 }
 
-// ---- four consecutive parameters ----------------------------------------------------------------------------------------------
-typedef float Four __attribute__((ext_vector_type(4)));
-// WIDE: all of a row's fours are aligned to their size, and read and stored at once
-template <typename T, bool WIDE> __device__ __forceinline__ void load_four(const T *p, size_t j, size_t N, T (&x)[4])
+// ---- four consecutive parameters of a lane ------------------------------------------------------------------------------------
+// How they are accessed: at once past the caches (what is read once and written once), at once, or element by element with a look at the
+// row's end (rows at other alignments, and the last 256 parameters).
+enum { ACCESS_STREAM, ACCESS_WIDE, ACCESS_EACH };
+template <typename T, int ACCESS> __device__ __forceinline__ void load_four(const T *p, size_t j, size_t N, T (&x)[4])
 {
     typedef T Vec __attribute__((ext_vector_type(4)));
-    if (WIDE && j + 4 <= N) {
-        const Vec v = *reinterpret_cast<const Vec *>(p + j);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = v[i];
-    } else {
+    if constexpr (ACCESS == ACCESS_EACH) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = j + i < N ? p[j + i] : (T)0;
+    } else {
+        const Vec *at = reinterpret_cast<const Vec *>(p + j);
+        Vec v;
+        if constexpr (ACCESS == ACCESS_STREAM) v = __builtin_nontemporal_load(at);
+        else v = *at;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = v[i];
     }
 }
-template <typename T, bool WIDE> __device__ __forceinline__ void store_four(T *p, size_t j, size_t N, const T (&x)[4])
+template <typename T, int ACCESS> __device__ __forceinline__ void store_four(T *p, size_t j, size_t N, const T (&x)[4])
 {
     typedef T Vec __attribute__((ext_vector_type(4)));
-    if (WIDE && j + 4 <= N) {
-        const Vec v = {x[0], x[1], x[2], x[3]};
-        *reinterpret_cast<Vec *>(p + j) = v;
-    } else {
+    if constexpr (ACCESS == ACCESS_EACH) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (j + i < N) p[j + i] = x[i];
+    } else {
+        const Vec v = {x[0], x[1], x[2], x[3]};
+        Vec *at = reinterpret_cast<Vec *>(p + j);
+        if constexpr (ACCESS == ACCESS_STREAM) __builtin_nontemporal_store(v, at);
+        else *at = v;
     }
 }
 
-// ---- a wavefront per 256 parameters, worker by worker ------------------------------------------------------------------------------
-template <int GT, bool EIGHT, bool CENTER, bool WIDE>
-__global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs a)
-{
+// A worker's share of 256 parameters, four of them a lane's, between load() and store().
+template <int GT, bool EIGHT, int ACCESS> struct Worker {
     using Grad = typename LogitType<GT>::Stored;
-    const size_t block = (size_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (block >= a.blocks) return;                      // wavefronts of a block have nothing in common
-    const int lane = threadIdx.x & 63;
-    const size_t j = block * 256 + (size_t)lane * 4;
-    const StepNumbers n(a);
-    float rate[4], decay[4];
-    TensorWalk tensor(a, block * 256);
-    if (tensor.end() >= block * 256 + 256) {            // uniform: one tensor for all
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            rate[q] = n.eta * tensor.rate();
-            decay[q] = tensor.decay();
-        }
-    } else {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            tensor.to(j + q);
-            rate[q] = n.eta * tensor.rate();
-            decay[q] = tensor.decay();
+    float w[4], m[4], v[4];
+    Grad g[4];
+    unsigned char mc[4], vc[4];
+    float ms, vs;                      // scales, the same for all lanes
+    __device__ __forceinline__ void load_moments(const AdamwArgs &a, int i, size_t j)
+    {
+        const size_t row = (size_t)i * a.ld;
+        load_four<Grad, ACCESS>((const Grad *)a.G + row, j, a.N, g);
+        if constexpr (EIGHT) {
+            load_four<unsigned char, ACCESS>((const unsigned char *)a.M + row, j, a.N, mc);
+            load_four<unsigned char, ACCESS>((const unsigned char *)a.S + row, j, a.N, vc);
+            const size_t block = (size_t)i * a.blocks + __builtin_amdgcn_readfirstlane((unsigned)(j >> 8));
+            ms = a.M_scale[block];
+            vs = a.S_scale[block];
+        } else {
+            load_four<float, ACCESS>((const float *)a.M + row, j, a.N, m);
+            load_four<float, ACCESS>((const float *)a.S + row, j, a.N, v);
         }
     }
-    float c[4] = {}, sum[4] = {};
-    if constexpr (CENTER) load_four<float, WIDE>(a.Wc, j, a.N, c);
-    for (int i = 0; i < a.P; ++i) {                     // ascending: fixed order of the sum
-        const size_t row = (size_t)i * a.ld;
-        const float clip = a.clip ? a.clip[i] : 1.f;
-        float w[4], step[4] = {};
-        load_four<float, WIDE>(a.W + row, j, a.N, w);
-        if (clip != 0.f) {
-            float m[4], v[4];
-            Grad gs[4];
-            load_four<Grad, WIDE>((const Grad *)a.G + row, j, a.N, gs);
-            unsigned char mc[4], vc[4];
-            float *const Ms = EIGHT ? a.M_scale + (size_t)i * a.blocks + block : nullptr, *const Ss = EIGHT ? a.S_scale + (size_t)i * a.blocks + block : nullptr;
-            if constexpr (EIGHT) {
-                load_four<unsigned char, WIDE>((const unsigned char *)a.M + row, j, a.N, mc);
-                load_four<unsigned char, WIDE>((const unsigned char *)a.S + row, j, a.N, vc);
-                const float ms = *Ms, vs = *Ss;
+    __device__ __forceinline__ void load_parameters(const AdamwArgs &a, int i, size_t j) { load_four<float, ACCESS>(a.W + (size_t)i * a.ld, j, a.N, w); }
+    // new moments, and what the parameters move by
+    __device__ __forceinline__ void step(const AdamwArgs &a, int i, size_t j, float clip, const Pace &pace, const StepNumbers &n, float (&move)[4])
+    {
+        if constexpr (EIGHT) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    m[q] = __builtin_amdgcn_cvt_f32_fp8((int)mc[q], 0) * ms;
-                    v[q] = __builtin_amdgcn_cvt_f32_bf8((int)vc[q], 0) * vs;
-                }
-            } else {
-                load_four<float, WIDE>((const float *)a.M + row, j, a.N, m);
-                load_four<float, WIDE>((const float *)a.S + row, j, a.N, v);
+            for (int q = 0; q < 4; ++q) {
+                m[q] = __builtin_amdgcn_cvt_f32_fp8((int)mc[q], 0) * ms;
+                v[q] = __builtin_amdgcn_cvt_f32_bf8((int)vc[q], 0) * vs;
             }
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            adamw_moments(m[q], v[q], clip * LogitType<GT>::widen(g[q]), n);
+            move[q] = adamw_move(w[q], m[q], v[q], pace.rate[q], pace.decay[q], n);
+        }
+        if constexpr (EIGHT) {
             unsigned most_m = 0, most_v = 0;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                adamw_moments(m[q], v[q], clip * LogitType<GT>::widen(gs[q]), n);
-                step[q] = adamw_move(w[q], m[q], v[q], rate[q], decay[q], n);
-                if (j + q < a.N) {
-                    most_m = max(most_m, __float_as_uint(m[q]) & 0x7fffffffu);
-                    most_v = max(most_v, __float_as_uint(v[q]) & 0x7fffffffu);
-                }
+                const bool in = ACCESS != ACCESS_EACH || j + q < a.N;
+                most_m = max(most_m, in ? __float_as_uint(m[q]) & 0x7fffffffu : 0u);
+                most_v = max(most_v, in ? __float_as_uint(v[q]) & 0x7fffffffu : 0u);
             }
-            if constexpr (EIGHT) {
-                const MomentM em(wave_max_bits(most_m));
-                const MomentS es(wave_max_bits(most_v));
+            const MomentM em(wave_max_bits(most_m));
+            const MomentS es(wave_max_bits(most_v));
+            ms = em.stored();
+            vs = es.stored();
+            const unsigned h[2] = {mix((unsigned)(j >> 2) ^ dither_key(a.seed, i, n.step, 0)), mix((unsigned)(j >> 2) ^ dither_key(a.seed, i, n.step, 1))};
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const unsigned h = mix((unsigned)(j >> 2) ^ dither_key(a.seed, i, n.step, q >> 1)), dither = q & 1 ? h >> 16 : h & 0xffffu;
-                    mc[q] = (unsigned char)(em.code(fabsf(m[q]), dither) | (m[q] < 0.f ? 0x80u : 0u));
-                    vc[q] = (unsigned char)max(es.code(v[q], dither), v[q] > 0.f && es.there ? 1u : 0u);
-                }
-                store_four<unsigned char, WIDE>((unsigned char *)a.M + row, j, a.N, mc);
-                store_four<unsigned char, WIDE>((unsigned char *)a.S + row, j, a.N, vc);
-                if (lane == 0) {
-                    *Ms = em.stored();
-                    *Ss = es.stored();
-                }
-            } else {
-                store_four<float, WIDE>((float *)a.M + row, j, a.N, m);
-                store_four<float, WIDE>((float *)a.S + row, j, a.N, v);
+            for (int q = 0; q < 4; ++q) {
+                const unsigned dither = q & 1 ? h[q >> 1] >> 16 : h[q >> 1] & 0xffffu;
+                mc[q] = (unsigned char)(em.code(fabsf(m[q]), dither) | (m[q] < 0.f ? 0x80u : 0u));
+                vc[q] = (unsigned char)max(es.code(v[q], dither), v[q] > 0.f ? 1u : 0u);
             }
+        }
+    }
+    __device__ __forceinline__ void store_moments(const AdamwArgs &a, int i, size_t j)
+    {
+        const size_t row = (size_t)i * a.ld;
+        if constexpr (EIGHT) {
+            store_four<unsigned char, ACCESS>((unsigned char *)a.M + row, j, a.N, mc);
+            store_four<unsigned char, ACCESS>((unsigned char *)a.S + row, j, a.N, vc);
+            const size_t block = (size_t)i * a.blocks + __builtin_amdgcn_readfirstlane((unsigned)(j >> 8));
+            if ((threadIdx.x & 63) == 0) {
+                a.M_scale[block] = ms;
+                a.S_scale[block] = vs;
+            }
+        } else {
+            store_four<float, ACCESS>((float *)a.M + row, j, a.N, m);
+            store_four<float, ACCESS>((float *)a.S + row, j, a.N, v);
+        }
+    }
+    __device__ __forceinline__ void store_parameters(const AdamwArgs &a, int i, size_t j) { store_four<float, ACCESS>(a.W + (size_t)i * a.ld, j, a.N, w); }
+};
+
+// One block of 256 parameters by a wavefront, workers [i0, i1).
+template <int GT, bool EIGHT, bool CENTER, int ACCESS>
+__device__ __forceinline__ void adamw_block(const AdamwArgs &a, const StepNumbers &n, size_t block, int i0, int i1)
+{
+    const size_t j = block * 256 + (size_t)(threadIdx.x & 63) * 4;
+    const Pace pace(a, n, block, j);
+    float c[4] = {}, sum[4] = {};
+    if constexpr (CENTER) load_four<float, ACCESS == ACCESS_EACH ? ACCESS_EACH : ACCESS_WIDE>(a.Wc, j, a.N, c);
+    for (int i = i0; i < i1; ++i) {                     // ascending: fixed order of the sum
+        const float clip = a.clip ? a.clip[i] : 1.f;
+        Worker<GT, EIGHT, ACCESS> worker;
+        float move[4] = {};
+        worker.load_parameters(a, i, j);
+        if (clip != 0.f) {
+            worker.load_moments(a, i, j);
+            worker.step(a, i, j, clip, pace, n, move);
+            worker.store_moments(a, i, j);
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             if constexpr (CENTER) {
-                const float d = w[q] - c[q];
+                const float d = worker.w[q] - c[q];
                 sum[q] += d;
-                step[q] = fmaf(n.alpha, d, step[q]);
+                move[q] = fmaf(n.alpha, d, move[q]);
             }
-            w[q] -= step[q];
+            worker.w[q] -= move[q];
         }
-        store_four<float, WIDE>(a.W + row, j, a.N, w);
+        worker.store_parameters(a, i, j);
     }
     if constexpr (CENTER) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) c[q] = fmaf(n.alpha, sum[q], c[q]);
-        store_four<float, WIDE>(a.Wc, j, a.N, c);
+        store_four<float, ACCESS == ACCESS_EACH ? ACCESS_EACH : ACCESS_WIDE>(a.Wc, j, a.N, c);
+    }
+}
+
+// ---- replicas at any alignment: a wavefront per 256 parameters, worker by worker (by its own without a center: blockIdx.y) ------------
+template <int GT, bool EIGHT, bool CENTER>
+__global__ __launch_bounds__(256) void adamw_each_kernel(AdamwArgs a)
+{
+    const size_t block = (size_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (block >= a.blocks) return;                      // wavefronts of a block have nothing in common
+    const StepNumbers n(a);
+    adamw_block<GT, EIGHT, CENTER, ACCESS_EACH>(a, n, block, CENTER ? 0 : (int)blockIdx.y, CENTER ? a.P : (int)blockIdx.y + 1);
+}
+
+// ---- many parameters: GROUPS blocks of 256 a wavefront, all requests of a worker under way at once -------------------------------------
+template <int GT, bool EIGHT, bool CENTER, bool NT, int GROUPS, bool DIES>
+__global__ __launch_bounds__(256) void adamw_tile_kernel(AdamwArgs a)
+{
+    typedef TileMap<GROUPS, DIES> Map;
+    constexpr int ACCESS = NT ? ACCESS_STREAM : ACCESS_WIDE;
+    const size_t full = a.N / 256;
+    const StepNumbers n(a);
+    const size_t first = Map::first(blockIdx.x, threadIdx.x), lead = Map::first(blockIdx.x, threadIdx.x & ~63u) >> 6;       // in groups of four; the wavefront's first block
+    const size_t b0 = (size_t)__builtin_amdgcn_readfirstlane((unsigned)lead);
+    constexpr size_t STEP = Map::STRIDE >> 6;
+    if (b0 + (GROUPS - 1) * STEP >= full) {             // uniform for the wavefront: at the row's end
+#pragma unroll 1
+        for (int q = 0; q < GROUPS; ++q) {
+            const size_t block = b0 + q * STEP;
+            if (block < full) adamw_block<GT, EIGHT, CENTER, ACCESS_WIDE>(a, n, block, 0, a.P);
+            else if (block < a.blocks) adamw_block<GT, EIGHT, CENTER, ACCESS_EACH>(a, n, block, 0, a.P);
+        }
+        return;
+    }
+    size_t j[GROUPS];
+    float c[GROUPS][4], sum[GROUPS][4] = {};
+    TilePace<GROUPS> pace;
+#pragma unroll
+    for (int q = 0; q < GROUPS; ++q) {
+        j[q] = (first + q * Map::STRIDE) * 4;
+        pace.set(a, n, q, b0 + q * STEP, j[q]);
+        if constexpr (CENTER) load_four<float, ACCESS_WIDE>(a.Wc, j[q], a.N, c[q]);
+    }
+    for (int i = 0; i < a.P; ++i) {                     // ascending: fixed order of the sum
+        const float clip = a.clip ? a.clip[i] : 1.f;
+        Worker<GT, EIGHT, ACCESS> worker[GROUPS];
+        if (clip != 0.f) {
+#pragma unroll
+            for (int q = 0; q < GROUPS; ++q) worker[q].load_moments(a, i, j[q]);
+        }
+#pragma unroll
+        for (int q = 0; q < GROUPS; ++q) worker[q].load_parameters(a, i, j[q]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int q = 0; q < GROUPS; ++q) {
+            float move[4] = {};
+            if (clip != 0.f) worker[q].step(a, i, j[q], clip, pace.of(a, n, q, j[q]), n, move);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (CENTER) {
+                    const float d = worker[q].w[e] - c[q][e];
+                    sum[q][e] += d;
+                    move[e] = fmaf(n.alpha, d, move[e]);
+                }
+                worker[q].w[e] -= move[e];
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (clip != 0.f) {
+#pragma unroll
+            for (int q = 0; q < GROUPS; ++q) worker[q].store_moments(a, i, j[q]);
+        }
+#pragma unroll
+        for (int q = 0; q < GROUPS; ++q) worker[q].store_parameters(a, i, j[q]);
+    }
+    if constexpr (CENTER) {
+#pragma unroll
+        for (int q = 0; q < GROUPS; ++q) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c[q][e] = fmaf(n.alpha, sum[q][e], c[q][e]);
+            store_four<float, ACCESS_WIDE>(a.Wc, j[q], a.N, c[q]);
+        }
     }
 }
 
 // ---- norms -------------------------------------------------------------------------------------------------------------------------
-// Squares are added in 64 bits: no gradient is too large or too small for them, and the order of addition is fixed.
+// Squares are added in 64 bits: no gradient is too large or too small for them, and the order of addition is fixed.  Bound: HBM.
 struct NormArgs {
     const void *G;
     int P;
     size_t N, ld;
     float max_norm, *norm, *clip;
     int parts;
-    size_t part;                       // elements of a part of a row
     double *partial;                   // [P][parts]
 };
 __device__ __forceinline__ void write_norm(const NormArgs &a, int i, double sum)
@@ -288,31 +439,62 @@ __device__ __forceinline__ void write_norm(const NormArgs &a, int i, double sum)
     a.norm[i] = stored;
     if (a.clip) a.clip[i] = !(stored < INFINITY) ? 0.f : norm <= (double)a.max_norm ? 1.f : (float)((double)a.max_norm / norm);
 }
-template <int GT, int BLOCK>
+// A row is cut into tiles of BLOCK * DEEP slots of 128 bits on the 16-byte grid; part p of it has tiles p, p + parts, ...: the chip reads
+// one window of memory at a time.  The elements in front of the first slot and behind the last one are part 0's.
+template <int GT, int BLOCK, int DEEP>
 __global__ __launch_bounds__(BLOCK) void norm_parts_kernel(NormArgs a)
 {
+    using Type = LogitType<GT>;
+    using Stored = typename Type::Stored;
+    constexpr int VEC = Type::VEC;
+    typedef unsigned Words __attribute__((ext_vector_type(4)));
     __shared__ double scratch[BLOCK / 64];
     const int i = blockIdx.y;
-    const auto *g = (const typename LogitType<GT>::Stored *)a.G + (size_t)i * a.ld;
-    const size_t j0 = (size_t)blockIdx.x * a.part, j1 = min(j0 + a.part, a.N);
-    double sum = 0.0;
-    for (size_t j = j0 + threadIdx.x; j < j1; j += BLOCK) {
-        const double x = (double)LogitType<GT>::widen(g[j]);
-        sum = fma(x, x, sum);
+    const Stored *row = (const Stored *)a.G + (size_t)i * a.ld;
+    const size_t skip = (size_t)((16u - ((uintptr_t)row & 15u)) & 15u) / sizeof(Stored), head = skip < a.N ? skip : a.N, slots = (a.N - head) / VEC;
+    const Words *at = reinterpret_cast<const Words *>(row + head);
+    double sum[2] = {0.0, 0.0};
+    auto add = [&](const Words &w) {
+        float x[VEC];
+        Type::unpack(make_uint4(w[0], w[1], w[2], w[3]), x);
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) sum[q & 1] = fma((double)x[q], (double)x[q], sum[q & 1]);
+    };
+    constexpr size_t TILE = (size_t)BLOCK * DEEP;
+    for (size_t t = blockIdx.x; t * TILE < slots; t += a.parts) {
+        const size_t s = t * TILE + threadIdx.x;
+        Words w[DEEP];
+        if ((t + 1) * TILE <= slots) {                  // uniform
+#pragma unroll
+            for (int q = 0; q < DEEP; ++q) w[q] = __builtin_nontemporal_load(at + s + q * BLOCK);
+#pragma unroll
+            for (int q = 0; q < DEEP; ++q) add(w[q]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < DEEP; ++q)
+                if (s + q * BLOCK < slots) add(at[s + q * BLOCK]);
+        }
     }
-    sum = block_sum<BLOCK>(sum, scratch);
+    if (blockIdx.x == 0) {
+        const size_t tail = head + slots * VEC;
+        auto one = [&](size_t j) {
+            const double x = (double)Type::widen(row[j]);
+            sum[0] = fma(x, x, sum[0]);
+        };
+        if (threadIdx.x < head) one(threadIdx.x);
+        if (tail + threadIdx.x < a.N) one(tail + threadIdx.x);
+    }
+    const double all = block_sum<BLOCK>(sum[0] + sum[1], scratch);
     if (threadIdx.x != 0) return;
-    if (a.parts == 1) write_norm(a, i, sum);
-    else a.partial[(size_t)i * a.parts + blockIdx.x] = sum;
+    if (a.parts == 1) write_norm(a, i, all);
+    else a.partial[(size_t)i * a.parts + blockIdx.x] = all;
 }
-template <int BLOCK>
-__global__ __launch_bounds__(BLOCK) void norm_join_kernel(NormArgs a)
+__global__ __launch_bounds__(64) void norm_join_kernel(NormArgs a)
 {
-    __shared__ double scratch[BLOCK / 64];
     const int i = blockIdx.x;
     double sum = 0.0;
-    for (int p = threadIdx.x; p < a.parts; p += BLOCK) sum += a.partial[(size_t)i * a.parts + p];
-    sum = block_sum<BLOCK>(sum, scratch);
+    for (int p = threadIdx.x; p < a.parts; p += 64) sum += a.partial[(size_t)i * a.parts + p];
+    sum = wave_sum(sum);
     if (threadIdx.x == 0) write_norm(a, i, sum);
 }
 
@@ -325,24 +507,34 @@ static int check_replicas(const char *name, const void *G, int dtype, int P, siz
     if (P < 1) return fail(EASGD_EINVAL, "%s: P must be >= 1, got %d", name, P);
     if (N == 0) return fail(EASGD_EINVAL, "%s: N must be >= 1", name);
     if (ld < N) return fail(EASGD_EINVAL, "%s: ld (%zu) < N (%zu)", name, ld, N);
+    if (P > 65535) return fail(EASGD_ERANGE, "%s: more than 65535 workers", name);
     if (N > MOST_N || ld > ((size_t)1 << 60) / (size_t)P) return fail(EASGD_ERANGE, "%s: N or P * ld too large", name);
     if (!aligned_to(G, dtype_bytes(dtype))) return fail(EASGD_EINVAL, "%s: G must be aligned to its elements (%zu bytes)", name, dtype_bytes(dtype));
     return EASGD_OK;
 }
 
-static constexpr int NORM_BLOCK = 256;
-static constexpr size_t NORM_PART = 8192;
-static int norm_parts(int P, size_t N)
+// Rows of up to NORM_ONE bytes take one block of 1024 threads each and one launch.
+static constexpr int NORM_BLOCK = 256, NORM_DEEP = 8, NORM_BLOCKS = 2048;
+static constexpr size_t NORM_ONE = (size_t)256 << 10, NORM_TILE = (size_t)NORM_BLOCK * NORM_DEEP * 16;
+static int norm_parts(int P, size_t bytes)
 {
-    const size_t most = (N + NORM_PART - 1) / NORM_PART, want = (4096 + P - 1) / P;
+    if (bytes <= NORM_ONE) return 1;
+    const size_t most = (bytes + NORM_TILE - 1) / NORM_TILE, want = (size_t)((NORM_BLOCKS + P - 1) / P);
     return (int)(want < most ? want : most);
 }
 
-template <int GT, bool EIGHT, bool WIDE> static void launch_adamw(const AdamwArgs &a, hipStream_t s)
+template <int GT, bool EIGHT, bool CENTER, bool NT> static void launch_tiles(const AdamwArgs &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)((a.blocks + 3) / 4));
-    if (a.Wc) EASGD_LAUNCH((adamw_kernel<GT, EIGHT, true, WIDE>), grid, dim3(256), 0, s, a);
-    else EASGD_LAUNCH((adamw_kernel<GT, EIGHT, false, WIDE>), grid, dim3(256), 0, s, a);
+    if (a.blocks >= (size_t)64 * num_cus())
+        EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, NT, 4, true>), dim3((unsigned)TileMap<4, true>::tiles(a.blocks * 64)), dim3(256), 0, s, a);
+    else EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, NT, 1, false>), dim3((unsigned)TileMap<1, false>::tiles(a.blocks * 64)), dim3(256), 0, s, a);
+}
+template <int GT, bool EIGHT, bool CENTER> static void launch_adamw(const AdamwArgs &a, bool wide, hipStream_t s)
+{
+    const size_t moved = (size_t)a.P * a.N * (8 + (GT == EASGD_F32 ? 4 : 2) + (EIGHT ? 4 : 16));
+    if (!wide) EASGD_LAUNCH((adamw_each_kernel<GT, EIGHT, CENTER>), dim3((unsigned)((a.blocks + 3) / 4), CENTER ? 1 : (unsigned)a.P), dim3(256), 0, s, a);
+    else if (update_nontemporal(moved)) launch_tiles<GT, EIGHT, CENTER, true>(a, s);
+    else launch_tiles<GT, EIGHT, CENTER, false>(a, s);
 }
 
 template <bool EIGHT> static int adamw(const char *name, AdamwArgs a, int dtype, void *stream)
@@ -357,7 +549,7 @@ template <bool EIGHT> static int adamw(const char *name, AdamwArgs a, int dtype,
         return fail(EASGD_EINVAL, "%s: ends, step_at must be 8-byte, rates, decays 4-byte aligned", name);
     if (!(a.beta1 >= 0.f && a.beta1 < 1.f) || !(a.beta2 >= 0.f && a.beta2 < 1.f))
         return fail(EASGD_EINVAL, "%s: beta1 and beta2 must be in [0, 1), got %g and %g", name, (double)a.beta1, (double)a.beta2);
-    if (!(a.eps > 0.f) || std::isinf(a.eps)) return fail(EASGD_EINVAL, "%s: eps must be finite and above 0, got %g", name, (double)a.eps);
+    if (!(a.eps >= 1e-30f && a.eps <= 1e30f)) return fail(EASGD_EINVAL, "%s: eps must be in [1e-30, 1e30], got %g", name, (double)a.eps);
     if (!std::isfinite(a.eta) || !std::isfinite(a.rho) || !std::isfinite(a.decay)) return fail(EASGD_EINVAL, "%s: eta, rho and decay must be finite", name);
     if (!a.Wc && a.rho != 0.f) return fail(EASGD_EINVAL, "%s: rho = %g needs a center", name, (double)a.rho);
     if (!a.step_at && a.step < 1) return fail(EASGD_EINVAL, "%s: step must be >= 1, got %lld", name, a.step);
@@ -369,8 +561,8 @@ template <bool EIGHT> static int adamw(const char *name, AdamwArgs a, int dtype,
     const hipStream_t s = static_cast<hipStream_t>(stream);
     by_dtype(dtype, [&](auto gt) {
         constexpr int GT = decltype(gt)::value;
-        if (wide) launch_adamw<GT, EIGHT, true>(a, s);
-        else launch_adamw<GT, EIGHT, false>(a, s);
+        if (a.Wc) launch_adamw<GT, EIGHT, true>(a, wide, s);
+        else launch_adamw<GT, EIGHT, false>(a, wide, s);
     });
     return check_launch(name);
 }
@@ -383,7 +575,7 @@ size_t easgd_grad_norms_workspace_bytes(int P, size_t N)
 {
     using namespace easgd;
     if (P < 1 || N == 0 || N > MOST_N) return 0;
-    const int parts = norm_parts(P, N);
+    const int parts = norm_parts(P, N * 4);             // fp32 rows have the most parts
     return parts == 1 ? 0 : ((size_t)P * parts * sizeof(double) + 255) / 256 * 256;
 }
 
@@ -396,16 +588,17 @@ int easgd_grad_norms(const void *G, int dtype, int P, size_t N, size_t ld, float
     if (!norm) return fail(EASGD_EINVAL, "%s: NULL pointer", name);
     if (!aligned_to(norm, 4) || !aligned_to(clip, 4)) return fail(EASGD_EINVAL, "%s: norm, clip must be 4-byte aligned", name);
     if (!(max_norm > 0.f)) return fail(EASGD_EINVAL, "%s: max_norm must be above 0, got %g", name, (double)max_norm);
-    if (P > 65535) return fail(EASGD_ERANGE, "%s: more than 65535 workers", name);
     if (int rc = check_workspace(name, workspace, workspace_bytes, easgd_grad_norms_workspace_bytes(P, N))) return rc;
     clear_error();
-    const int parts = norm_parts(P, N);
-    const NormArgs a = {G, P, N, ld, max_norm, norm, clip, parts, (N + parts - 1) / parts, static_cast<double *>(workspace)};
+    const int parts = norm_parts(P, N * dtype_bytes(dtype));
+    const NormArgs a = {G, P, N, ld, max_norm, norm, clip, parts, static_cast<double *>(workspace)};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     by_dtype(dtype, [&](auto gt) {
-        EASGD_LAUNCH((norm_parts_kernel<decltype(gt)::value, NORM_BLOCK>), dim3((unsigned)parts, (unsigned)P), dim3(NORM_BLOCK), 0, s, a);
+        constexpr int GT = decltype(gt)::value;
+        if (parts == 1) EASGD_LAUNCH((norm_parts_kernel<GT, 1024, 4>), dim3(1, (unsigned)P), dim3(1024), 0, s, a);
+        else EASGD_LAUNCH((norm_parts_kernel<GT, NORM_BLOCK, NORM_DEEP>), dim3((unsigned)parts, (unsigned)P), dim3(NORM_BLOCK), 0, s, a);
     });
-    if (parts > 1) EASGD_LAUNCH((norm_join_kernel<NORM_BLOCK>), dim3((unsigned)P), dim3(NORM_BLOCK), 0, s, a);
+    if (parts > 1) EASGD_LAUNCH(norm_join_kernel, dim3((unsigned)P), dim3(64), 0, s, a);
     return check_launch(name);
 }
 
