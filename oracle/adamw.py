@@ -83,9 +83,7 @@ def encode(m, v, worker, step, seed):
     for b in range(blocks):
         at = slice(b * BLOCK, min((b + 1) * BLOCK, N))
         code, ms[b] = _encode(np.abs(m[at]), 3, 7, r[at])
-        mc[at] = code | ((m[at] < 0) & np.isfinite(ms[b])).astype(np.uint8) << 7
-        if np.isnan(ms[b]):
-            mc[at] = (m[at] < 0).astype(np.uint8) << 7
+        mc[at] = code | np.signbit(m[at]).astype(np.uint8) << 7
         code, vs[b] = _encode(v[at], 2, 14, r[at])
         vc[at] = np.maximum(code, (v[at] > 0) & np.isfinite(vs[b]))
     return mc, vc, ms, vs

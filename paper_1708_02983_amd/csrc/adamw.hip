@@ -82,7 +82,7 @@ struct TensorWalk {
     __device__ __forceinline__ float decay() const { return at < a.tensors ? a.decays[at] : a.decay; }
 };
 
-// The rates (eta among them) and decays of a lane's four parameters in a block of 256; nearly always one tensor has the whole block.
+// What multiplies m / (sqrt(v) + eps) and w of a lane's four parameters in a block of 256; nearly always one tensor has the whole block.
 __device__ __forceinline__ bool in_one_tensor(const TensorWalk &tensor, size_t block) { return tensor.end() >= block * 256 + 256; }
 struct Pace {
     float rate[4], decay[4];
@@ -101,8 +101,9 @@ struct Pace {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             if (!one) tensor.to(j + q);
-            rate[q] = n.eta * tensor.rate();
-            decay[q] = tensor.decay();
+            const float eta = n.eta * tensor.rate();
+            rate[q] = eta * n.by1;
+            decay[q] = eta * tensor.decay();
         }
     }
 };
@@ -114,8 +115,9 @@ template <int GROUPS> struct TilePace {
     {
         const TensorWalk tensor(a, block * 256);
         one[q] = in_one_tensor(tensor, block);
-        rate[q] = n.eta * tensor.rate();
-        decay[q] = tensor.decay();
+        const float eta = n.eta * tensor.rate();
+        rate[q] = eta * n.by1;
+        decay[q] = eta * tensor.decay();
     }
     __device__ __forceinline__ Pace of(const AdamwArgs &a, const StepNumbers &n, int q, size_t j) const
     {
@@ -132,14 +134,23 @@ __device__ __forceinline__ void adamw_moments(float &m, float &v, float g, const
     m = m * n.beta1 + g * n.rest1;
     v = v * n.beta2 + (g * n.rest2) * g;
 }
-// What a parameter moves by: eta (m' / (sqrt(v') + eps) + decay w)
-__device__ __forceinline__ float adamw_move(float w, float m, float v, float eta, float decay, const StepNumbers &n)
+// What four parameters move by: eta (m / (1 - b1^t) / (sqrt(v / (1 - b2^t)) + eps) + decay w).  The hardware's root and reciprocal are right to
+// one unit; it takes subnormal numbers for 0, so roots of what is below 2^-64 are taken of 2^64 times it.  eps is at least 1e-30: the
+// reciprocal is of a normal number.
+__device__ __forceinline__ void adamw_move(const float (&w)[4], const float (&m)[4], const float (&v)[4], const Pace &pace, const StepNumbers &n, float (&move)[4])
 {
-    // The hardware's root and reciprocal are right to one unit; roots of what is below 2^-64 are taken of 2^64 times it, since the instruction
-    // has no subnormal numbers.  d is at least eps, so its reciprocal is a normal number.
-    const bool small = v < 0x1p-64f;
-    const float root = __builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v) * (small ? n.by2 * 0x1p-32f : n.by2);
-    return eta * fmaf(decay, w, m * (n.by1 * __builtin_amdgcn_rcpf(root + n.eps)));
+    float root[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) root[q] = __builtin_amdgcn_sqrtf(v[q]);
+    if (__any(fminf(fminf(v[0], v[1]), fminf(v[2], v[3])) < 0x1p-64f)) {         // uniform
+#pragma unroll
+        for (int q = 0; q < 4; ++q) root[q] = v[q] < 0x1p-64f ? __builtin_amdgcn_sqrtf(v[q] * 0x1p64f) * 0x1p-32f : root[q];
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const float d = fmaf(root[q], n.by2, n.eps);
+        move[q] = fmaf(pace.decay[q], w[q], m[q] * (pace.rate[q] * __builtin_amdgcn_rcpf(d)));
+    }
 }
 
 // ---- moments in 8 bits -----------------------------------------------------------------------------------------------------
@@ -161,7 +172,7 @@ __device__ __forceinline__ unsigned dither_key(unsigned seed, unsigned worker, u
 }
 // bits: of the type's fraction; top: exponent of the largest number's place
 template <int BITS, int TOP> struct EightBits {
-    static constexpr float UNIT = BITS == 2 ? 0x1p-112f : 0x1p-120f;
+    static constexpr int UNIT = BITS == 2 ? -112 : -120;
     unsigned scale;                    // biased exponent of the block's power of two
     bool there;                        // neither infinite nor NaN in the block
     __device__ __forceinline__ explicit EightBits(unsigned most)        // the largest magnitude of the block, as bits
@@ -169,16 +180,32 @@ template <int BITS, int TOP> struct EightBits {
         there = most < 0x7f800000u;
         scale = (unsigned)max((int)(most >> 23) - TOP, 1);
     }
+    // (codes under the scale NaN say nothing)
     __device__ __forceinline__ float stored() const { return there ? __uint_as_float(scale << 23) : NAN; }
-    __device__ __forceinline__ unsigned code(float magnitude, unsigned dither) const
+    // fp32 bits whose upper part, from bit 23 - BITS on, is the code (of a magnitude), random: 20 bits
+    __device__ __forceinline__ unsigned code(float x, unsigned random) const
     {
-#pragma clang fp contract(off)
-        const float y = magnitude * __uint_as_float((254u - scale) << 23) * UNIT;
-        return there ? (__float_as_uint(y) + (dither << (7 - BITS)) + (1u << (6 - BITS))) >> (23 - BITS) : 0u;
+        return __float_as_uint(__builtin_amdgcn_ldexpf(x, 127 + UNIT - (int)scale)) + (random << (3 - BITS));
     }
 };
 using MomentM = EightBits<3, 7>;
 using MomentS = EightBits<2, 14>;
+
+// Codes of four moments in a word, from the sums that code() gave.
+__device__ __forceinline__ unsigned pack_m(const unsigned (&y)[4])
+{
+    unsigned t[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) t[q] = (y[q] << 4 & 0x7fffffffu) | (y[q] & 0x80000000u);          // the code in the upper byte
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(t[3], t[2], 0x0c0c0703u), __builtin_amdgcn_perm(t[1], t[0], 0x0c0c0703u), 0x05040100u);
+}
+__device__ __forceinline__ unsigned pack_s(const unsigned (&y)[4], const float (&v)[4])
+{
+    unsigned t[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) t[q] = max(y[q] >> 21, min(__float_as_uint(v[q]), 1u));           // what is above 0 stays above 0
+    return (t[3] << 8 | t[2]) << 16 | (t[1] << 8 | t[0]);
+}
 
 // the largest magnitude's bits over a wavefront: within rows of 16 lanes by data-parallel moves, then the four rows as scalars
 __device__ __forceinline__ unsigned wave_max_bits(unsigned v)
@@ -194,6 +221,7 @@ __device__ __forceinline__ unsigned wave_max_bits(unsigned v)
 }
 
 // ---- four consecutive parameters of a lane ------------------------------------------------------------------------------------
+typedef float Four __attribute__((ext_vector_type(4)));
 // How they are accessed: at once past the caches (what is read once and written once), at once, or element by element with a look at the
 // row's end (rows at other alignments, and the last 256 parameters).
 enum { ACCESS_STREAM, ACCESS_WIDE, ACCESS_EACH };
@@ -227,20 +255,39 @@ template <typename T, int ACCESS> __device__ __forceinline__ void store_four(T *
     }
 }
 
-// A worker's share of 256 parameters, four of them a lane's, between load() and store().
+// four codes in a word
+template <int ACCESS> __device__ __forceinline__ unsigned load_codes(const unsigned char *p, size_t j, size_t N)
+{
+    if constexpr (ACCESS == ACCESS_EACH) {
+        unsigned char c[4];
+        load_four<unsigned char, ACCESS>(p, j, N, c);
+        return (unsigned)c[3] << 24 | (unsigned)c[2] << 16 | (unsigned)c[1] << 8 | c[0];
+    } else if constexpr (ACCESS == ACCESS_STREAM) return __builtin_nontemporal_load(reinterpret_cast<const unsigned *>(p + j));
+    else return *reinterpret_cast<const unsigned *>(p + j);
+}
+template <int ACCESS> __device__ __forceinline__ void store_codes(unsigned char *p, size_t j, size_t N, unsigned codes)
+{
+    if constexpr (ACCESS == ACCESS_EACH) {
+        const unsigned char c[4] = {(unsigned char)codes, (unsigned char)(codes >> 8), (unsigned char)(codes >> 16), (unsigned char)(codes >> 24)};
+        store_four<unsigned char, ACCESS>(p, j, N, c);
+    } else if constexpr (ACCESS == ACCESS_STREAM) __builtin_nontemporal_store(codes, reinterpret_cast<unsigned *>(p + j));
+    else *reinterpret_cast<unsigned *>(p + j) = codes;
+}
+
+// A worker's share of 256 parameters, four of them a lane's, between loads and stores.
 template <int GT, bool EIGHT, int ACCESS> struct Worker {
     using Grad = typename LogitType<GT>::Stored;
     float w[4], m[4], v[4];
     Grad g[4];
-    unsigned char mc[4], vc[4];
+    unsigned mc, vc;                   // four codes each
     float ms, vs;                      // scales, the same for all lanes
     __device__ __forceinline__ void load_moments(const AdamwArgs &a, int i, size_t j)
     {
         const size_t row = (size_t)i * a.ld;
         load_four<Grad, ACCESS>((const Grad *)a.G + row, j, a.N, g);
         if constexpr (EIGHT) {
-            load_four<unsigned char, ACCESS>((const unsigned char *)a.M + row, j, a.N, mc);
-            load_four<unsigned char, ACCESS>((const unsigned char *)a.S + row, j, a.N, vc);
+            mc = load_codes<ACCESS>((const unsigned char *)a.M + row, j, a.N);
+            vc = load_codes<ACCESS>((const unsigned char *)a.S + row, j, a.N);
             const size_t block = (size_t)i * a.blocks + __builtin_amdgcn_readfirstlane((unsigned)(j >> 8));
             ms = a.M_scale[block];
             vs = a.S_scale[block];
@@ -255,43 +302,50 @@ template <int GT, bool EIGHT, int ACCESS> struct Worker {
     {
         if constexpr (EIGHT) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                m[q] = __builtin_amdgcn_cvt_f32_fp8((int)mc[q], 0) * ms;
-                v[q] = __builtin_amdgcn_cvt_f32_bf8((int)vc[q], 0) * vs;
+            for (int q = 0; q < 4; q += 2) {
+                const auto pm = q ? __builtin_amdgcn_cvt_pk_f32_fp8((int)mc, true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)mc, false);
+                const auto pv = q ? __builtin_amdgcn_cvt_pk_f32_bf8((int)vc, true) : __builtin_amdgcn_cvt_pk_f32_bf8((int)vc, false);
+                m[q] = pm[0] * ms;
+                m[q + 1] = pm[1] * ms;
+                v[q] = pv[0] * vs;
+                v[q + 1] = pv[1] * vs;
             }
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            adamw_moments(m[q], v[q], clip * LogitType<GT>::widen(g[q]), n);
-            move[q] = adamw_move(w[q], m[q], v[q], pace.rate[q], pace.decay[q], n);
-        }
+        for (int q = 0; q < 4; ++q) adamw_moments(m[q], v[q], clip * LogitType<GT>::widen(g[q]), n);
+        adamw_move(w, m, v, pace, n, move);
         if constexpr (EIGHT) {
             unsigned most_m = 0, most_v = 0;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const bool in = ACCESS != ACCESS_EACH || j + q < a.N;
-                most_m = max(most_m, in ? __float_as_uint(m[q]) & 0x7fffffffu : 0u);
-                most_v = max(most_v, in ? __float_as_uint(v[q]) & 0x7fffffffu : 0u);
+                most_m = max(most_m, in ? __float_as_uint(m[q]) << 1 : 0u);
+                most_v = max(most_v, in ? __float_as_uint(v[q]) : 0u);           // v >= 0, or NaN of either sign
             }
-            const MomentM em(wave_max_bits(most_m));
+            const MomentM em(wave_max_bits(most_m) >> 1);
             const MomentS es(wave_max_bits(most_v));
             ms = em.stored();
             vs = es.stored();
-            const unsigned h[2] = {mix((unsigned)(j >> 2) ^ dither_key(a.seed, i, n.step, 0)), mix((unsigned)(j >> 2) ^ dither_key(a.seed, i, n.step, 1))};
+            unsigned ym[4], yv[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const unsigned dither = q & 1 ? h[q >> 1] >> 16 : h[q >> 1] & 0xffffu;
-                mc[q] = (unsigned char)(em.code(fabsf(m[q]), dither) | (m[q] < 0.f ? 0x80u : 0u));
-                vc[q] = (unsigned char)max(es.code(v[q], dither), v[q] > 0.f ? 1u : 0u);
+            for (int q = 0; q < 4; q += 2) {
+                const unsigned h = mix((unsigned)(j >> 2) ^ dither_key(a.seed, i, n.step, q >> 1));
+                const unsigned low = ((h & 0xffffu) << 4) + 8u, high = (h >> 16 << 4) + 8u;
+                ym[q] = em.code(m[q], low);
+                ym[q + 1] = em.code(m[q + 1], high);
+                yv[q] = es.code(v[q], low);
+                yv[q + 1] = es.code(v[q + 1], high);
             }
+            mc = pack_m(ym);
+            vc = pack_s(yv, v);
         }
     }
     __device__ __forceinline__ void store_moments(const AdamwArgs &a, int i, size_t j)
     {
         const size_t row = (size_t)i * a.ld;
         if constexpr (EIGHT) {
-            store_four<unsigned char, ACCESS>((unsigned char *)a.M + row, j, a.N, mc);
-            store_four<unsigned char, ACCESS>((unsigned char *)a.S + row, j, a.N, vc);
+            store_codes<ACCESS>((unsigned char *)a.M + row, j, a.N, mc);
+            store_codes<ACCESS>((unsigned char *)a.S + row, j, a.N, vc);
             const size_t block = (size_t)i * a.blocks + __builtin_amdgcn_readfirstlane((unsigned)(j >> 8));
             if ((threadIdx.x & 63) == 0) {
                 a.M_scale[block] = ms;
@@ -341,14 +395,82 @@ __device__ __forceinline__ void adamw_block(const AdamwArgs &a, const StepNumber
     }
 }
 
-// ---- replicas at any alignment: a wavefront per 256 parameters, worker by worker (by its own without a center: blockIdx.y) ------------
-template <int GT, bool EIGHT, bool CENTER>
-__global__ __launch_bounds__(256) void adamw_each_kernel(AdamwArgs a)
+// ---- no center: a wavefront per 256 parameters of a worker (blockIdx.y) -------------------------------------------------------------------
+template <int GT, bool EIGHT, int ACCESS>
+__global__ __launch_bounds__(256) void adamw_own_kernel(AdamwArgs a)
 {
     const size_t block = (size_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (block >= a.blocks) return;                      // wavefronts of a block have nothing in common
     const StepNumbers n(a);
-    adamw_block<GT, EIGHT, CENTER, ACCESS_EACH>(a, n, block, CENTER ? 0 : (int)blockIdx.y, CENTER ? a.P : (int)blockIdx.y + 1);
+    const int i = (int)blockIdx.y;
+    if (ACCESS != ACCESS_EACH && block < a.N / 256) adamw_block<GT, EIGHT, false, ACCESS>(a, n, block, i, i + 1);
+    else adamw_block<GT, EIGHT, false, ACCESS_EACH>(a, n, block, i, i + 1);
+}
+
+// ---- a center and few parameters: 256 of them a block, whose wavefronts take the workers in turn ------------------------------------------
+// What the workers are apart from the center meets in LDS, SPLIT_ROOM workers at a time, and is added in ascending order: the same sums as
+// worker by worker.
+static constexpr int SPLIT_ROOM = 16;
+template <int GT, bool EIGHT, int ACCESS, int WAVES>
+__device__ __forceinline__ void adamw_split_block(const AdamwArgs &a, const StepNumbers &n, size_t block, Four (&apart)[SPLIT_ROOM][64])
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const size_t j = block * 256 + (size_t)lane * 4;
+    const Pace pace(a, n, block, j);
+    constexpr int SPLIT_AHEAD = EIGHT ? 1 : 2;
+    constexpr int CENTER_ACCESS = ACCESS == ACCESS_EACH ? ACCESS_EACH : ACCESS_WIDE;
+    float c[4];
+    load_four<float, CENTER_ACCESS>(a.Wc, j, a.N, c);
+    Four sum = {0.f, 0.f, 0.f, 0.f};
+    for (int first = 0; first < a.P; first += SPLIT_ROOM) {
+        const int end = min(first + SPLIT_ROOM, a.P);
+        for (int i0 = first + wave; i0 < end; i0 += SPLIT_AHEAD * WAVES) {
+            Worker<GT, EIGHT, ACCESS> worker[SPLIT_AHEAD];
+            float clip[SPLIT_AHEAD];
+#pragma unroll
+            for (int u = 0; u < SPLIT_AHEAD; ++u) {
+                const int i = i0 + u * WAVES;
+                if (i >= end) break;
+                clip[u] = a.clip ? a.clip[i] : 1.f;
+                if (clip[u] != 0.f) worker[u].load_moments(a, i, j);
+                worker[u].load_parameters(a, i, j);
+            }
+#pragma unroll
+            for (int u = 0; u < SPLIT_AHEAD; ++u) {
+                const int i = i0 + u * WAVES;
+                if (i >= end) break;
+                float move[4] = {};
+                if (clip[u] != 0.f) {
+                    worker[u].step(a, i, j, clip[u], pace, n, move);
+                    worker[u].store_moments(a, i, j);
+                }
+                Four d;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    d[q] = worker[u].w[q] - c[q];
+                    worker[u].w[q] -= fmaf(n.alpha, d[q], move[q]);
+                }
+                apart[i - first][lane] = d;
+                worker[u].store_parameters(a, i, j);
+            }
+        }
+        __syncthreads();
+        if (wave == 0)
+            for (int i = first; i < end; ++i) sum += apart[i - first][lane];
+        __syncthreads();
+    }
+    if (wave != 0) return;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) c[q] = fmaf(n.alpha, sum[q], c[q]);
+    store_four<float, CENTER_ACCESS>(a.Wc, j, a.N, c);
+}
+template <int GT, bool EIGHT, int ACCESS, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void adamw_split_kernel(AdamwArgs a)
+{
+    __shared__ Four apart[SPLIT_ROOM][64];
+    const StepNumbers n(a);
+    if (ACCESS != ACCESS_EACH && blockIdx.x < a.N / 256) adamw_split_block<GT, EIGHT, ACCESS, WAVES>(a, n, blockIdx.x, apart);      // uniform
+    else adamw_split_block<GT, EIGHT, ACCESS_EACH, WAVES>(a, n, blockIdx.x, apart);
 }
 
 // ---- many parameters: GROUPS blocks of 256 a wavefront, all requests of a worker under way at once -------------------------------------
@@ -389,7 +511,6 @@ __global__ __launch_bounds__(256) void adamw_tile_kernel(AdamwArgs a)
         }
 #pragma unroll
         for (int q = 0; q < GROUPS; ++q) worker[q].load_parameters(a, i, j[q]);
-        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int q = 0; q < GROUPS; ++q) {
             float move[4] = {};
@@ -404,7 +525,6 @@ __global__ __launch_bounds__(256) void adamw_tile_kernel(AdamwArgs a)
                 worker[q].w[e] -= move[e];
             }
         }
-        __builtin_amdgcn_sched_barrier(0);
         if (clip != 0.f) {
 #pragma unroll
             for (int q = 0; q < GROUPS; ++q) worker[q].store_moments(a, i, j[q]);
@@ -523,18 +643,27 @@ static int norm_parts(int P, size_t bytes)
     return (int)(want < most ? want : most);
 }
 
-template <int GT, bool EIGHT, bool CENTER, bool NT> static void launch_tiles(const AdamwArgs &a, hipStream_t s)
-{
-    if (a.blocks >= (size_t)64 * num_cus())
-        EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, NT, 4, true>), dim3((unsigned)TileMap<4, true>::tiles(a.blocks * 64)), dim3(256), 0, s, a);
-    else EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, NT, 1, false>), dim3((unsigned)TileMap<1, false>::tiles(a.blocks * 64)), dim3(256), 0, s, a);
-}
+// Tiles of 8 x 61 M, us (1 / 2 / 4 blocks of 256 a wavefront): moments in 32 bits 2306 / 2097 / 2024, in 8 bits 1436 / 1377 / 1489: these need more wavefronts
+// under way, whose arithmetic hides behind each other's loads.
 template <int GT, bool EIGHT, bool CENTER> static void launch_adamw(const AdamwArgs &a, bool wide, hipStream_t s)
 {
+    constexpr int GROUPS = EIGHT ? 2 : 4;
     const size_t moved = (size_t)a.P * a.N * (8 + (GT == EASGD_F32 ? 4 : 2) + (EIGHT ? 4 : 16));
-    if (!wide) EASGD_LAUNCH((adamw_each_kernel<GT, EIGHT, CENTER>), dim3((unsigned)((a.blocks + 3) / 4), CENTER ? 1 : (unsigned)a.P), dim3(256), 0, s, a);
-    else if (update_nontemporal(moved)) launch_tiles<GT, EIGHT, CENTER, true>(a, s);
-    else launch_tiles<GT, EIGHT, CENTER, false>(a, s);
+    if (wide && a.blocks >= (size_t)64 * num_cus()) {
+        const dim3 grid((unsigned)TileMap<GROUPS, true>::tiles(a.blocks * 64));
+        if (update_nontemporal(moved)) EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, true, GROUPS, true>), grid, dim3(256), 0, s, a);
+        else EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, false, GROUPS, true>), grid, dim3(256), 0, s, a);
+    } else if constexpr (CENTER) {
+        const dim3 grid((unsigned)a.blocks);
+        if (!wide) EASGD_LAUNCH((adamw_split_kernel<GT, EIGHT, ACCESS_EACH, 4>), grid, dim3(256), 0, s, a);
+        else if (update_nontemporal(moved)) EASGD_LAUNCH((adamw_split_kernel<GT, EIGHT, ACCESS_STREAM, 4>), grid, dim3(256), 0, s, a);
+        else EASGD_LAUNCH((adamw_split_kernel<GT, EIGHT, ACCESS_WIDE, 4>), grid, dim3(256), 0, s, a);
+    } else {
+        const dim3 grid((unsigned)((a.blocks + 3) / 4), (unsigned)a.P);
+        if (!wide) EASGD_LAUNCH((adamw_own_kernel<GT, EIGHT, ACCESS_EACH>), grid, dim3(256), 0, s, a);
+        else if (update_nontemporal(moved)) EASGD_LAUNCH((adamw_own_kernel<GT, EIGHT, ACCESS_STREAM>), grid, dim3(256), 0, s, a);
+        else EASGD_LAUNCH((adamw_own_kernel<GT, EIGHT, ACCESS_WIDE>), grid, dim3(256), 0, s, a);
+    }
 }
 
 template <bool EIGHT> static int adamw(const char *name, AdamwArgs a, int dtype, void *stream)
