@@ -35,6 +35,14 @@ template <int DT> struct GradRow {
         for (int i = 0; i < VEC; ++i)
             if ((unsigned)(j + i) < (unsigned)V) row[j + i] = Type::narrow(x[i]);
     }
+    // the gradient of slot `from` + thread, which is full, where the alignments agree: a uniform address and an offset
+    __device__ __forceinline__ void store_at(int from, const float (&x)[VEC]) const
+    {
+        typedef unsigned Four __attribute__((ext_vector_type(4)));
+        const uint4 p = Type::pack(x);
+        const Four v = {p.x, p.y, p.z, p.w};
+        __builtin_nontemporal_store(v, reinterpret_cast<Four *>(row + from * VEC - shift) + (unsigned)threadIdx.x);
+    }
     __device__ __forceinline__ void put(int j, float d) const { row[j] = Type::narrow(d); }
     // 0 for slots first + thread, first + thread + block, ... below last
     __device__ __forceinline__ void clear(int last, int block, int first = 0) const

@@ -39,6 +39,7 @@ struct ScoreArgs {
     unsigned long long *words;     // [rows][segments][k]: the first k of every part (0: none left)
 };
 
+static constexpr float LN2 = 0.693147180559945309f;
 static constexpr double LN2_64 = 0.69314718055994530942;
 // the exponent that stands for any smaller one in e_j y_j, where e_j is 0: a masked place must not make it 0 times infinity
 static constexpr float LEAST = -256.f;
@@ -214,17 +215,13 @@ template <int DT, int BLOCK, int DEEP, typename F> __device__ __forceinline__ vo
 
 template <int BLOCK> struct JoinLds {
     float4 part[BLOCK / 64];
-    unsigned before[BLOCK / 64];
 };
-// the sums of a block's wavefronts and its count, for every thread
-template <int BLOCK, typename S> __device__ __forceinline__ float4 block_sums(const S &sums, unsigned before, JoinLds<BLOCK> &lds, const Scales &q)
+// the sums of a block's wavefronts (w: of this one; the last number counts), for every thread
+template <int BLOCK> __device__ __forceinline__ float4 join_waves(float4 w, JoinLds<BLOCK> &lds, const Scales &q)
 {
     constexpr int WAVES = BLOCK / 64;
-    float4 w = sums.of_wave();
-    if ((threadIdx.x & 63) == 0) {
-        w.w = __uint_as_float(before);
-        lds.part[threadIdx.x >> 6] = w;
-    }
+    __syncthreads();                                    // everyone is done with the sums before these
+    if ((threadIdx.x & 63) == 0) lds.part[threadIdx.x >> 6] = w;
     __syncthreads();
     w = lds.part[threadIdx.x & (WAVES - 1)];
     unsigned n = __float_as_uint(w.w);
@@ -240,6 +237,12 @@ template <int BLOCK, typename S> __device__ __forceinline__ float4 block_sums(co
     }
     w.w = __uint_as_float(n);
     return w;
+}
+template <int BLOCK, typename S> __device__ __forceinline__ float4 block_sums(const S &sums, unsigned before, JoinLds<BLOCK> &lds, const Scales &q)
+{
+    float4 w = sums.of_wave();
+    w.w = __uint_as_float(before);
+    return join_waves<BLOCK>(w, lds, q);
 }
 
 template <int DT, int BLOCK, bool ENTROPY, bool RANK>
@@ -372,51 +375,71 @@ __global__ __launch_bounds__(BLOCK) void score_top_join_kernel(ScoreArgs a)
 }
 
 // ---- gradients -----------------------------------------------------------------------------------------------------------------
-// The gradient of a row from its reference, sum and entropy, as a function of the logit.
+// The gradient of a row from its reference, sum and mean exponent (u / s), as a function of the logit.  log q[j] + H is ln2 (y_j - u / s):
+// no logarithm is taken, and nothing here needs 64 bits.
 template <int VEC> struct TokenSlope {
     Reference<VEC> at;
     float a, b, of_token;
     bool none;                 // nothing to learn: the gradient is 0
     // differences: of() is not called; exponents are those of exact differences to m
-    __device__ __forceinline__ TokenSlope(const ScoreArgs &args, size_t r, bool padding, float m, float sum, double entropy, float z_token, const Scales &q,
+    __device__ __forceinline__ TokenSlope(const ScoreArgs &args, size_t r, bool padding, float m, float sum, float mean, float z_token, const Scales &q,
                                           bool differences = false)
         : at(uniform(m), q)
     {
         none = padding || sum == 0.f;
-        const double scale = (double)args.scale, T = (double)args.temperature;
-        double gl, gh;
+        float gl, gh;
         if (args.loss) {
-            gl = -scale * (args.weight ? (double)args.weight[r] : 1.0);
-            gh = -scale * (double)args.bonus;
+            gl = -args.scale * (args.weight ? args.weight[r] : 1.f);
+            gh = -args.scale * args.bonus * LN2;
         } else {
-            gl = args.dlogprob ? scale * (double)args.dlogprob[r] : 0.0;
-            gh = args.dentropy ? scale * (double)args.dentropy[r] : 0.0;
+            gl = args.dlogprob ? args.scale * args.dlogprob[r] : 0.f;
+            gh = args.dentropy ? args.scale * args.dentropy[r] * LN2 : 0.f;
         }
-        const double log_s = log((double)sum), lost = differences ? 0.0 : (double)at.lost, factor = 1.0 / ((double)sum * T);
-        const float f = differences ? 1.f : exp2_fast(-at.lost);
-        a = uniform((float)((-gl - gh * (entropy - log_s - LN2_64 * lost)) * factor) * f);
-        b = uniform((float)(-gh * LN2_64 * factor) * f);
-        const double log_q = ((double)z_token - (double)m) / T - log_s, p = exp(log_q);
-        of_token = uniform((float)((gl * (1.0 - p) - (p > 0.0 ? gh * p * (log_q + entropy) : 0.0)) / T));
+        const float by_T = 1.f / args.temperature, by_sum = 1.f / sum;
+        const float lost = differences ? 0.f : at.lost, factor = by_T * by_sum * (differences ? 1.f : exp2_fast(-at.lost));
+        a = uniform(fmaf(gh, mean + lost, -gl) * factor);
+        b = uniform(-gh * factor);
+        const float y = (z_token - m) * q.c, p = exp2_fast(y) * by_sum;
+        of_token = uniform((gl * (1.f - p) - (p > 0.f ? gh * p * (y - mean) : 0.f)) * by_T);
         if (isnan(sum)) of_token = NAN;
     }
-    template <bool ENTROPY> __device__ __forceinline__ void of(float (&x)[VEC], const Scales &q) const
+    // clamped: there may be masked places among them
+    template <bool ENTROPY, bool CLAMPED = true> __device__ __forceinline__ void of(float (&x)[VEC]) const
     {
-        if (at.by_difference()) {                       // uniform, and rare
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const float y = (x[i] - at.ref) * q.c;
-                x[i] = exp2_fast(y) * fmaf(b, fmaxf(y, LEAST), a);
-            }
-            return;
-        }
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
             const float y = fmaf(x[i], at.c, -at.rc), e = exp2_fast(y);
-            x[i] = ENTROPY ? e * fmaf(b, fmaxf(y, LEAST), a) : e * a;
+            x[i] = ENTROPY ? e * fmaf(b, CLAMPED ? fmaxf(y, LEAST) : y, a) : e * a;
+        }
+    }
+    // where the reference asks for it (large logits)
+    __device__ __forceinline__ void of_difference(float (&x)[VEC], const Scales &q) const
+    {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const float y = (x[i] - at.ref) * q.c;
+            x[i] = exp2_fast(y) * fmaf(b, fmaxf(y, LEAST), a);
         }
     }
 };
+
+// The token's own gradient among those of a slot.
+template <int DT> struct TokenPlace {
+    static constexpr int VEC = Row<DT>::VEC;
+    const Row<DT> &row;
+    int token, slot;           // slot -1: the row has no token
+    float d;
+    __device__ __forceinline__ TokenPlace(const Row<DT> &row, int token, float d)
+        : row(row), token(token), slot(token < 0 ? -1 : (int)((unsigned)(token + row.shift) / VEC)), d(d) {}
+    __device__ __forceinline__ void put(float (&x)[VEC], int s) const
+    {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) x[i] = s == slot && row.index(s, i) == token ? d : x[i];
+    }
+};
+
+// u / s from the sum and the entropy that the forward pass left
+__device__ __forceinline__ float mean_exponent(float sum, float entropy) { return (float)((log((double)sum) - (double)entropy) / LN2_64); }
 
 template <int DT, int BLOCK, bool ENTROPY>
 __global__ __launch_bounds__(BLOCK) void score_grad_kernel(ScoreArgs a)
@@ -435,20 +458,19 @@ __global__ __launch_bounds__(BLOCK) void score_grad_kernel(ScoreArgs a)
     }
     const Scales q(a.temperature);
     const float4 state = a.state[r];
-    const TokenSlope<VEC> g(a, r, padding, state.x, state.y, (double)state.z, a.tokens ? row.load_one(token) : 0.f, q);
+    const TokenSlope<VEC> g(a, r, padding, state.x, state.y, mean_exponent(state.y, state.z), a.tokens ? row.load_one(token) : 0.f, q);
     if (g.none) {
         out.clear(s1, BLOCK, s0);
         return;
     }
-    const int slot = a.tokens ? (token + row.shift) / VEC : -1;
+    const TokenPlace<DT> place(row, token, g.of_token);
+    const int wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x & ~63u);
     auto put = [&](const uint4 &raw, int s) {
         float x[VEC];
         Row<DT>::Type::unpack(raw, x);
-        g.template of<ENTROPY>(x, q);
-        if (s == slot) {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) x[i] = row.index(s, i) == token ? g.of_token : x[i];
-        }
+        if (g.at.by_difference()) g.of_difference(x, q);        // uniform, and rare
+        else g.template of<ENTROPY>(x);
+        if ((unsigned)(place.slot - (s - (int)threadIdx.x + wave)) < 64u) place.put(x, s);         // uniform for the wavefront
         out.store(s, x, row.full(s));
     };
     int s = s0 + (int)threadIdx.x;
@@ -460,6 +482,228 @@ __global__ __launch_bounds__(BLOCK) void score_grad_kernel(ScoreArgs a)
         for (int i = 0; i < DEEP; ++i) put(v[i], s + i * BLOCK);
     }
     for (; s < s1; s += BLOCK) put(row.load(s), s);
+}
+
+// ---- loss and gradient in one pass over memory -----------------------------------------------------------------------------------
+// A block holds its row in registers between the sums and the gradient, NV slots a thread; what is longer is read again.
+//
+// The sums of a wavefront's slots relative to the largest logit of its first slots, without a look at each; where they come out wrong
+// (a logit far above that one, masked places, NaN, large logits), once more relative to the largest of all.
+template <int DT, int BLOCK, int NV, int NL, bool ENTROPY> struct HeldRow {
+    using Type = LogitType<DT>;
+    static constexpr int VEC = Type::VEC;
+    uint4 v[NV], edge;
+    uint4 *own;                // in LDS: slot NV + k of this thread at own[k * BLOCK]
+    // full slots [f0, f1): thread t has f0 + t + i * BLOCK; threads 0 and 1 have the partial slots at the row's ends
+    __device__ __forceinline__ void fetch(const Row<DT> &row, int i)
+    {
+        const int from = row.first_full() + i * BLOCK;
+        if (lead(row) + i * BLOCK < row.end_full()) v[i] = from + (int)threadIdx.x < row.end_full() ? load_at(row, from) : Row<DT>::empty();
+    }
+    // slot `from` + thread: a uniform address and an offset, so that no slot's address takes registers
+    __device__ __forceinline__ static uint4 load_at(const Row<DT> &row, int from)
+    {
+        typedef unsigned Words __attribute__((ext_vector_type(4)));
+        const Words w = __builtin_nontemporal_load(reinterpret_cast<const Words *>(row.base) + from + (unsigned)threadIdx.x);
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __device__ __forceinline__ static int lead(const Row<DT> &row) { return row.first_full() + (int)__builtin_amdgcn_readfirstlane(threadIdx.x & ~63u); }
+    __device__ __forceinline__ static int edge_slot(const Row<DT> &row)
+    {
+        if (threadIdx.x == 0 && row.shift) return 0;
+        if (threadIdx.x == 1 && row.slots > row.end_full() && (row.slots > 1 || !row.shift)) return row.slots - 1;
+        return -1;
+    }
+    __device__ __forceinline__ void fetch_edge(const Row<DT> &row)
+    {
+        const int s = edge_slot(row);
+        edge = s >= 0 ? row.load(s) : Row<DT>::empty();
+    }
+    // f(raw) for the slots of the wavefront, held or read again; FIRST: those that LDS holds come from memory
+    template <bool FIRST, typename F> __device__ __forceinline__ void each(const Row<DT> &row, F f) const
+    {
+        const int lead = this->lead(row), f0 = row.first_full(), f1 = row.end_full();
+        if (threadIdx.x < 64) f(edge);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (lead + i * BLOCK < f1) f(v[i]);         // uniform for the wavefront
+        auto more = [&](int i, auto keep) {             // slots i ... i + 3
+            uint4 w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int s = f0 + (int)threadIdx.x + (i + k) * BLOCK;
+                // what LDS keeps is read once; the rest is wanted again soon
+                w[k] = s >= f1 ? Row<DT>::empty() : decltype(keep)::value ? load_at(row, f0 + (i + k) * BLOCK) : row.load_full(s);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (lead + (i + k) * BLOCK >= f1) break;
+                f(w[k]);
+                if constexpr (decltype(keep)::value) own[(i + k - NV) * BLOCK] = w[k];
+            }
+        };
+        static_assert(NL % 4 == 0, "slots go in groups of four");
+        if constexpr (NL > 0) {
+            if constexpr (FIRST) {
+#pragma unroll 1
+                for (int i = NV; i < NV + NL && lead + i * BLOCK < f1; i += 4) more(i, std::true_type{});
+            } else {
+#pragma unroll 1
+                for (int i = NV; i < NV + NL && lead + i * BLOCK < f1; ++i) f(own[(i - NV) * BLOCK]);
+            }
+        }
+#pragma unroll 1
+        for (int i = NV + NL; lead + i * BLOCK < f1; i += 4) more(i, std::false_type{});
+    }
+    // masked: there may be masked places among the slots
+    __device__ __forceinline__ float4 sums(const Row<DT> &row, const Scales &q, bool &masked) const
+    {
+        auto largest = [&](float t, const uint4 &raw) {
+            float x[VEC];
+            Type::unpack(raw, x);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) t = fmaxf(t, x[j]);
+            return t;
+        };
+        float t = -INFINITY;
+        if (lead(row) < row.end_full()) t = largest(t, v[0]);
+        if (threadIdx.x < 64) t = largest(t, edge);
+        Reference<VEC> at(uniform(wave_max(t)), q);
+        float s = 0.f, u = 0.f;
+        masked = false;
+        each<true>(row, [&](const uint4 &raw) {
+            float x[VEC];
+            Type::unpack(raw, x);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float y = fmaf(x[j], at.c, -at.rc), e = exp2_fast(y);
+                s += e;
+                if constexpr (ENTROPY) u = fmaf(e, y, u);
+            }
+        });
+        if (__any(!(at.ref > -INFINITY && s <= 0x1p12f && (!ENTROPY || fabsf(u) <= 0x1p30f)))) {
+            float most = t;
+            bool odd = false;
+            masked = true;
+            each<false>(row, [&](const uint4 &raw) { most = largest(most, raw); });
+            at.set(uniform(wave_max(most)), q);
+            s = u = 0.f;
+            if (at.ref > -INFINITY) {
+                each<false>(row, [&](const uint4 &raw) {
+                    float x[VEC];
+                    Type::unpack(raw, x);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        const float y = at.by_difference() ? (x[j] - at.ref) * q.c : fmaf(x[j], at.c, -at.rc), e = exp2_fast(y);
+                        s += e;
+                        if constexpr (ENTROPY) u = fmaf(e, fmaxf(y, LEAST), u);
+                    }
+                });
+            } else {
+                each<false>(row, [&](const uint4 &raw) {
+                    float x[VEC];
+                    Type::unpack(raw, x);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) odd = odd || isnan(x[j]);
+                });
+                return make_float4(-INFINITY, __any(odd) ? NAN : 0.f, 0.f, 0.f);
+            }
+        }
+        const float f = exp2_fast(-at.lost), ws = wave_sum(s), wu = ENTROPY ? wave_sum(u) : 0.f;
+        return make_float4(at.ref, ws * f, ENTROPY ? f * fmaf(-at.lost, ws, wu) : 0.f, 0.f);
+    }
+};
+
+template <int DT, int BLOCK, int NV, int NL, bool ENTROPY>
+__global__ __launch_bounds__(BLOCK, 4) void token_loss_rows_kernel(ScoreArgs a)
+{
+    using Type = LogitType<DT>;
+    constexpr int VEC = Type::VEC;
+    __shared__ JoinLds<BLOCK> lds;
+    __shared__ uint4 rest[NL > 0 ? NL * BLOCK : 1];
+    const Scales q(a.temperature);
+    for (size_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        const Row<DT> row(a.logits, r, a.ld, a.V);
+        const GradRow<DT> out(a.dlogits, a.dld, a.V, r, row);
+        const int token = a.tokens[r];
+        if (padded(a, token)) {
+            out.clear(row.slots, BLOCK);
+            continue;
+        }
+        HeldRow<DT, BLOCK, NV, NL, ENTROPY> held;
+        held.own = rest + threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) held.fetch(row, i);
+        held.fetch_edge(row);
+        const float z_token = row.load_one(token);
+        bool masked;
+        const float4 w = join_waves<BLOCK>(held.sums(row, q, masked), lds, q);
+        if (threadIdx.x == 0) a.partial[r] = make_float4(w.x, w.y, w.z, z_token);
+        const TokenSlope<VEC> g(a, r, false, w.x, w.y, w.z / w.y, z_token, q);
+        if (g.none) {                                   // uniform
+            out.clear(row.slots, BLOCK);
+            continue;
+        }
+        const TokenPlace<DT> place(row, token, g.of_token);
+        if (g.at.by_difference() || !out.same) {        // uniform, and rare (large logits, a gradient at another alignment): the row is read again
+#pragma unroll 1
+            for (int s = threadIdx.x; s < row.slots; s += BLOCK) {
+                float x[VEC];
+                Type::unpack(row.load(s), x);
+                if (g.at.by_difference()) g.of_difference(x, q);
+                else g.template of<ENTROPY>(x);
+                place.put(x, s);
+                out.store(s, x, row.full(s));
+            }
+            continue;
+        }
+        const int f0 = row.first_full(), f1 = row.end_full(), lead = held.lead(row), edge_slot = held.edge_slot(row);
+        if (edge_slot >= 0) {
+            float x[VEC];
+            Type::unpack(held.edge, x);
+            g.template of<ENTROPY>(x);
+            place.put(x, edge_slot);
+            out.store(edge_slot, x, false);
+        }
+        auto store = [&](auto clamped) {
+            // full slots f0 + i * BLOCK + thread
+            auto put = [&](const uint4 &raw, int i) {
+                float x[VEC];
+                Type::unpack(raw, x);
+                g.template of<ENTROPY, decltype(clamped)::value>(x);
+                if ((unsigned)(place.slot - (lead + i * BLOCK)) < 64u) place.put(x, f0 + i * BLOCK + (int)threadIdx.x);        // uniform for the wavefront
+                out.store_at(f0 + i * BLOCK, x);
+            };
+            if constexpr (NL > 0) {
+#pragma unroll 2
+                for (int i = NV; i < NV + NL; ++i)
+                    if (f0 + (int)threadIdx.x + i * BLOCK < f1) put(held.own[(i - NV) * BLOCK], i);
+            }
+#pragma unroll 1
+            for (int i = NV + NL; lead + i * BLOCK < f1; i += 4) {
+                uint4 v[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (f0 + (int)threadIdx.x + (i + k) * BLOCK < f1) v[k] = row.load_full(f0 + (int)threadIdx.x + (i + k) * BLOCK);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (f0 + (int)threadIdx.x + (i + k) * BLOCK < f1) put(v[k], i + k);
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (f0 + (int)threadIdx.x + i * BLOCK < f1) put(held.v[i], i);
+        };
+        if (ENTROPY && masked) store(std::true_type{});         // uniform for the wavefront
+        else store(std::false_type{});
+    }
+    // what the rows' sums say in 64 bits, a row a thread, where no row is held any more
+    __syncthreads();
+    for (size_t r = blockIdx.x + (size_t)threadIdx.x * gridDim.x; r < a.rows; r += (size_t)BLOCK * gridDim.x) {
+        const bool padding = padded(a, a.tokens[r]);
+        float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (!padding) w = a.partial[r];
+        write_score(a, r, padding, true, w, w.w, 0);
+    }
 }
 
 // ---- short rows: a wavefront each, all calls --------------------------------------------------------------------------------------
@@ -514,7 +758,8 @@ __global__ __launch_bounds__(256) void score_short_kernel(ScoreArgs a)
         s += e[i];
         u = fmaf(e[i], y[i], u);
     }
-    double entropy = (double)w.z;
+    float mean = 0.f;
+    if constexpr (!(MODE & SCORE_SUMS)) mean = mean_exponent(w.y, w.z);
     if constexpr (MODE & SCORE_SUMS) {
         w.y = wave_sum(s);
         w.z = wave_sum(u);
@@ -526,9 +771,9 @@ __global__ __launch_bounds__(256) void score_short_kernel(ScoreArgs a)
                 before += __popcll(__ballot(masked ? x[i] > -INFINITY : x[i] > z_token || (x[i] == z_token && lane + 64 * i < token)));
         }
         if (lane == 0) write_score(a, r, padding, given, w, z_token, before);
-        const RowScore score(w);
-        entropy = score.entropy;
+        mean = w.z / w.y;
         if constexpr (TOP) {
+            const RowScore score(w);
             unsigned long long *words = all_words[wave];
             const unsigned n = short_first(x, (unsigned)a.k, words);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");         // LDS accesses of one wavefront are executed in order
@@ -543,7 +788,7 @@ __global__ __launch_bounds__(256) void score_short_kernel(ScoreArgs a)
         }
     }
     if constexpr (MODE & SCORE_GRAD) {
-        const TokenSlope<4> g(a, r, padding, from, w.y, entropy, z_token, q, true);
+        const TokenSlope<4> g(a, r, padding, from, w.y, mean, z_token, q, true);
         const Row<DT> out(a.dlogits, r, a.dld, a.V);
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
@@ -596,6 +841,18 @@ template <int DT> static void launch_grad(const ScoreArgs &a, bool entropy, hipS
     by_flag(entropy, [&](auto h) {
         EASGD_LAUNCH((score_grad_kernel<DT, SCORE_BLOCK, decltype(h)::value>), dim3((unsigned)(a.rows * a.segments)), dim3(SCORE_BLOCK), 0, s, a);
     });
+}
+template <int DT, int BLOCK, int NV, int NL> static void launch_held(const ScoreArgs &a, bool entropy, hipStream_t s)
+{
+    by_flag(entropy, [&](auto h) {
+        EASGD_LAUNCH((token_loss_rows_kernel<DT, BLOCK, NV, NL, decltype(h)::value>), dim3((unsigned)a.rows), dim3(BLOCK), 0, s, a);
+    });
+}
+template <int DT> static void launch_loss(const ScoreArgs &a, int slots, bool entropy, hipStream_t s)
+{
+    if (slots <= 2048) launch_held<DT, 256, 4, 0>(a, entropy, s);
+    else if (slots <= 8192 + 2) launch_held<DT, 256, 8, 8>(a, entropy, s);
+    else launch_held<DT, 1024, 4, 8>(a, entropy, s);
 }
 template <int DT, int MODE, bool TOP> static void launch_short(const ScoreArgs &a, hipStream_t s)
 {
@@ -734,15 +991,16 @@ int easgd_token_loss(const void *logits, int dtype, size_t rows, int V, size_t l
     a.logits = logits; a.ld = ld; a.rows = rows; a.V = V;
     a.tokens = tokens; a.temperature = temperature; a.weight = weight; a.bonus = bonus;
     a.loss = loss; a.logprob = logprob; a.entropy = entropy; a.scale = scale; a.dlogits = dlogits; a.dld = dld; a.parts = 1;
+    a.partial = static_cast<float4 *>(workspace);
     const int slots = most_slots(dtype, V);
     set_segments(a, score_segments(rows, slots), slots);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     by_dtype(dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         if (V <= SCORE_SHORT_V) launch_short<DT, SCORE_BOTH, false>(a, s);
+        else if (a.segments == 1) launch_loss<DT>(a, slots, entropy || bonus != 0.f, s);
         else {
-            a.state = static_cast<float4 *>(workspace);
-            a.partial = a.state + rows;
+            a.state = a.partial + rows * a.segments;
             launch_sums<DT>(a, entropy || bonus != 0.f, s);
             launch_grad<DT>(a, bonus != 0.f, s);
         }
