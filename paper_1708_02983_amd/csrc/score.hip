@@ -44,6 +44,9 @@ static constexpr double LN2_64 = 0.69314718055994530942;
 // the exponent that stands for any smaller one in e_j y_j, where e_j is 0: a masked place must not make it 0 times infinity
 static constexpr float LEAST = -256.f;
 
+// The hardware's product in which 0 times anything, infinities and NaN among it, is 0.
+extern "C" __device__ float mul_zero_first(float, float) __asm("llvm.amdgcn.fmul.legacy");
+
 // ---- sums ----------------------------------------------------------------------------------------------------------------
 // Running sums of a thread relative to a reference that its wavefront shares (Reference in row_sums.h): the largest logit of the
 // first slots that hold any, moved when a slot's exponentials sum up to more than 2^12, so that the usual slot needs neither a
@@ -54,8 +57,8 @@ template <int VEC, bool ENTROPY> struct TokenSums {
     float s = 0.f, u = 0.f;
 
     __device__ __forceinline__ explicit TokenSums(const Scales &q) : q(q), at(q) {}
-    // whole wavefronts call it (lanes without a slot with an empty one)
-    __device__ __forceinline__ void add(const float (&x)[VEC])
+    // whole wavefronts call it (lanes without a slot with an empty one); returns the slot's sum
+    __device__ __forceinline__ float add(const float (&x)[VEC])
     {
         float sum = 0.f, more = 0.f;
 #pragma unroll
@@ -69,7 +72,10 @@ template <int VEC, bool ENTROPY> struct TokenSums {
         if (__any(!fine)) careful(x, sum, more);        // uniform for the wavefront
         s += sum;
         if constexpr (ENTROPY) u += more;
+        return sum;
     }
+    // below it, the sum of a slot has no exponential of a logit from z on (exponentials are right to a few units)
+    __device__ __forceinline__ float bar(float z) const { return exp2_fast(fmaf(z, at.c, -at.rc)) * (1.f - 0x1p-16f); }
     // a slot whose sums are not as they should be: the first one, a logit far above the reference, masked places, NaN, large logits
     __device__ __forceinline__ void careful(const float (&x)[VEC], float &sum, float &more)
     {
@@ -118,10 +124,12 @@ __device__ __forceinline__ float4 rebased(const float4 &p, float m, const Scales
 // ---- ranks -----------------------------------------------------------------------------------------------------------------
 // How many logits of the row come before the token in its order: z > z_t, or z == z_t at a lower index.  Slots before the
 // token's compare with z >= z_t, slots behind it with z >= the next larger number, and the token's own slot looks closely.
+// A slot whose sum of exponentials is below the token's own has nothing to count: one comparison a slot for tokens of any standing.
 struct RankCount {
     float z, from;             // of the token; the next larger number
+    float ref = NAN, bar = 0.f;      // the reference of the sums for which `bar` is the token's
     int slot, index;           // of the token
-    unsigned n = 0;            // uniform for the wavefront
+    unsigned n = 0;            // of this lane
     template <int DT> __device__ __forceinline__ void set(const Row<DT> &row, int token)
     {
         slot = (token + row.shift) / Row<DT>::VEC;
@@ -134,15 +142,20 @@ struct RankCount {
             from = z == 0.f ? __uint_as_float(1u) : __uint_as_float(b & 0x80000000u ? b - 1 : b + 1);
         }
     }
-    template <int DT> __device__ __forceinline__ void add(const Row<DT> &row, const float (&x)[Row<DT>::VEC], int s)
+    template <int DT, typename S> __device__ __forceinline__ void add(const Row<DT> &row, const float (&x)[Row<DT>::VEC], int s, float sum, const S &sums)
     {
+        if (sums.at.ref != ref) {                       // uniform, and rare
+            ref = sums.at.ref;
+            bar = sums.bar(z);
+        }
+        if (!__any(!(sum < bar))) return;               // uniform for the wavefront
         const float least = s < slot ? z : from;
         if (__any(s == slot)) {
 #pragma unroll
-            for (int i = 0; i < Row<DT>::VEC; ++i) n += __popcll(__ballot(x[i] >= (s == slot && row.index(s, i) < index ? z : least)));
+            for (int i = 0; i < Row<DT>::VEC; ++i) n += x[i] >= (s == slot && row.index(s, i) < index ? z : least);
         } else {
 #pragma unroll
-            for (int i = 0; i < Row<DT>::VEC; ++i) n += __popcll(__ballot(x[i] >= least));
+            for (int i = 0; i < Row<DT>::VEC; ++i) n += x[i] >= least;
         }
     }
 };
@@ -201,14 +214,18 @@ template <int DT, int BLOCK, int DEEP, typename F> __device__ __forceinline__ vo
     uint4 v[DEEP];
     int s = s0 + (int)threadIdx.x;
     const int lead = s0 + (int)__builtin_amdgcn_readfirstlane(threadIdx.x & ~63);
+    auto load = [&](int s, int first) {                 // first: of the wavefront
+        if (first * Row<DT>::VEC >= row.shift && first + 64 <= s1 && (first + 64) * Row<DT>::VEC <= row.end) return row.load_once(s);
+        return s < s1 ? row.load(s) : row.empty();
+    };
 #pragma unroll
-    for (int i = 0; i < DEEP; ++i) v[i] = row.load_wave(s + i * BLOCK, s1);
+    for (int i = 0; i < DEEP; ++i) v[i] = load(s + i * BLOCK, lead + i * BLOCK);
     for (int first = lead; first < s1; first += DEEP * BLOCK, s += DEEP * BLOCK) {
 #pragma unroll
         for (int i = 0; i < DEEP; ++i) {
             if (first + i * BLOCK >= s1) break;         // uniform: the whole wavefront is behind the end
             f(v[i], s + i * BLOCK);
-            if (first + (DEEP + i) * BLOCK < s1) v[i] = row.load_wave(s + (DEEP + i) * BLOCK, s1);
+            if (first + (DEEP + i) * BLOCK < s1) v[i] = load(s + (DEEP + i) * BLOCK, first + (DEEP + i) * BLOCK);
         }
     }
 }
@@ -263,13 +280,13 @@ __global__ __launch_bounds__(BLOCK) void score_rows_kernel(ScoreArgs a)
     TokenSums<VEC, ENTROPY> sums(q);
     RankCount rank;
     if constexpr (RANK) rank.set(row, token);
-    walk<DT, BLOCK, 8>(row, s0, s1, [&](const uint4 &raw, int s) {
+    walk<DT, BLOCK, 4>(row, s0, s1, [&](const uint4 &raw, int s) {
         float x[VEC];
         Row<DT>::Type::unpack(raw, x);
-        sums.add(x);
-        if constexpr (RANK) rank.add(row, x, s);
+        const float sum = sums.add(x);
+        if constexpr (RANK) rank.add(row, x, s, sum, sums);
     });
-    const float4 w = block_sums<BLOCK>(sums, RANK ? rank.n : 0u, lds, q);
+    const float4 w = block_sums<BLOCK>(sums, RANK ? wave_sum(rank.n) : 0u, lds, q);
     if (threadIdx.x != 0) return;
     if (a.segments > 1) a.partial[blockIdx.x] = w;
     else write_score(a, r, false, a.tokens, w, a.tokens ? row.load_one(token) : 0.f, __float_as_uint(w.w));
@@ -296,10 +313,9 @@ __global__ __launch_bounds__(BLOCK) void score_top_kernel(ScoreArgs a)
     RankCount rank;
     rank.set(row, token);
     const unsigned n = first_of<DT, BLOCK>(row, s0, s1, (unsigned)a.k, top, [&](const float (&x)[VEC], int s) {
-        sums.add(x);
-        rank.add(row, x, s);
+        rank.add(row, x, s, sums.add(x), sums);
     });
-    const float4 w = block_sums<BLOCK>(sums, rank.n, lds, q);
+    const float4 w = block_sums<BLOCK>(sums, wave_sum(rank.n), lds, q);
     const unsigned i = threadIdx.x;
     if (a.segments > 1) {
         if (i == 0) a.partial[blockIdx.x] = w;
@@ -401,15 +417,18 @@ template <int VEC> struct TokenSlope {
         b = uniform(-gh * factor);
         const float y = (z_token - m) * q.c, p = exp2_fast(y) * by_sum;
         of_token = uniform((gl * (1.f - p) - (p > 0.f ? gh * p * (y - mean) : 0.f)) * by_T);
-        if (isnan(sum)) of_token = NAN;
+        if (isnan(sum)) {                               // a row with a NaN or +inf: every exponential is 1, or NaN, and a and b are NaN
+            of_token = NAN;
+            at.c = at.rc = 0.f;
+        }
     }
-    // clamped: there may be masked places among them
-    template <bool ENTROPY, bool CLAMPED = true> __device__ __forceinline__ void of(float (&x)[VEC]) const
+    // A masked place has e = 0 and y = -inf: the product in which 0 times anything is 0.
+    template <bool ENTROPY> __device__ __forceinline__ void of(float (&x)[VEC]) const
     {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
             const float y = fmaf(x[i], at.c, -at.rc), e = exp2_fast(y);
-            x[i] = ENTROPY ? e * fmaf(b, CLAMPED ? fmaxf(y, LEAST) : y, a) : e * a;
+            x[i] = ENTROPY ? mul_zero_first(e, fmaf(b, y, a)) : e * a;
         }
     }
     // where the reference asks for it (large logits)
@@ -418,7 +437,7 @@ template <int VEC> struct TokenSlope {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
             const float y = (x[i] - at.ref) * q.c;
-            x[i] = exp2_fast(y) * fmaf(b, fmaxf(y, LEAST), a);
+            x[i] = mul_zero_first(exp2_fast(y), fmaf(b, y, a));
         }
     }
 };
@@ -555,8 +574,7 @@ template <int DT, int BLOCK, int NV, int NL, bool ENTROPY> struct HeldRow {
 #pragma unroll 1
         for (int i = NV + NL; lead + i * BLOCK < f1; i += 4) more(i, std::false_type{});
     }
-    // masked: there may be masked places among the slots
-    __device__ __forceinline__ float4 sums(const Row<DT> &row, const Scales &q, bool &masked) const
+    __device__ __forceinline__ float4 sums(const Row<DT> &row, const Scales &q) const
     {
         auto largest = [&](float t, const uint4 &raw) {
             float x[VEC];
@@ -570,7 +588,6 @@ template <int DT, int BLOCK, int NV, int NL, bool ENTROPY> struct HeldRow {
         if (threadIdx.x < 64) t = largest(t, edge);
         Reference<VEC> at(uniform(wave_max(t)), q);
         float s = 0.f, u = 0.f;
-        masked = false;
         each<true>(row, [&](const uint4 &raw) {
             float x[VEC];
             Type::unpack(raw, x);
@@ -584,7 +601,6 @@ template <int DT, int BLOCK, int NV, int NL, bool ENTROPY> struct HeldRow {
         if (__any(!(at.ref > -INFINITY && s <= 0x1p12f && (!ENTROPY || fabsf(u) <= 0x1p30f)))) {
             float most = t;
             bool odd = false;
-            masked = true;
             each<false>(row, [&](const uint4 &raw) { most = largest(most, raw); });
             at.set(uniform(wave_max(most)), q);
             s = u = 0.f;
@@ -615,7 +631,7 @@ template <int DT, int BLOCK, int NV, int NL, bool ENTROPY> struct HeldRow {
 };
 
 template <int DT, int BLOCK, int NV, int NL, bool ENTROPY>
-__global__ __launch_bounds__(BLOCK, 4) void token_loss_rows_kernel(ScoreArgs a)
+__global__ __launch_bounds__(BLOCK, NL > 0 ? 4 : 5) void token_loss_rows_kernel(ScoreArgs a)
 {
     using Type = LogitType<DT>;
     constexpr int VEC = Type::VEC;
@@ -636,8 +652,7 @@ __global__ __launch_bounds__(BLOCK, 4) void token_loss_rows_kernel(ScoreArgs a)
         for (int i = 0; i < NV; ++i) held.fetch(row, i);
         held.fetch_edge(row);
         const float z_token = row.load_one(token);
-        bool masked;
-        const float4 w = join_waves<BLOCK>(held.sums(row, q, masked), lds, q);
+        const float4 w = join_waves<BLOCK>(held.sums(row, q), lds, q);
         if (threadIdx.x == 0) a.partial[r] = make_float4(w.x, w.y, w.z, z_token);
         const TokenSlope<VEC> g(a, r, false, w.x, w.y, w.z / w.y, z_token, q);
         if (g.none) {                                   // uniform
@@ -665,36 +680,32 @@ __global__ __launch_bounds__(BLOCK, 4) void token_loss_rows_kernel(ScoreArgs a)
             place.put(x, edge_slot);
             out.store(edge_slot, x, false);
         }
-        auto store = [&](auto clamped) {
-            // full slots f0 + i * BLOCK + thread
-            auto put = [&](const uint4 &raw, int i) {
-                float x[VEC];
-                Type::unpack(raw, x);
-                g.template of<ENTROPY, decltype(clamped)::value>(x);
-                if ((unsigned)(place.slot - (lead + i * BLOCK)) < 64u) place.put(x, f0 + i * BLOCK + (int)threadIdx.x);        // uniform for the wavefront
-                out.store_at(f0 + i * BLOCK, x);
-            };
-            if constexpr (NL > 0) {
-#pragma unroll 2
-                for (int i = NV; i < NV + NL; ++i)
-                    if (f0 + (int)threadIdx.x + i * BLOCK < f1) put(held.own[(i - NV) * BLOCK], i);
-            }
-#pragma unroll 1
-            for (int i = NV + NL; lead + i * BLOCK < f1; i += 4) {
-                uint4 v[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (f0 + (int)threadIdx.x + (i + k) * BLOCK < f1) v[k] = row.load_full(f0 + (int)threadIdx.x + (i + k) * BLOCK);
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (f0 + (int)threadIdx.x + (i + k) * BLOCK < f1) put(v[k], i + k);
-            }
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (f0 + (int)threadIdx.x + i * BLOCK < f1) put(held.v[i], i);
+        // full slots f0 + i * BLOCK + thread
+        auto put = [&](const uint4 &raw, int i) {
+            float x[VEC];
+            Type::unpack(raw, x);
+            g.template of<ENTROPY>(x);
+            if ((unsigned)(place.slot - (lead + i * BLOCK)) < 64u) place.put(x, f0 + i * BLOCK + (int)threadIdx.x);        // uniform for the wavefront
+            out.store_at(f0 + i * BLOCK, x);
         };
-        if (ENTROPY && masked) store(std::true_type{});         // uniform for the wavefront
-        else store(std::false_type{});
+        if constexpr (NL > 0) {
+#pragma unroll 2
+            for (int i = NV; i < NV + NL; ++i)
+                if (f0 + (int)threadIdx.x + i * BLOCK < f1) put(held.own[(i - NV) * BLOCK], i);
+        }
+#pragma unroll 1
+        for (int i = NV + NL; lead + i * BLOCK < f1; i += 4) {
+            uint4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (f0 + (int)threadIdx.x + (i + k) * BLOCK < f1) v[k] = row.load_full(f0 + (int)threadIdx.x + (i + k) * BLOCK);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (f0 + (int)threadIdx.x + (i + k) * BLOCK < f1) put(v[k], i + k);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (f0 + (int)threadIdx.x + i * BLOCK < f1) put(held.v[i], i);
     }
     // what the rows' sums say in 64 bits, a row a thread, where no row is held any more
     __syncthreads();
@@ -808,6 +819,13 @@ static int score_segments(size_t rows, int slots)
     const int want = (int)((SCORE_SPLIT_BLOCKS + rows - 1) / rows), most = slots / SCORE_SPLIT_SLOTS;
     return want < most ? want : most;
 }
+// Gradients of rows whose sums are there: parts of at least 1024 slots, 2048 blocks
+static constexpr int GRAD_BLOCKS = 2048;
+static int grad_segments(size_t rows, int slots)
+{
+    const size_t want = (GRAD_BLOCKS + rows - 1) / rows, most = (size_t)slots / SCORE_SPLIT_SLOTS;
+    return (int)(most < 1 ? 1 : want < most ? want : most);
+}
 static void set_segments(ScoreArgs &a, int segments, int slots)
 {
     a.segments = segments;
@@ -836,10 +854,13 @@ template <int DT> static void launch_top(const ScoreArgs &a, hipStream_t s)
     EASGD_LAUNCH((score_top_kernel<DT, TOP_BLOCK>), dim3((unsigned)(a.rows * a.segments)), dim3(TOP_BLOCK), 0, s, a);
     if (a.segments > 1) EASGD_LAUNCH((score_top_join_kernel<DT, TOP_BLOCK>), dim3((unsigned)a.rows), dim3(TOP_BLOCK), 0, s, a);
 }
+// 512 threads where a part has work for them, us (256 / 512): 1024 x 32000 bf16 24.6 / 22.5, 777 x 50001 fp16 30.4 / 28.6, 4096 x 2000 bf16 12 / 18
 template <int DT> static void launch_grad(const ScoreArgs &a, bool entropy, hipStream_t s)
 {
+    const dim3 grid((unsigned)(a.rows * a.segments));
     by_flag(entropy, [&](auto h) {
-        EASGD_LAUNCH((score_grad_kernel<DT, SCORE_BLOCK, decltype(h)::value>), dim3((unsigned)(a.rows * a.segments)), dim3(SCORE_BLOCK), 0, s, a);
+        if (a.seg_slots >= 1024) EASGD_LAUNCH((score_grad_kernel<DT, 512, decltype(h)::value>), grid, dim3(512), 0, s, a);
+        else EASGD_LAUNCH((score_grad_kernel<DT, 256, decltype(h)::value>), grid, dim3(256), 0, s, a);
     });
 }
 template <int DT, int BLOCK, int NV, int NL> static void launch_held(const ScoreArgs &a, bool entropy, hipStream_t s)
@@ -851,7 +872,7 @@ template <int DT, int BLOCK, int NV, int NL> static void launch_held(const Score
 template <int DT> static void launch_loss(const ScoreArgs &a, int slots, bool entropy, hipStream_t s)
 {
     if (slots <= 2048) launch_held<DT, 256, 4, 0>(a, entropy, s);
-    else if (slots <= 8192 + 2) launch_held<DT, 256, 8, 8>(a, entropy, s);
+    else if (slots <= 8192 + 2) launch_held<DT, 256, 4, 8>(a, entropy, s);
     else launch_held<DT, 1024, 4, 8>(a, entropy, s);
 }
 template <int DT, int MODE, bool TOP> static void launch_short(const ScoreArgs &a, hipStream_t s)
@@ -955,7 +976,7 @@ int easgd_score_tokens_grad(const void *logits, int dtype, size_t rows, int V, s
     a.tokens = tokens; a.temperature = temperature; a.state = reinterpret_cast<float4 *>(const_cast<float *>(state));
     a.dlogprob = dlogprob; a.dentropy = dentropy; a.scale = scale; a.dlogits = dlogits; a.dld = dld; a.parts = 1;
     const int slots = most_slots(dtype, V);
-    set_segments(a, score_segments(rows, slots), slots);
+    set_segments(a, grad_segments(rows, slots), slots);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     by_dtype(dtype, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
