@@ -154,6 +154,7 @@ def _check(code: int) -> None:
 
 
 _raw_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device     # where a tensor on a GPU is at hand
 
 
 def _stream(stream) -> ctypes.c_void_p:
@@ -167,6 +168,13 @@ def _stream(stream) -> ctypes.c_void_p:
     if isinstance(device, torch.device) and device.index not in (None, torch.cuda.current_device()):
         raise ValueError(f"stream is on {device}, the current device is cuda:{torch.cuda.current_device()}")
     return ctypes.c_void_p(stream.cuda_stream)
+
+
+def _stream_on(stream, device: int):
+    """_stream for calls whose tensors are known to be on the current device, `device`."""
+    if stream is None and _raw_current_stream is not None:
+        return _raw_current_stream(device)
+    return _stream(stream)
 
 
 def _dev(name: str, t: torch.Tensor, dtype, min_numel: int) -> int:
@@ -452,7 +460,7 @@ def _logit_rows(name: str, t: torch.Tensor):
         ld = max(V, 1)
     elif ld < V:
         raise ValueError(f"{name}: rows must not overlap (stride {ld}, length {V})")
-    here = torch.cuda.current_device()
+    here = _current_device()
     if t.get_device() != here:
         raise ValueError(f"{name} is on {t.device}, the current device is cuda:{here}")
     return t.data_ptr(), code, rows, V, ld
@@ -681,7 +689,7 @@ def easgd_score_tokens(logits, tokens=None, temperature: float = 1.0, k: int = 0
                                    _given("logprob", logprob, _F32, shape, on), _given("entropy", entropy, _F32, shape, on),
                                    _given("rank", rank, _I32, shape, on), k, _given("top_logprob", top_logprob, _F32, (rows, k), on),
                                    _given("top_indices", top_indices, _I32, (rows, k), on), _given("state", state, _F32, (rows, 4), on),
-                                   ws, nbytes, _stream(stream)))
+                                   ws, nbytes, _stream_on(stream, on)))
     return TokenScores(logprob, entropy, rank, top_logprob, top_indices, state)
 
 
@@ -694,7 +702,7 @@ def easgd_score_tokens_grad(logits, tokens, state, temperature: float = 1.0, dlo
     dlogits, dptr, dld = _gradient_rows(logits, dlogits, rows, V, stream)
     _check(_lib.easgd_score_tokens_grad(ptr, code, rows, V, ld, _given("tokens", tokens, _I32, shape, on), temperature,
                                         _given("state", state, _F32, (rows, 4), on), _given("dlogprob", dlogprob, _F32, shape, on),
-                                        _given("dentropy", dentropy, _F32, shape, on), scale, dptr, dld, _stream(stream)))
+                                        _given("dentropy", dentropy, _F32, shape, on), scale, dptr, dld, _stream_on(stream, on)))
     return dlogits
 
 
@@ -713,7 +721,7 @@ def easgd_token_loss(logits, tokens, weight=None, bonus: float = 0.0, temperatur
     keep, ws, nbytes = _scratch(easgd_token_loss_workspace_bytes(rows, V), workspace, logits, stream)
     _check(_lib.easgd_token_loss(ptr, code, rows, V, ld, _given("tokens", tokens, _I32, shape, on), _given("weight", weight, _F32, shape, on),
                                  bonus, temperature, scale, _given("loss", loss, _F32, shape, on), _given("logprob", logprob, _F32, shape, on),
-                                 _given("entropy", entropy, _F32, shape, on), dptr, dld, ws, nbytes, _stream(stream)))
+                                 _given("entropy", entropy, _F32, shape, on), dptr, dld, ws, nbytes, _stream_on(stream, on)))
     return loss, logprob, entropy, dlogits
 
 
@@ -739,7 +747,7 @@ def easgd_grad_token_loss(dims: Sequence[int], W, X, tokens, G, loss=None, weigh
     _check(_lib.easgd_grad_token_loss(arr, L, W.data_ptr(), ld, _given("X", X, _F32, (P, b, dims[0]), on), _given("tokens", tokens, _I32, shape, on),
                                       _given("weight", weight, _F32, shape, on), P, b, bonus, temperature, G.data_ptr(),
                                       _given("loss", loss, _F32, (P,), on), _given("logprob", logprob, _F32, shape, on),
-                                      _given("entropy", entropy, _F32, shape, on), ws, size, _stream(stream)))
+                                      _given("entropy", entropy, _F32, shape, on), ws, size, _stream_on(stream, on)))
     return workspace
 
 
@@ -757,7 +765,7 @@ def _replica_rows(name: str, t, N: Optional[int]):
     P, ld, N = _replica_shape(t, N)
     if N < 1 or N > ld:
         raise ValueError(f"N must be in [1, {ld}], got {N}")
-    here = torch.cuda.current_device()
+    here = _current_device()
     if t.get_device() != here:
         raise ValueError(f"{name} is on {t.device}, the current device is cuda:{here}")
     return t.data_ptr(), code, P, N, ld, here
@@ -778,7 +786,7 @@ def easgd_grad_norms(G, max_norm: float = float("inf"), N: Optional[int] = None,
         clip = _new((P,), _F32, G, stream)
     keep, ws, nbytes = _scratch(easgd_grad_norms_workspace_bytes(P, N), workspace, G, stream)
     _check(_lib.easgd_grad_norms(ptr, code, P, N, ld, max_norm, _given("norm", norm, _F32, (P,), on), _given("clip", clip, _F32, (P,), on),
-                                 ws, nbytes, _stream(stream)))
+                                 ws, nbytes, _stream_on(stream, on)))
     return norm, clip
 
 
@@ -822,12 +830,12 @@ def adamw_round(W, M, S, G, step, eta, Wc=None, rho: float = 0.0, beta1: float =
             raise ValueError("moments in 8 bits need M_scale and S_scale")
         _check(_lib.adamw_round_8bit(wptr, mptr, sptr, _given("M_scale", M_scale, _F32, blocks, on), _given("S_scale", S_scale, _F32, blocks, on), gptr, code,
                                      center, P, N, ld, ends, rates, decays, n, clip, eta, eta_at, rho, beta1, beta2, eps, decay, step, step_at,
-                                     seed & 0xFFFFFFFF, _stream(stream)))
+                                     seed & 0xFFFFFFFF, _stream_on(stream, on)))
         return
     if M_scale is not None or S_scale is not None:
         raise ValueError("M_scale and S_scale belong to moments in 8 bits")
     _check(_lib.adamw_round(wptr, mptr, sptr, gptr, code, center, P, N, ld, ends, rates, decays, n, clip, eta, eta_at, rho, beta1, beta2, eps, decay,
-                            step, step_at, _stream(stream)))
+                            step, step_at, _stream_on(stream, on)))
 
 
 def stream_copy(dst, src, stream=None) -> None:

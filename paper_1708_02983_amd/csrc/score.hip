@@ -331,18 +331,19 @@ __global__ __launch_bounds__(BLOCK) void score_top_kernel(ScoreArgs a)
 __device__ __forceinline__ float4 join_parts(const ScoreArgs &a, size_t r, const Scales &q)
 {
     const int lane = threadIdx.x & 63;
-    float m = -INFINITY;
-    for (int i = lane; i < a.segments; i += 64) m = fmaxf(m, a.partial[r * a.segments + i].x);
-    m = wave_max(m);
-    float s = 0.f, u = 0.f;
+    const float4 *parts = a.partial + r * a.segments;
+    float4 own = make_float4(-INFINITY, 0.f, 0.f, 0.f);
     unsigned before = 0;
     for (int i = lane; i < a.segments; i += 64) {
-        const float4 p = a.partial[r * a.segments + i], w = rebased(p, m, q);
-        s += w.y;
-        u += w.z;
+        const float4 p = parts[i], w = own;
+        const float m = fmaxf(w.x, p.x);
+        const float4 x = rebased(w, m, q), y = rebased(p, m, q);
+        own = make_float4(m, x.y + y.y, x.z + y.z, 0.f);
         before += __float_as_uint(p.w);
     }
-    return make_float4(m, wave_sum(s), wave_sum(u), __uint_as_float(wave_sum(before)));
+    const float m = wave_max(own.x);
+    own = rebased(own, m, q);
+    return make_float4(m, wave_sum(own.y), wave_sum(own.z), __uint_as_float(wave_sum(before)));
 }
 
 template <int DT>
@@ -383,6 +384,20 @@ __global__ __launch_bounds__(BLOCK) void score_top_join_kernel(ScoreArgs a)
     if (threadIdx.x == 0) top.n = all;
     for (unsigned i = threadIdx.x; i < all; i += BLOCK) top.list[i] = a.words[r * all + i];
     __syncthreads();
+    if (all <= BLOCK) {                                 // a look at every pair: places that are left over are 0, behind all words
+        const unsigned long long word = threadIdx.x < all ? top.list[threadIdx.x] : 0;
+        unsigned at = 0, there = 0;
+#pragma unroll 8
+        for (unsigned i = 0; i < all; ++i) {
+            const unsigned long long other = top.list[i];
+            at += other > word;
+            there += other != 0;
+        }
+        const RowScore score(sums);
+        if (word && at < (unsigned)a.k) write_alternative(a, r, at, word, score, sums.x);
+        if (threadIdx.x >= there && threadIdx.x < (unsigned)a.k) write_alternative(a, r, threadIdx.x, 0, score, sums.x);
+        return;
+    }
     unsigned n = keep_from<BLOCK>(top, all, FIRST_WORD);           // the words that are there
     if (n > 512) n = keep_from<BLOCK>(top, n, select_nth<BLOCK>(EachListed{top.list, n, BLOCK}, FIRST_WORD, a.k, top.select));
     rank_list<BLOCK>(top, n, a.k);
@@ -638,83 +653,77 @@ __global__ __launch_bounds__(BLOCK, NL > 0 ? 4 : 5) void token_loss_rows_kernel(
     __shared__ JoinLds<BLOCK> lds;
     __shared__ uint4 rest[NL > 0 ? NL * BLOCK : 1];
     const Scales q(a.temperature);
-    for (size_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const Row<DT> row(a.logits, r, a.ld, a.V);
-        const GradRow<DT> out(a.dlogits, a.dld, a.V, r, row);
-        const int token = a.tokens[r];
-        if (padded(a, token)) {
-            out.clear(row.slots, BLOCK);
-            continue;
-        }
-        HeldRow<DT, BLOCK, NV, NL, ENTROPY> held;
-        held.own = rest + threadIdx.x;
+    const size_t r = blockIdx.x;
+    const Row<DT> row(a.logits, r, a.ld, a.V);
+    const GradRow<DT> out(a.dlogits, a.dld, a.V, r, row);
+    const int token = a.tokens[r];
+    if (padded(a, token)) {
+        out.clear(row.slots, BLOCK);
+        if (threadIdx.x == 0) write_score(a, r, true, false, make_float4(0.f, 0.f, 0.f, 0.f), 0.f, 0);
+        return;
+    }
+    HeldRow<DT, BLOCK, NV, NL, ENTROPY> held;
+    held.own = rest + threadIdx.x;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) held.fetch(row, i);
-        held.fetch_edge(row);
-        const float z_token = row.load_one(token);
-        const float4 w = join_waves<BLOCK>(held.sums(row, q), lds, q);
-        if (threadIdx.x == 0) a.partial[r] = make_float4(w.x, w.y, w.z, z_token);
-        const TokenSlope<VEC> g(a, r, false, w.x, w.y, w.z / w.y, z_token, q);
-        if (g.none) {                                   // uniform
-            out.clear(row.slots, BLOCK);
-            continue;
-        }
-        const TokenPlace<DT> place(row, token, g.of_token);
-        if (g.at.by_difference() || !out.same) {        // uniform, and rare (large logits, a gradient at another alignment): the row is read again
+    for (int i = 0; i < NV; ++i) held.fetch(row, i);
+    held.fetch_edge(row);
+    const float z_token = row.load_one(token);
+    const float4 w = join_waves<BLOCK>(held.sums(row, q), lds, q);
+    const TokenSlope<VEC> g(a, r, false, w.x, w.y, w.z / w.y, z_token, q);
+    if (g.none) {                                   // uniform
+        out.clear(row.slots, BLOCK);
+        if (threadIdx.x == 0) write_score(a, r, false, true, w, z_token, 0);
+        return;
+    }
+    const TokenPlace<DT> place(row, token, g.of_token);
+    if (g.at.by_difference() || !out.same) {        // uniform, and rare (large logits, a gradient at another alignment): the row is read again
 #pragma unroll 1
-            for (int s = threadIdx.x; s < row.slots; s += BLOCK) {
-                float x[VEC];
-                Type::unpack(row.load(s), x);
-                if (g.at.by_difference()) g.of_difference(x, q);
-                else g.template of<ENTROPY>(x);
-                place.put(x, s);
-                out.store(s, x, row.full(s));
-            }
-            continue;
-        }
-        const int f0 = row.first_full(), f1 = row.end_full(), lead = held.lead(row), edge_slot = held.edge_slot(row);
-        if (edge_slot >= 0) {
+        for (int s = threadIdx.x; s < row.slots; s += BLOCK) {
             float x[VEC];
-            Type::unpack(held.edge, x);
-            g.template of<ENTROPY>(x);
-            place.put(x, edge_slot);
-            out.store(edge_slot, x, false);
+            Type::unpack(row.load(s), x);
+            if (g.at.by_difference()) g.of_difference(x, q);
+            else g.template of<ENTROPY>(x);
+            place.put(x, s);
+            out.store(s, x, row.full(s));
         }
-        // full slots f0 + i * BLOCK + thread
-        auto put = [&](const uint4 &raw, int i) {
-            float x[VEC];
-            Type::unpack(raw, x);
-            g.template of<ENTROPY>(x);
-            if ((unsigned)(place.slot - (lead + i * BLOCK)) < 64u) place.put(x, f0 + i * BLOCK + (int)threadIdx.x);        // uniform for the wavefront
-            out.store_at(f0 + i * BLOCK, x);
-        };
-        if constexpr (NL > 0) {
+        if (threadIdx.x == 0) write_score(a, r, false, true, w, z_token, 0);
+        return;
+    }
+    const int f0 = row.first_full(), f1 = row.end_full(), lead = held.lead(row), edge_slot = held.edge_slot(row);
+    if (edge_slot >= 0) {
+        float x[VEC];
+        Type::unpack(held.edge, x);
+        g.template of<ENTROPY>(x);
+        place.put(x, edge_slot);
+        out.store(edge_slot, x, false);
+    }
+    // full slots f0 + i * BLOCK + thread
+    auto put = [&](const uint4 &raw, int i) {
+        float x[VEC];
+        Type::unpack(raw, x);
+        g.template of<ENTROPY>(x);
+        if ((unsigned)(place.slot - (lead + i * BLOCK)) < 64u) place.put(x, f0 + i * BLOCK + (int)threadIdx.x);        // uniform for the wavefront
+        out.store_at(f0 + i * BLOCK, x);
+    };
+    if constexpr (NL > 0) {
 #pragma unroll 2
-            for (int i = NV; i < NV + NL; ++i)
-                if (f0 + (int)threadIdx.x + i * BLOCK < f1) put(held.own[(i - NV) * BLOCK], i);
-        }
+        for (int i = NV; i < NV + NL; ++i)
+            if (f0 + (int)threadIdx.x + i * BLOCK < f1) put(held.own[(i - NV) * BLOCK], i);
+    }
 #pragma unroll 1
-        for (int i = NV + NL; lead + i * BLOCK < f1; i += 4) {
-            uint4 v[4];
+    for (int i = NV + NL; lead + i * BLOCK < f1; i += 4) {
+        uint4 v[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (f0 + (int)threadIdx.x + (i + k) * BLOCK < f1) v[k] = row.load_full(f0 + (int)threadIdx.x + (i + k) * BLOCK);
+        for (int k = 0; k < 4; ++k)
+            if (f0 + (int)threadIdx.x + (i + k) * BLOCK < f1) v[k] = row.load_full(f0 + (int)threadIdx.x + (i + k) * BLOCK);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (f0 + (int)threadIdx.x + (i + k) * BLOCK < f1) put(v[k], i + k);
-        }
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (f0 + (int)threadIdx.x + i * BLOCK < f1) put(held.v[i], i);
+        for (int k = 0; k < 4; ++k)
+            if (f0 + (int)threadIdx.x + (i + k) * BLOCK < f1) put(v[k], i + k);
     }
-    // what the rows' sums say in 64 bits, a row a thread, where no row is held any more
-    __syncthreads();
-    for (size_t r = blockIdx.x + (size_t)threadIdx.x * gridDim.x; r < a.rows; r += (size_t)BLOCK * gridDim.x) {
-        const bool padding = padded(a, a.tokens[r]);
-        float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (!padding) w = a.partial[r];
-        write_score(a, r, padding, true, w, w.w, 0);
-    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (f0 + (int)threadIdx.x + i * BLOCK < f1) put(held.v[i], i);
+    if (threadIdx.x == 0) write_score(a, r, false, true, w, z_token, 0);        // 64 bits, where no row is held any more
 }
 
 // ---- short rows: a wavefront each, all calls --------------------------------------------------------------------------------------
@@ -852,7 +861,8 @@ template <int DT> static void launch_sums(const ScoreArgs &a, bool entropy, hipS
 template <int DT> static void launch_top(const ScoreArgs &a, hipStream_t s)
 {
     EASGD_LAUNCH((score_top_kernel<DT, TOP_BLOCK>), dim3((unsigned)(a.rows * a.segments)), dim3(TOP_BLOCK), 0, s, a);
-    if (a.segments > 1) EASGD_LAUNCH((score_top_join_kernel<DT, TOP_BLOCK>), dim3((unsigned)a.rows), dim3(TOP_BLOCK), 0, s, a);
+    if (a.segments > 1 && a.segments * a.k <= 256) EASGD_LAUNCH((score_top_join_kernel<DT, 256>), dim3((unsigned)a.rows), dim3(256), 0, s, a);
+    else if (a.segments > 1) EASGD_LAUNCH((score_top_join_kernel<DT, TOP_BLOCK>), dim3((unsigned)a.rows), dim3(TOP_BLOCK), 0, s, a);
 }
 // 512 threads where a part has work for them, us (256 / 512): 1024 x 32000 bf16 24.6 / 22.5, 777 x 50001 fp16 30.4 / 28.6, 4096 x 2000 bf16 12 / 18
 template <int DT> static void launch_grad(const ScoreArgs &a, bool entropy, hipStream_t s)
@@ -872,8 +882,8 @@ template <int DT, int BLOCK, int NV, int NL> static void launch_held(const Score
 template <int DT> static void launch_loss(const ScoreArgs &a, int slots, bool entropy, hipStream_t s)
 {
     if (slots <= 2048) launch_held<DT, 256, 4, 0>(a, entropy, s);
-    else if (slots <= 8192 + 2) launch_held<DT, 256, 4, 8>(a, entropy, s);
-    else launch_held<DT, 1024, 4, 8>(a, entropy, s);
+    else if (slots <= 8192 + 2) launch_held<DT, 256, 8, 8>(a, entropy, s);
+    else launch_held<DT, 512, 16, 8>(a, entropy, s);
 }
 template <int DT, int MODE, bool TOP> static void launch_short(const ScoreArgs &a, hipStream_t s)
 {
@@ -990,7 +1000,8 @@ size_t easgd_token_loss_workspace_bytes(size_t rows, int V)
 {
     using namespace easgd;
     if (rows == 0 || rows > LOGITS_MAX_ROWS || V <= SCORE_SHORT_V || V > LOGITS_MAX_V) return 0;
-    return rounded(rows * (score_segments(rows, most_slots(EASGD_F32, V)) + 1) * sizeof(float4));
+    const int n = score_segments(rows, most_slots(EASGD_F32, V));
+    return n == 1 ? 0 : rounded(rows * (n + 1) * sizeof(float4));
 }
 
 int easgd_token_loss(const void *logits, int dtype, size_t rows, int V, size_t ld, const int32_t *tokens, const float *weight, float bonus,
