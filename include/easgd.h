@@ -219,12 +219,12 @@ int sync_sgd_round(float *W, float *V, const float *G,
  *                                         values of its replay (step_at below 1 counts as 1)
  *   beta1, beta2 in [0, 1), eps in [1e-30, 1e30], step >= 1; N <= 2^34, P <= 65535.
  * The moments' arithmetic is fixed, every operation rounded on its own: fl(fl(beta1*M) + fl(fl(1-beta1)*g)), fl(fl(beta2*S) +
- * fl(fl(fl(1-beta2)*g)*g)).  Results are the same bits from run to run.  128-bit accesses where W, Wc (and M, S) are 16-byte and G is
- * four elements aligned and ld % 4 == 0; element by element otherwise, with the same values.
+ * fl(fl(fl(1-beta2)*g)*g)).  Results are the same bits from run to run.  Every alignment and ld takes 128-bit
+ * accesses; rows that start at multiples of 16 bytes (4 for moments in 8 bits) are the fastest.
  *
  * adamw_round_8bit: the moments held in 8 bits between the steps, M as e4m3 and S as e5m2 (OCP), 256 consecutive parameters of a
  * replica (the last ones fewer) with a power of two in common per moment:
- *   M, S               DEVICE in/out [P][ld] one byte each (4-byte aligned for the fast path); entries [N, ld) are neither read nor written
+ *   M, S               DEVICE in/out [P][ld] one byte each; entries [N, ld) are neither read nor written
  *   M_scale, S_scale   DEVICE in/out [P][ceil(N/256)] fp32: M[i][j] stands for e4m3(M[i][j]) * M_scale[i][j/256], likewise S (all 0 before the first step)
  * W moves by the new moments before they are rounded.  Then, with e such that the block's largest |M| is in [2^(e+7), 2^(e+8)) (its largest S in
  * [2^(e+14), 2^(e+15)); e >= -126), 2^e becomes the block's scale and every moment times 2^-e is rounded to one of its two neighbours at

@@ -223,11 +223,11 @@ __device__ __forceinline__ unsigned wave_max_bits(unsigned v)
 // ---- four consecutive parameters of a lane ------------------------------------------------------------------------------------
 typedef float Four __attribute__((ext_vector_type(4)));
 // How they are accessed: at once past the caches (what is read once and written once), at once, or element by element with a look at the
-// row's end (rows at other alignments, and the last 256 parameters).
+// row's end (the last 256 parameters).  The hardware's wide accesses need the element's alignment only, so rows of any stride take them.
 enum { ACCESS_STREAM, ACCESS_WIDE, ACCESS_EACH };
 template <typename T, int ACCESS> __device__ __forceinline__ void load_four(const T *p, size_t j, size_t N, T (&x)[4])
 {
-    typedef T Vec __attribute__((ext_vector_type(4)));
+    typedef T Vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
     if constexpr (ACCESS == ACCESS_EACH) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = j + i < N ? p[j + i] : (T)0;
@@ -242,7 +242,7 @@ template <typename T, int ACCESS> __device__ __forceinline__ void load_four(cons
 }
 template <typename T, int ACCESS> __device__ __forceinline__ void store_four(T *p, size_t j, size_t N, const T (&x)[4])
 {
-    typedef T Vec __attribute__((ext_vector_type(4)));
+    typedef T Vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
     if constexpr (ACCESS == ACCESS_EACH) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -256,22 +256,23 @@ template <typename T, int ACCESS> __device__ __forceinline__ void store_four(T *
 }
 
 // four codes in a word
+typedef unsigned Codes __attribute__((aligned(1)));
 template <int ACCESS> __device__ __forceinline__ unsigned load_codes(const unsigned char *p, size_t j, size_t N)
 {
     if constexpr (ACCESS == ACCESS_EACH) {
         unsigned char c[4];
         load_four<unsigned char, ACCESS>(p, j, N, c);
         return (unsigned)c[3] << 24 | (unsigned)c[2] << 16 | (unsigned)c[1] << 8 | c[0];
-    } else if constexpr (ACCESS == ACCESS_STREAM) return __builtin_nontemporal_load(reinterpret_cast<const unsigned *>(p + j));
-    else return *reinterpret_cast<const unsigned *>(p + j);
+    } else if constexpr (ACCESS == ACCESS_STREAM) return __builtin_nontemporal_load(reinterpret_cast<const Codes *>(p + j));
+    else return *reinterpret_cast<const Codes *>(p + j);
 }
 template <int ACCESS> __device__ __forceinline__ void store_codes(unsigned char *p, size_t j, size_t N, unsigned codes)
 {
     if constexpr (ACCESS == ACCESS_EACH) {
         const unsigned char c[4] = {(unsigned char)codes, (unsigned char)(codes >> 8), (unsigned char)(codes >> 16), (unsigned char)(codes >> 24)};
         store_four<unsigned char, ACCESS>(p, j, N, c);
-    } else if constexpr (ACCESS == ACCESS_STREAM) __builtin_nontemporal_store(codes, reinterpret_cast<unsigned *>(p + j));
-    else *reinterpret_cast<unsigned *>(p + j) = codes;
+    } else if constexpr (ACCESS == ACCESS_STREAM) __builtin_nontemporal_store((Codes)codes, reinterpret_cast<Codes *>(p + j));
+    else *reinterpret_cast<Codes *>(p + j) = codes;
 }
 
 // A worker's share of 256 parameters, four of them a lane's, between loads and stores.
@@ -403,7 +404,7 @@ __global__ __launch_bounds__(256) void adamw_own_kernel(AdamwArgs a)
     if (block >= a.blocks) return;                      // wavefronts of a block have nothing in common
     const StepNumbers n(a);
     const int i = (int)blockIdx.y;
-    if (ACCESS != ACCESS_EACH && block < a.N / 256) adamw_block<GT, EIGHT, false, ACCESS>(a, n, block, i, i + 1);
+    if (block < a.N / 256) adamw_block<GT, EIGHT, false, ACCESS>(a, n, block, i, i + 1);
     else adamw_block<GT, EIGHT, false, ACCESS_EACH>(a, n, block, i, i + 1);
 }
 
@@ -469,7 +470,7 @@ __global__ __launch_bounds__(WAVES * 64) void adamw_split_kernel(AdamwArgs a)
 {
     __shared__ Four apart[SPLIT_ROOM][64];
     const StepNumbers n(a);
-    if (ACCESS != ACCESS_EACH && blockIdx.x < a.N / 256) adamw_split_block<GT, EIGHT, ACCESS, WAVES>(a, n, blockIdx.x, apart);      // uniform
+    if (blockIdx.x < a.N / 256) adamw_split_block<GT, EIGHT, ACCESS, WAVES>(a, n, blockIdx.x, apart);      // uniform
     else adamw_split_block<GT, EIGHT, ACCESS_EACH, WAVES>(a, n, blockIdx.x, apart);
 }
 
@@ -645,23 +646,21 @@ static int norm_parts(int P, size_t bytes)
 
 // Tiles of 8 x 61 M, us (1 / 2 / 4 blocks of 256 a wavefront): moments in 32 bits 2306 / 2097 / 2024, in 8 bits 1436 / 1377 / 1489: these need more wavefronts
 // under way, whose arithmetic hides behind each other's loads.
-template <int GT, bool EIGHT, bool CENTER> static void launch_adamw(const AdamwArgs &a, bool wide, hipStream_t s)
+template <int GT, bool EIGHT, bool CENTER> static void launch_adamw(const AdamwArgs &a, hipStream_t s)
 {
     constexpr int GROUPS = EIGHT ? 2 : 4;
-    const size_t moved = (size_t)a.P * a.N * (8 + (GT == EASGD_F32 ? 4 : 2) + (EIGHT ? 4 : 16));
-    if (wide && a.blocks >= (size_t)64 * num_cus()) {
+    const bool stream = update_nontemporal((size_t)a.P * a.N * (8 + (GT == EASGD_F32 ? 4 : 2) + (EIGHT ? 4 : 16)));
+    if (a.blocks >= (size_t)64 * num_cus()) {
         const dim3 grid((unsigned)TileMap<GROUPS, true>::tiles(a.blocks * 64));
-        if (update_nontemporal(moved)) EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, true, GROUPS, true>), grid, dim3(256), 0, s, a);
+        if (stream) EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, true, GROUPS, true>), grid, dim3(256), 0, s, a);
         else EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, false, GROUPS, true>), grid, dim3(256), 0, s, a);
     } else if constexpr (CENTER) {
         const dim3 grid((unsigned)a.blocks);
-        if (!wide) EASGD_LAUNCH((adamw_split_kernel<GT, EIGHT, ACCESS_EACH, 4>), grid, dim3(256), 0, s, a);
-        else if (update_nontemporal(moved)) EASGD_LAUNCH((adamw_split_kernel<GT, EIGHT, ACCESS_STREAM, 4>), grid, dim3(256), 0, s, a);
+        if (stream) EASGD_LAUNCH((adamw_split_kernel<GT, EIGHT, ACCESS_STREAM, 4>), grid, dim3(256), 0, s, a);
         else EASGD_LAUNCH((adamw_split_kernel<GT, EIGHT, ACCESS_WIDE, 4>), grid, dim3(256), 0, s, a);
     } else {
         const dim3 grid((unsigned)((a.blocks + 3) / 4), (unsigned)a.P);
-        if (!wide) EASGD_LAUNCH((adamw_own_kernel<GT, EIGHT, ACCESS_EACH>), grid, dim3(256), 0, s, a);
-        else if (update_nontemporal(moved)) EASGD_LAUNCH((adamw_own_kernel<GT, EIGHT, ACCESS_STREAM>), grid, dim3(256), 0, s, a);
+        if (stream) EASGD_LAUNCH((adamw_own_kernel<GT, EIGHT, ACCESS_STREAM>), grid, dim3(256), 0, s, a);
         else EASGD_LAUNCH((adamw_own_kernel<GT, EIGHT, ACCESS_WIDE>), grid, dim3(256), 0, s, a);
     }
 }
@@ -685,13 +684,11 @@ template <bool EIGHT> static int adamw(const char *name, AdamwArgs a, int dtype,
     clear_error();
     a.blocks = (a.N + 255) / 256;
     if (a.tensors == 0) a.ends = nullptr;
-    const size_t size = dtype_bytes(dtype);
-    const bool wide = a.ld % 4 == 0 && aligned16(a.W) && aligned16(a.Wc) && aligned_to(a.G, 4 * size) && aligned_to(a.M, EIGHT ? 4 : 16) && aligned_to(a.S, EIGHT ? 4 : 16);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     by_dtype(dtype, [&](auto gt) {
         constexpr int GT = decltype(gt)::value;
-        if (a.Wc) launch_adamw<GT, EIGHT, true>(a, wide, s);
-        else launch_adamw<GT, EIGHT, false>(a, wide, s);
+        if (a.Wc) launch_adamw<GT, EIGHT, true>(a, s);
+        else launch_adamw<GT, EIGHT, false>(a, s);
     });
     return check_launch(name);
 }
