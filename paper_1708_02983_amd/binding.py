@@ -805,17 +805,18 @@ def adamw_round(W, M, S, G, step, eta, Wc=None, rho: float = 0.0, beta1: float =
     wptr, _, P, N, ld, on = _replica_rows("W", W, N)
     if W.dtype != _F32:
         raise TypeError(f"W must be torch.float32, got {W.dtype}")
-    gptr, code, *_ = _replica_rows("G", G, N)
     shape = (P, ld)
-    if G.shape != shape:
-        raise ValueError(f"G must be {list(shape)}, got {list(G.shape)}")
-    eight = M.dtype == torch.float8_e4m3fn
+    code = _LOGIT_TYPES.get(getattr(G, "dtype", None))
+    if code is None:
+        raise TypeError("G must be a torch.float32, torch.bfloat16 or torch.float16 tensor")
+    gptr = _given("G", G, G.dtype, shape, on)
+    eight = getattr(M, "dtype", None) == torch.float8_e4m3fn
     mptr = _given("M", M, torch.float8_e4m3fn if eight else _F32, shape, on)
     sptr = _given("S", S, torch.float8_e5m2 if eight else _F32, shape, on)
     n, ends, rates, decays = 0, None, None, None
     if tensors is not None:
         ends, rates, decays = tensors
-        n = ends.numel()
+        n = len(ends)
         ends, rates, decays = _given("ends", ends, torch.int64, (n,), on), _given("rates", rates, _F32, (n,), on), _given("decays", decays, _F32, (n,), on)
     step_at = eta_at = None
     if isinstance(step, torch.Tensor):

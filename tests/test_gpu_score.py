@@ -243,3 +243,70 @@ def test_one_call_and_two_agree(hip):
                 down[j] -= 1e-4
                 slope = (ot.token_loss(up, t, 1.0, 0.5)[0] - ot.token_loss(down, t, 1.0, 0.5)[0]) / 2e-4
                 assert abs(d[r, j].item() - slope) <= 1e-6
+
+
+@pytest.mark.parametrize("V,rows", [(5, 12), (700, 12), (3000, 12), (20000, 12), (20000, 264), (70000, 264)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+def test_losses_of_rows_with_masks_and_numbers_that_are_none(hip, V, rows, dtype):
+    """The rows of test_masks_and_numbers_that_are_none through the one call, held whole and in parts, and large logits among them."""
+    rng = np.random.default_rng(V)
+    z = rng.normal(size=(12, V)) * 2
+    ninf, inf = -np.inf, np.inf
+    z[0] = ninf
+    z[1] = ninf
+    z[1, V // 2] = 1.5
+    z[2] = ninf
+    z[2, V // 2] = 1.5
+    z[3, : V // 2] = ninf
+    z[4, V // 2:] = ninf
+    z[5, ::2] = ninf
+    z[6, V - 1] = inf
+    z[7, 0] = np.nan
+    z[8] = np.float32(6e4) + rng.normal(size=V) * 3 if dtype == "fp16" else np.float32(3e8) + rng.normal(size=V) * 3      # differences count
+    z[8] = np.minimum(z[8], 6.5e4) if dtype == "fp16" else z[8]
+    z[9, :] = np.finfo(np.float16).min
+    z[9, V // 3] = 2.0
+    z[10, :] = 3.0
+    z[11, 3:] += 60.0                                   # far above what the row begins with
+    tokens = np.array([1, V // 2, 0, V - 1, V // 4, 2, 1, 1, 0, 1, V - 1, V - 1])
+    times = rows // 12
+    dz, z64 = place(np.tile(z, (times, 1)), dtype)
+    given = torch.tensor(np.tile(tokens, times), dtype=torch.int32, device="cuda")
+    for bonus in (0.0, 0.25):
+        loss, logprob, entropy, d = hip.easgd_token_loss(dz, given, bonus=bonus, entropy=True)
+        first = [x[:12].clone() for x in (loss, logprob, entropy, d)]
+        for i in range(1, times):                       # the same rows give the same bits wherever they are on the same grid
+            if (i * 12 * V * dz.element_size()) % 16 == 0:
+                assert all(torch.equal(x[12 * i:12 * i + 12].view(torch.uint8), y.view(torch.uint8)) for x, y in zip((loss, logprob, entropy, d), first))
+        loss, logprob, entropy, d = (x.double().cpu().numpy() for x in first)
+        for r in range(12):
+            token = int(tokens[r])
+            want, grad = ot.token_loss(z64[r], token, 1.0, bonus)
+            lp, h, *_ = ot.score(z64[r], token)
+            with np.errstate(invalid="ignore"):
+                e_lp, e_h = bounds(z64[r], token, 1.0)
+            e_lp += U * abs(lp) if np.isfinite(lp) else 0.0
+            assert close(logprob[r], lp, e_lp) and close(entropy[r], h, e_h), (r, logprob[r], lp, entropy[r], h)
+            assert close(loss[r], want, e_lp + bonus * e_h + 2 * U * abs(want)), (r, loss[r], want)
+            if np.isnan(grad).any():
+                assert np.isnan(d[r]).all(), r
+                continue
+            # masked rows: 0 exactly; where one place has all of the mass, 1 - q is 0 but for the sum's error
+            bound = gradient_bound(z64[r], token, 1.0, -1.0, -bonus, grad, dtype)
+            if (z64[r] > -np.inf).any():
+                bound[token] += sum_error(V)
+            off = np.abs(d[r] - grad) - bound
+            assert (off <= 0).all(), (r, int(off.argmax()), d[r][off.argmax()], grad[off.argmax()], bound[off.argmax()])
+
+
+@pytest.mark.parametrize("T", [1e-6, 1e-3, 1e6])
+@pytest.mark.parametrize("V", [50, 3000, 20000])
+def test_temperatures(hip, V, T):
+    rng = np.random.default_rng(V)
+    z = rng.normal(size=(6, V)) * (3 * T if T < 1 else 3)
+    z[1] = rng.normal(size=V) * 5                       # far apart, or nearly equal, at such a temperature
+    z[2, ::2] = -np.inf
+    tokens = rng.integers(0, V, 6)
+    tokens[0], tokens[2] = z[0].argmax(), 1
+    check(hip, z, tokens, T=T, k=3, a=np.ones(6), b=np.ones(6))
+    check(hip, z, tokens, T=T, k=0, a=np.ones(6), b=np.ones(6))
