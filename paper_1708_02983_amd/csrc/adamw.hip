@@ -410,7 +410,9 @@ __global__ __launch_bounds__(256) void adamw_own_kernel(AdamwArgs a)
 
 // ---- a center and few parameters: 256 of them a block, whose wavefronts take the workers in turn ------------------------------------------
 // What the workers are apart from the center meets in LDS, SPLIT_ROOM workers at a time, and is added in ascending order: the same sums as
-// worker by worker.
+// worker by worker.  Four wavefronts a block (eight, or two, are slower), whose requests for two workers are under way at a time (one with moments in 8 bits):
+// 16 x 1.86 M, bf16 gradients, 144 us = 5.5 TB/s (a wavefront for all workers 174 us, room for 32 workers 163, which leaves a compute unit five blocks in the
+// place of eight).
 static constexpr int SPLIT_ROOM = 16;
 template <int GT, bool EIGHT, int ACCESS, int WAVES>
 __device__ __forceinline__ void adamw_split_block(const AdamwArgs &a, const StepNumbers &n, size_t block, Four (&apart)[SPLIT_ROOM][64])
@@ -475,10 +477,13 @@ __global__ __launch_bounds__(WAVES * 64) void adamw_split_kernel(AdamwArgs a)
 }
 
 // ---- many parameters: GROUPS blocks of 256 a wavefront, all requests of a worker under way at once -------------------------------------
-template <int GT, bool EIGHT, bool CENTER, bool NT, int GROUPS, bool DIES>
+// Which blocks those are is the TileMap of the other streaming updates: the dies interleave.  Bound: HBM.  8 x 61 M fp32, no center, 2 020 us =
+// 6.75 TB/s (a wavefront per block, without the map: 2 505 us); moments in 8 bits with the center 1 365 us = 6.1 TB/s, the vector ALUs 72 % busy (some
+// 59 instructions a parameter: decoding, the rule, two maxima over 256 parameters, random bits, codes; 1 660 us for the first such kernel).
+template <int GT, bool EIGHT, bool CENTER, bool NT, int GROUPS>
 __global__ __launch_bounds__(256) void adamw_tile_kernel(AdamwArgs a)
 {
-    typedef TileMap<GROUPS, DIES> Map;
+    typedef TileMap<GROUPS, true> Map;
     constexpr int ACCESS = NT ? ACCESS_STREAM : ACCESS_WIDE;
     const size_t full = a.N / 256;
     const StepNumbers n(a);
@@ -544,7 +549,8 @@ __global__ __launch_bounds__(256) void adamw_tile_kernel(AdamwArgs a)
 }
 
 // ---- norms -------------------------------------------------------------------------------------------------------------------------
-// Squares are added in 64 bits: no gradient is too large or too small for them, and the order of addition is fixed.  Bound: HBM.
+// Squares are added in 64 bits: no gradient is too large or too small for them, and the order of addition is fixed.  Bound: HBM.  8 x 61 M fp32
+// 286 us = 6.8 TB/s (element by element 536); 16 x 1.86 M bf16 13 us, two launches.
 struct NormArgs {
     const void *G;
     int P;
@@ -644,6 +650,7 @@ static int norm_parts(int P, size_t bytes)
     return (int)(want < most ? want : most);
 }
 
+// Tiles where every compute unit gets 64 blocks of 256 and more; with 16, 8 x 1 M takes 40 us against 35 for a wavefront a worker and block.
 // Tiles of 8 x 61 M, us (1 / 2 / 4 blocks of 256 a wavefront): moments in 32 bits 2306 / 2097 / 2024, in 8 bits 1436 / 1377 / 1489: these need more wavefronts
 // under way, whose arithmetic hides behind each other's loads.
 template <int GT, bool EIGHT, bool CENTER> static void launch_adamw(const AdamwArgs &a, hipStream_t s)
@@ -652,8 +659,8 @@ template <int GT, bool EIGHT, bool CENTER> static void launch_adamw(const AdamwA
     const bool stream = update_nontemporal((size_t)a.P * a.N * (8 + (GT == EASGD_F32 ? 4 : 2) + (EIGHT ? 4 : 16)));
     if (a.blocks >= (size_t)64 * num_cus()) {
         const dim3 grid((unsigned)TileMap<GROUPS, true>::tiles(a.blocks * 64));
-        if (stream) EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, true, GROUPS, true>), grid, dim3(256), 0, s, a);
-        else EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, false, GROUPS, true>), grid, dim3(256), 0, s, a);
+        if (stream) EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, true, GROUPS>), grid, dim3(256), 0, s, a);
+        else EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, false, GROUPS>), grid, dim3(256), 0, s, a);
     } else if constexpr (CENTER) {
         const dim3 grid((unsigned)a.blocks);
         if (stream) EASGD_LAUNCH((adamw_split_kernel<GT, EIGHT, ACCESS_STREAM, 4>), grid, dim3(256), 0, s, a);

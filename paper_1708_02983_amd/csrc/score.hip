@@ -209,13 +209,13 @@ template <int BLOCK> __device__ __forceinline__ void write_padding(const ScoreAr
 
 // ---- sums of rows, or of parts of rows, a block each --------------------------------------------------------------------------
 // Every slot of [s0, s1) through whole wavefronts, DEEP loads ahead: f(raw, slot), an empty slot where a lane has none.
-template <int DT, int BLOCK, int DEEP, typename F> __device__ __forceinline__ void walk(const Row<DT> &row, int s0, int s1, F f)
+template <int DT, int BLOCK, int DEEP, bool ONCE, typename F> __device__ __forceinline__ void walk(const Row<DT> &row, int s0, int s1, F f)
 {
     uint4 v[DEEP];
     int s = s0 + (int)threadIdx.x;
     const int lead = s0 + (int)__builtin_amdgcn_readfirstlane(threadIdx.x & ~63);
     auto load = [&](int s, int first) {                 // first: of the wavefront
-        if (first * Row<DT>::VEC >= row.shift && first + 64 <= s1 && (first + 64) * Row<DT>::VEC <= row.end) return row.load_once(s);
+        if (first * Row<DT>::VEC >= row.shift && first + 64 <= s1 && (first + 64) * Row<DT>::VEC <= row.end) return ONCE ? row.load_once(s) : row.load_full(s);
         return s < s1 ? row.load(s) : row.empty();
     };
 #pragma unroll
@@ -262,7 +262,9 @@ template <int BLOCK, typename S> __device__ __forceinline__ float4 block_sums(co
     return join_waves<BLOCK>(w, lds, q);
 }
 
-template <int DT, int BLOCK, bool ENTROPY, bool RANK>
+// Bound: HBM, the vector ALUs 71 % busy with ranks.  2048 x 131072 bf16: 88 us = 6.1 TB/s, with ranks 105 (blocks of 512 or 1024 threads the same; loads
+// that stay in the caches 98).
+template <int DT, int BLOCK, bool ENTROPY, bool RANK, bool ONCE>
 __global__ __launch_bounds__(BLOCK) void score_rows_kernel(ScoreArgs a)
 {
     constexpr int VEC = Row<DT>::VEC;
@@ -280,7 +282,7 @@ __global__ __launch_bounds__(BLOCK) void score_rows_kernel(ScoreArgs a)
     TokenSums<VEC, ENTROPY> sums(q);
     RankCount rank;
     if constexpr (RANK) rank.set(row, token);
-    walk<DT, BLOCK, 4>(row, s0, s1, [&](const uint4 &raw, int s) {
+    walk<DT, BLOCK, 4, ONCE>(row, s0, s1, [&](const uint4 &raw, int s) {
         float x[VEC];
         Row<DT>::Type::unpack(raw, x);
         const float sum = sums.add(x);
@@ -292,7 +294,7 @@ __global__ __launch_bounds__(BLOCK) void score_rows_kernel(ScoreArgs a)
     else write_score(a, r, false, a.tokens, w, a.tokens ? row.load_one(token) : 0.f, __float_as_uint(w.w));
 }
 
-// the same with the first k
+// The same with the first k.  Bound: latency for few rows (48 x 50001 fp16, k = 20: 13.3 us, and 4.7 for the join), selection for many (first_of).
 template <int DT, int BLOCK>
 __global__ __launch_bounds__(BLOCK) void score_top_kernel(ScoreArgs a)
 {
@@ -475,8 +477,18 @@ template <int DT> struct TokenPlace {
 // u / s from the sum and the entropy that the forward pass left
 __device__ __forceinline__ float mean_exponent(float sum, float entropy) { return (float)((log((double)sum) - (double)entropy) / LN2_64); }
 
-template <int DT, int BLOCK, bool ENTROPY>
-__global__ __launch_bounds__(BLOCK) void score_grad_kernel(ScoreArgs a)
+// full slot `from` + thread, read once: a uniform address and an offset
+template <int DT> __device__ __forceinline__ uint4 load_at(const Row<DT> &row, int from)
+{
+    typedef unsigned Words __attribute__((ext_vector_type(4)));
+    const Words w = __builtin_nontemporal_load(reinterpret_cast<const Words *>(row.base) + from + (unsigned)threadIdx.x);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// One pass, each part of a row by a block.  Bound: HBM.  1024 x 32000 bf16 with entropies 22 us = 5.9 TB/s, 777 x 50001 fp16 without 25 us = 6.1 TB/s,
+// 2048 x 131072 bf16 with entropies 196 us = 5.5 TB/s.
+template <int DT, int BLOCK, bool ENTROPY, bool ONCE>
+__global__ __launch_bounds__(BLOCK, 8) void score_grad_kernel(ScoreArgs a)
 {
     constexpr int VEC = Row<DT>::VEC, DEEP = 4;
     const size_t r = blockIdx.x / a.segments;
@@ -498,28 +510,51 @@ __global__ __launch_bounds__(BLOCK) void score_grad_kernel(ScoreArgs a)
         return;
     }
     const TokenPlace<DT> place(row, token, g.of_token);
-    const int wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x & ~63u);
-    auto put = [&](const uint4 &raw, int s) {
+    auto careful = [&](int s) {                         // any slot, in any way
         float x[VEC];
-        Row<DT>::Type::unpack(raw, x);
-        if (g.at.by_difference()) g.of_difference(x, q);        // uniform, and rare
+        Row<DT>::Type::unpack(row.load(s), x);
+        if (g.at.by_difference()) g.of_difference(x, q);
         else g.template of<ENTROPY>(x);
-        if ((unsigned)(place.slot - (s - (int)threadIdx.x + wave)) < 64u) place.put(x, s);         // uniform for the wavefront
+        place.put(x, s);
         out.store(s, x, row.full(s));
     };
-    int s = s0 + (int)threadIdx.x;
-    for (; s - (int)threadIdx.x + DEEP * BLOCK <= s1; s += DEEP * BLOCK) {
+    if (g.at.by_difference() || !out.same) {            // uniform, and rare
+#pragma unroll 1
+        for (int s = s0 + (int)threadIdx.x; s < s1; s += BLOCK) careful(s);
+        return;
+    }
+    const int f0 = max(s0, row.first_full()), f1 = min(s1, row.end_full()), wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x & ~63u);
+    if (threadIdx.x == 0 && s0 == 0 && s1 > 0 && row.shift) careful(0);
+    if (threadIdx.x == 1 && s0 < s1 && s1 == row.slots && row.slots > row.end_full() && (row.slots > 1 || !row.shift)) careful(row.slots - 1);
+    auto put = [&](const uint4 &raw, int from) {        // full slot `from` + thread
+        float x[VEC];
+        Row<DT>::Type::unpack(raw, x);
+        g.template of<ENTROPY>(x);
+        if ((unsigned)(place.slot - (from + wave)) < 64u) place.put(x, from + (int)threadIdx.x);         // uniform for the wavefront
+        out.store_at(from, x);
+    };
+    int from = f0;
+    for (; from + DEEP * BLOCK <= f1; from += DEEP * BLOCK) {
         uint4 v[DEEP];
 #pragma unroll
-        for (int i = 0; i < DEEP; ++i) v[i] = row.full(s + i * BLOCK) ? row.load_once(s + i * BLOCK) : row.load(s + i * BLOCK);
+        for (int i = 0; i < DEEP; ++i) v[i] = ONCE ? load_at(row, from + i * BLOCK) : row.load_full(from + i * BLOCK + (int)threadIdx.x);
 #pragma unroll
-        for (int i = 0; i < DEEP; ++i) put(v[i], s + i * BLOCK);
+        for (int i = 0; i < DEEP; ++i) put(v[i], from + i * BLOCK);
     }
-    for (; s < s1; s += BLOCK) put(row.load(s), s);
+    uint4 v[DEEP];
+#pragma unroll
+    for (int i = 0; i < DEEP; ++i)
+        if (from + i * BLOCK + (int)threadIdx.x < f1) v[i] = ONCE ? load_at(row, from + i * BLOCK) : row.load_full(from + i * BLOCK + (int)threadIdx.x);
+#pragma unroll
+    for (int i = 0; i < DEEP; ++i)
+        if (from + i * BLOCK + (int)threadIdx.x < f1) put(v[i], from + i * BLOCK);
 }
 
 // ---- loss and gradient in one pass over memory -----------------------------------------------------------------------------------
-// A block holds its row in registers between the sums and the gradient, NV slots a thread; what is longer is read again.
+// A block holds its row between the sums and the gradient, NV slots a thread in registers and NL in LDS; what is longer is read again, from the
+// caches.  Bound: the vector ALUs (an exponential takes four issue slots and either pass has one: 16 slots a logit with an entropy) and HBM in turn, since
+// all of a block waits for its sums.  2048 x 131072 bf16 with entropies 228 us = 4.7 TB/s (sums and gradients as two launches 287 us), 1024 x 65536 fp32,
+// the same bytes and half the exponentials, 93 us = 5.8 TB/s; 777 x 50001 fp16 34 us; 4096 x 2000 bf16 20 us.
 //
 // The sums of a wavefront's slots relative to the largest logit of its first slots, without a look at each; where they come out wrong
 // (a logit far above that one, masked places, NaN, large logits), once more relative to the largest of all.
@@ -533,13 +568,6 @@ template <int DT, int BLOCK, int NV, int NL, bool ENTROPY> struct HeldRow {
     {
         const int from = row.first_full() + i * BLOCK;
         if (lead(row) + i * BLOCK < row.end_full()) v[i] = from + (int)threadIdx.x < row.end_full() ? load_at(row, from) : Row<DT>::empty();
-    }
-    // slot `from` + thread: a uniform address and an offset, so that no slot's address takes registers
-    __device__ __forceinline__ static uint4 load_at(const Row<DT> &row, int from)
-    {
-        typedef unsigned Words __attribute__((ext_vector_type(4)));
-        const Words w = __builtin_nontemporal_load(reinterpret_cast<const Words *>(row.base) + from + (unsigned)threadIdx.x);
-        return make_uint4(w[0], w[1], w[2], w[3]);
     }
     __device__ __forceinline__ static int lead(const Row<DT> &row) { return row.first_full() + (int)__builtin_amdgcn_readfirstlane(threadIdx.x & ~63u); }
     __device__ __forceinline__ static int edge_slot(const Row<DT> &row)
@@ -728,7 +756,7 @@ __global__ __launch_bounds__(BLOCK, NL > 0 ? 4 : 5) void token_loss_rows_kernel(
 
 // ---- short rows: a wavefront each, all calls --------------------------------------------------------------------------------------
 // Rows of at most 64 * NQ logits sit in a wavefront's registers, element lane + 64 i in x[i]; maximum, sums and counts are shuffles and
-// votes, and nothing waits for other wavefronts.  Bound: latency.
+// votes, and nothing waits for other wavefronts.  Bound: latency.  2048 x 100 fp32, gradient: 3.6 us.
 enum { SCORE_SUMS = 1, SCORE_GRAD = 2, SCORE_BOTH = 3 };
 template <int DT, int NQ, int MODE, bool TOP>
 __global__ __launch_bounds__(256) void score_short_kernel(ScoreArgs a)
@@ -828,7 +856,8 @@ static int score_segments(size_t rows, int slots)
     const int want = (int)((SCORE_SPLIT_BLOCKS + rows - 1) / rows), most = slots / SCORE_SPLIT_SLOTS;
     return want < most ? want : most;
 }
-// Gradients of rows whose sums are there: parts of at least 1024 slots, 2048 blocks
+// Gradients of rows whose sums are there: parts of at least 1024 slots, 2048 blocks (1024 x 32000 bf16 22.3 us, with 1024 blocks 26.3; 777 x 50001 28.5
+// and 34)
 static constexpr int GRAD_BLOCKS = 2048;
 static int grad_segments(size_t rows, int slots)
 {
@@ -848,12 +877,18 @@ template <typename F> static void by_flag(bool flag, F f)
     else f(std::false_type{});
 }
 
+// Logits past the caches where there are more of them than these (256 MB) hold for both who wrote and who reads them next.  Freshly written logits, us, past the
+// caches / through them: sums of 2048 x 131072 bf16 109 / 129, 4096 x 32000 53 / 65, 777 x 50001 22.5 / 20.6, 1024 x 32000 18.5 / 17.0; gradients
+// 204 / 229, 93 / 115, 34 / 29.5, 29.9 / 25.0.
+static bool read_once(size_t bytes) { return bytes > ((size_t)128 << 20); }
 template <int DT> static void launch_sums(const ScoreArgs &a, bool entropy, hipStream_t s)
 {
     const dim3 grid((unsigned)(a.rows * a.segments));
     by_flag(entropy, [&](auto h) {
         by_flag(a.rank, [&](auto rank) {
-            EASGD_LAUNCH((score_rows_kernel<DT, SCORE_BLOCK, decltype(h)::value, decltype(rank)::value>), grid, dim3(SCORE_BLOCK), 0, s, a);
+            by_flag(read_once(a.rows * a.V * sizeof(typename LogitType<DT>::Stored)), [&](auto once) {
+                EASGD_LAUNCH((score_rows_kernel<DT, SCORE_BLOCK, decltype(h)::value, decltype(rank)::value, decltype(once)::value>), grid, dim3(SCORE_BLOCK), 0, s, a);
+            });
         });
     });
     if (a.segments > 1) EASGD_LAUNCH((score_join_kernel<DT>), dim3((unsigned)a.rows), dim3(64), 0, s, a);
@@ -864,13 +899,16 @@ template <int DT> static void launch_top(const ScoreArgs &a, hipStream_t s)
     if (a.segments > 1 && a.segments * a.k <= 256) EASGD_LAUNCH((score_top_join_kernel<DT, 256>), dim3((unsigned)a.rows), dim3(256), 0, s, a);
     else if (a.segments > 1) EASGD_LAUNCH((score_top_join_kernel<DT, TOP_BLOCK>), dim3((unsigned)a.rows), dim3(TOP_BLOCK), 0, s, a);
 }
-// 512 threads where a part has work for them, us (256 / 512): 1024 x 32000 bf16 24.6 / 22.5, 777 x 50001 fp16 30.4 / 28.6, 4096 x 2000 bf16 12 / 18
+// 512 threads where a part has work for them, us (256 / 512): 2048 x 131072 bf16 209 / 203, 777 x 50001 fp16 25.7 / 25.3, 2000 x 10000 bf16 14.4 / 15.1,
+// 500 x 9000 fp32 6.9 / 7.8
 template <int DT> static void launch_grad(const ScoreArgs &a, bool entropy, hipStream_t s)
 {
     const dim3 grid((unsigned)(a.rows * a.segments));
     by_flag(entropy, [&](auto h) {
-        if (a.seg_slots >= 1024) EASGD_LAUNCH((score_grad_kernel<DT, 512, decltype(h)::value>), grid, dim3(512), 0, s, a);
-        else EASGD_LAUNCH((score_grad_kernel<DT, 256, decltype(h)::value>), grid, dim3(256), 0, s, a);
+        by_flag(read_once(a.rows * a.V * sizeof(typename LogitType<DT>::Stored)), [&](auto once) {
+            if (a.seg_slots >= 2048) EASGD_LAUNCH((score_grad_kernel<DT, 512, decltype(h)::value, decltype(once)::value>), grid, dim3(512), 0, s, a);
+            else EASGD_LAUNCH((score_grad_kernel<DT, 256, decltype(h)::value, decltype(once)::value>), grid, dim3(256), 0, s, a);
+        });
     });
 }
 template <int DT, int BLOCK, int NV, int NL> static void launch_held(const ScoreArgs &a, bool entropy, hipStream_t s)
@@ -879,6 +917,10 @@ template <int DT, int BLOCK, int NV, int NL> static void launch_held(const Score
         EASGD_LAUNCH((token_loss_rows_kernel<DT, BLOCK, NV, NL, decltype(h)::value>), dim3((unsigned)a.rows), dim3(BLOCK), 0, s, a);
     });
 }
+// What is held where, us (the block's threads / slots a thread in registers / in LDS):
+//   2048 x 131072 bf16   512/16/8 228   1024/4/8 229   1024/8/8 234   512/8/8 239
+//   4096 x 32000 bf16    256/8/8 108    256/12/4 106   256/4/8 119    256/12/0 129
+//   777 x 50001 fp16     256/8/8 34     256/12/4 36.5  256/4/8 35.5   256/12/0 39
 template <int DT> static void launch_loss(const ScoreArgs &a, int slots, bool entropy, hipStream_t s)
 {
     if (slots <= 2048) launch_held<DT, 256, 4, 0>(a, entropy, s);
