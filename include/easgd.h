@@ -12,6 +12,7 @@
  *                                   backward propagation
  *   extension     *_bf16, *_bf16v   the same updates with gradients and/or momentum buffers
  *                                   stored as bfloat16 (fp32 replicas, center and arithmetic)
+ *   extension     adamw_round*      steps (2)-(5) with AdamW as the worker rule
  *
  * Conventions shared by every entry point
  *   - every pointer marked DEVICE is a device (HBM) pointer owned by the caller;
@@ -31,7 +32,8 @@
  *   - process-wide state: the launch-shape options below, a launch counter, and per device
  *     what easgd_mlp_round and easgd_grad_static create on first use (described there);
  *   - all floating point is IEEE fp32 (storage and arithmetic), except the *_bf16 / *_bf16v entry points,
- *     which keep fp32 arithmetic and store gradients and momentum buffers as bfloat16;
+ *     which keep fp32 arithmetic and store gradients and momentum buffers as bfloat16, and the calls that
+ *     name other types (rows of logits, adamw_round*, easgd_grad_norms);
  *   - matrix products accumulate in fp32, either with the fp32 matrix instruction or with bfloat16 ones on operands that
  *     are split into three bfloat16 parts without loss (six products of parts, the small ones summed apart; at least as
  *     close to the exact sums).  Results that meet an infinity, a NaN, a finite operand from 2^96 on or a sum from 2^64 on

@@ -8,6 +8,8 @@
 
 namespace easgd {
 
+typedef float Four __attribute__((ext_vector_type(4)));
+
 struct AdamwArgs {
     float *W;
     void *M, *S;
@@ -107,22 +109,37 @@ struct Pace {
         }
     }
 };
-// The same for the blocks of a tile: two numbers a block, and a walk anew where a tensor ends inside one.
+// The same for the blocks of a tile: two numbers a block, and eight a lane, kept in LDS, where a tensor ends inside one.
 template <int GROUPS> struct TilePace {
     float rate[GROUPS], decay[GROUPS];
     bool one[GROUPS];
-    __device__ __forceinline__ void set(const AdamwArgs &a, const StepNumbers &n, int q, size_t block, size_t)
+    Four (*lanes)[2][256];             // [GROUPS]: rates and decays, a thread's own
+    __device__ __forceinline__ explicit TilePace(Four (*lanes)[2][256]) : lanes(lanes) {}
+    __device__ __forceinline__ void set(const AdamwArgs &a, const StepNumbers &n, int q, size_t block, size_t j)
     {
         const TensorWalk tensor(a, block * 256);
         one[q] = in_one_tensor(tensor, block);
         const float eta = n.eta * tensor.rate();
         rate[q] = eta * n.by1;
         decay[q] = eta * tensor.decay();
+        if (!one[q]) {                                  // uniform for the wavefront
+            const Pace pace(a, n, block, j);
+            lanes[q][0][threadIdx.x] = (Four){pace.rate[0], pace.rate[1], pace.rate[2], pace.rate[3]};
+            lanes[q][1][threadIdx.x] = (Four){pace.decay[0], pace.decay[1], pace.decay[2], pace.decay[3]};
+        }
     }
-    __device__ __forceinline__ Pace of(const AdamwArgs &a, const StepNumbers &n, int q, size_t j) const
+    __device__ __forceinline__ Pace of(int q) const
     {
-        if (one[q]) return Pace(rate[q], decay[q]);
-        return Pace(a, n, __builtin_amdgcn_readfirstlane((unsigned)(j >> 8)), j);
+        Pace pace(rate[q], decay[q]);
+        if (!one[q]) {
+            const Four r = lanes[q][0][threadIdx.x], d = lanes[q][1][threadIdx.x];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                pace.rate[e] = r[e];
+                pace.decay[e] = d[e];
+            }
+        }
+        return pace;
     }
 };
 
@@ -221,7 +238,6 @@ __device__ __forceinline__ unsigned wave_max_bits(unsigned v)
 }
 
 // ---- four consecutive parameters of a lane ------------------------------------------------------------------------------------
-typedef float Four __attribute__((ext_vector_type(4)));
 // How they are accessed: at once past the caches (what is read once and written once), at once, or element by element with a look at the
 // row's end (the last 256 parameters).  The hardware's wide accesses need the element's alignment only, so rows of any stride take them.
 enum { ACCESS_STREAM, ACCESS_WIDE, ACCESS_EACH };
@@ -480,10 +496,10 @@ __global__ __launch_bounds__(WAVES * 64) void adamw_split_kernel(AdamwArgs a)
 // Which blocks those are is the TileMap of the other streaming updates: the dies interleave.  Bound: HBM.  8 x 61 M fp32, no center, 2 020 us =
 // 6.75 TB/s (a wavefront per block, without the map: 2 505 us); moments in 8 bits with the center 1 365 us = 6.1 TB/s, the vector ALUs 72 % busy (some
 // 59 instructions a parameter: decoding, the rule, two maxima over 256 parameters, random bits, codes; 1 660 us for the first such kernel).
-template <int GT, bool EIGHT, bool CENTER, bool NT, int GROUPS>
+template <int GT, bool EIGHT, bool CENTER, bool NT, int GROUPS, bool DIES>
 __global__ __launch_bounds__(256) void adamw_tile_kernel(AdamwArgs a)
 {
-    typedef TileMap<GROUPS, true> Map;
+    typedef TileMap<GROUPS, DIES> Map;
     constexpr int ACCESS = NT ? ACCESS_STREAM : ACCESS_WIDE;
     const size_t full = a.N / 256;
     const StepNumbers n(a);
@@ -501,7 +517,8 @@ __global__ __launch_bounds__(256) void adamw_tile_kernel(AdamwArgs a)
     }
     size_t j[GROUPS];
     float c[GROUPS][4], sum[GROUPS][4] = {};
-    TilePace<GROUPS> pace;
+    __shared__ Four lanes[GROUPS][2][256];
+    TilePace<GROUPS> pace(lanes);
 #pragma unroll
     for (int q = 0; q < GROUPS; ++q) {
         j[q] = (first + q * Map::STRIDE) * 4;
@@ -520,7 +537,7 @@ __global__ __launch_bounds__(256) void adamw_tile_kernel(AdamwArgs a)
 #pragma unroll
         for (int q = 0; q < GROUPS; ++q) {
             float move[4] = {};
-            if (clip != 0.f) worker[q].step(a, i, j[q], clip, pace.of(a, n, q, j[q]), n, move);
+            if (clip != 0.f) worker[q].step(a, i, j[q], clip, pace.of(q), n, move);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if constexpr (CENTER) {
@@ -659,8 +676,12 @@ template <int GT, bool EIGHT, bool CENTER> static void launch_adamw(const AdamwA
     const bool stream = update_nontemporal((size_t)a.P * a.N * (8 + (GT == EASGD_F32 ? 4 : 2) + (EIGHT ? 4 : 16)));
     if (a.blocks >= (size_t)64 * num_cus()) {
         const dim3 grid((unsigned)TileMap<GROUPS, true>::tiles(a.blocks * 64));
-        if (stream) EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, true, GROUPS>), grid, dim3(256), 0, s, a);
-        else EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, false, GROUPS>), grid, dim3(256), 0, s, a);
+        // codes of rows at other alignments share lines between neighbouring pieces: through the caches and one die after the other (30 x 6 M packed 690 us,
+        // interleaved past the caches 781; with moments in 32 bits there is no difference: 8 x 30 M 1 390 to 1 438 us)
+        const bool apart = EIGHT && (a.ld % 4 != 0 || !aligned_to(a.M, 4) || !aligned_to(a.S, 4));
+        if (apart) EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, false, GROUPS, !EIGHT>), dim3((unsigned)TileMap<GROUPS, !EIGHT>::tiles(a.blocks * 64)), dim3(256), 0, s, a);
+        else if (stream) EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, true, GROUPS, true>), grid, dim3(256), 0, s, a);
+        else EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, false, GROUPS, true>), grid, dim3(256), 0, s, a);
     } else if constexpr (CENTER) {
         const dim3 grid((unsigned)a.blocks);
         if (stream) EASGD_LAUNCH((adamw_split_kernel<GT, EIGHT, ACCESS_STREAM, 4>), grid, dim3(256), 0, s, a);
