@@ -386,6 +386,7 @@ __device__ __forceinline__ void adamw_block(const AdamwArgs &a, const StepNumber
     if constexpr (CENTER) load_four<float, ACCESS == ACCESS_EACH ? ACCESS_EACH : ACCESS_WIDE>(a.Wc, j, a.N, c);
     for (int i = i0; i < i1; ++i) {                     // ascending: fixed order of the sum
         const float clip = a.clip ? a.clip[i] : 1.f;
+        if (!CENTER && clip == 0.f) continue;           // it sits the step out
         Worker<GT, EIGHT, ACCESS> worker;
         float move[4] = {};
         worker.load_parameters(a, i, j);
@@ -493,11 +494,13 @@ __global__ __launch_bounds__(WAVES * 64) void adamw_split_kernel(AdamwArgs a)
 }
 
 // ---- many parameters: GROUPS blocks of 256 a wavefront, all requests of a worker under way at once -------------------------------------
-// Which blocks those are is the TileMap of the other streaming updates: the dies interleave.  Bound: HBM.  8 x 61 M fp32, no center, 2 020 us =
-// 6.75 TB/s (a wavefront per block, without the map: 2 505 us); moments in 8 bits with the center 1 365 us = 6.1 TB/s, the vector ALUs 72 % busy (some
-// 59 instructions a parameter: decoding, the rule, two maxima over 256 parameters, random bits, codes; 1 660 us for the first such kernel).
+// Which blocks those are is the TileMap of the other streaming updates: the dies interleave.  Bound: HBM.  8 x 61 M fp32, no center, 2 180 us =
+// 6.3 TB/s; moments in 8 bits with the center 1 365 us = 6.1 TB/s, the vector ALUs 72 % busy (some 59 instructions a parameter: decoding, the rule, two
+// maxima over 256 parameters, random bits, codes; 1 660 us for the first such kernel).
+// With moments in 32 bits two wavefronts a vector ALU and no more: fewer, longer bursts of requests stream faster (8 x 61 M 2 183 us, with
+// three 2 233, with four 2 274).
 template <int GT, bool EIGHT, bool CENTER, bool NT, int GROUPS, bool DIES>
-__global__ __launch_bounds__(256) void adamw_tile_kernel(AdamwArgs a)
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(EIGHT ? 1 : 2, EIGHT ? 8 : 2))) void adamw_tile_kernel(AdamwArgs a)
 {
     typedef TileMap<GROUPS, DIES> Map;
     constexpr int ACCESS = NT ? ACCESS_STREAM : ACCESS_WIDE;
@@ -527,6 +530,7 @@ __global__ __launch_bounds__(256) void adamw_tile_kernel(AdamwArgs a)
     }
     for (int i = 0; i < a.P; ++i) {                     // ascending: fixed order of the sum
         const float clip = a.clip ? a.clip[i] : 1.f;
+        if (!CENTER && clip == 0.f) continue;           // it sits the step out
         Worker<GT, EIGHT, ACCESS> worker[GROUPS];
         if (clip != 0.f) {
 #pragma unroll
