@@ -154,7 +154,6 @@ def _check(code: int) -> None:
 
 
 _raw_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device     # where a tensor on a GPU is at hand
 
 
 def _stream(stream) -> ctypes.c_void_p:
@@ -460,7 +459,7 @@ def _logit_rows(name: str, t: torch.Tensor):
         ld = max(V, 1)
     elif ld < V:
         raise ValueError(f"{name}: rows must not overlap (stride {ld}, length {V})")
-    here = _current_device()
+    here = torch.cuda.current_device()
     if t.get_device() != here:
         raise ValueError(f"{name} is on {t.device}, the current device is cuda:{here}")
     return t.data_ptr(), code, rows, V, ld
@@ -765,7 +764,7 @@ def _replica_rows(name: str, t, N: Optional[int]):
     P, ld, N = _replica_shape(t, N)
     if N < 1 or N > ld:
         raise ValueError(f"N must be in [1, {ld}], got {N}")
-    here = _current_device()
+    here = torch.cuda.current_device()
     if t.get_device() != here:
         raise ValueError(f"{name} is on {t.device}, the current device is cuda:{here}")
     return t.data_ptr(), code, P, N, ld, here
