@@ -153,7 +153,8 @@ __device__ __forceinline__ void adamw_moments(float &m, float &v, float g, const
 }
 // What four parameters move by: eta (m / (1 - b1^t) / (sqrt(v / (1 - b2^t)) + eps) + decay w).  The hardware's root and reciprocal are right to
 // one unit; it takes subnormal numbers for 0, so roots of what is below 2^-64 are taken of 2^64 times it.  eps is at least 1e-30: the
-// reciprocal is of a normal number.
+// reciprocal is of a normal number.  The quotient comes first and the rate then, as in the formula: rate times reciprocal may be above what 32 bits
+// hold (a large rate over a small eps) where the quotient is 0.
 __device__ __forceinline__ void adamw_move(const float (&w)[4], const float (&m)[4], const float (&v)[4], const Pace &pace, const StepNumbers &n, float (&move)[4])
 {
     float root[4];
@@ -166,7 +167,7 @@ __device__ __forceinline__ void adamw_move(const float (&w)[4], const float (&m)
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const float d = fmaf(root[q], n.by2, n.eps);
-        move[q] = fmaf(pace.decay[q], w[q], m[q] * (pace.rate[q] * __builtin_amdgcn_rcpf(d)));
+        move[q] = fmaf(pace.decay[q], w[q], m[q] * __builtin_amdgcn_rcpf(d) * pace.rate[q]);
     }
 }
 
