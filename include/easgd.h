@@ -230,8 +230,9 @@ int sync_sgd_round(float *W, float *V, const float *G,
  *   M_scale, S_scale   DEVICE in/out [P][ceil(N/256)] fp32: M[i][j] stands for e4m3(M[i][j]) * M_scale[i][j/256], likewise S (all 0 before the first step)
  * W moves by the new moments before they are rounded.  Then, with e such that the block's largest |M| is in [2^(e+7), 2^(e+8)) (its largest S in
  * [2^(e+14), 2^(e+15)); e >= -126), 2^e becomes the block's scale and every moment times 2^-e is rounded to one of its two neighbours at
- * random, up with its distance from the lower one as probability (16 bits of it), so that moments are exact on average; an S above 0 never becomes 0, and signs
- * are kept, also of zeros.
+ * random, up with its distance from the lower one as probability (16 bits of it), so that moments are exact on average.  The exception: an S above 0 never
+ * becomes 0, so one below 2^-16 of the block's scale (some 2^-30 of its largest S, where e is above -126) is always raised to that.
+ * Signs are kept, also of zeros.  M and S of a parameter are rounded with the same random bits.
  * The random bits of parameter j = 4 g + 2 w + h of worker i in step t are bits [16 h, 16 h + 16) of mix(g ^ mix(mix(seed + i*0x9E3779B1) +
  * t*0x85157AF5 + w*0x632BE5AB)) in 32-bit arithmetic, mix(x): x ^= x >> 16, x *= 0x6C8E9CF5, x ^= x >> 15, x *= 0x2F5D7A4B, x ^= x >> 16: stored codes
  * are the same for the same seed and step.  A block in which a new moment is infinite or NaN gets the scale NaN (its codes say nothing).

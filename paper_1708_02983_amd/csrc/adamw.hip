@@ -174,8 +174,8 @@ __device__ __forceinline__ void adamw_move(const float (&w)[4], const float (&m)
 // ---- moments in 8 bits -----------------------------------------------------------------------------------------------------
 // 256 consecutive parameters of a replica share a power of two per moment: the largest |m| of them lands in [2^7, 2^8) of e4m3,
 // the largest v in [2^14, 2^15) of e5m2, and a number x of 2^-e m (2^-e v) becomes one of its two neighbours, at random, with its
-// distance from the other one as probability: exact on average, where rounding to the nearest would never let v move (b2 = 0.999
-// changes it by 0.1 % a step, half a step of the type is 12 %).  Multiplied by 2^-120 (2^-112) the type's exponents are those of fp32,
+// distance from the other one as probability: exact on average (but for a v above 0 that is less than the type's smallest number: it is raised to that, never
+// 0), where rounding to the nearest would never let v move (b2 = 0.999 changes it by 0.1 % a step, half a step of the type is 12 %).  Multiplied by 2^-120 (2^-112) the type's exponents are those of fp32,
 // subnormal numbers included, so 16 random bits are added below the last kept one, and what is behind it is cut off.
 // The random bits of parameter j = 4 g + 2 w + h of worker i in step t are half h of mix(g ^ key(i, t, w)).
 __device__ __forceinline__ unsigned mix(unsigned x)

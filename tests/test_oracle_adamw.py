@@ -92,3 +92,18 @@ def test_blocks_with_nothing_or_without_end():
     tiny = np.full(3, 1e-44, F)
     mc, vc, ms, vs = oa.encode(tiny, tiny, 0, 1, 0)
     assert (vc >= 1).all()
+
+
+def test_the_smallest_second_moments_are_held_where_they_cannot_fall_below():
+    """What is exact on average and what is not: an S below 2^-16 of its block's scale is always stored as that, whatever the random bits are, and stays there
+    as it decays; from there on up the mean is S itself."""
+    largest = F(1.5 * 2.0 ** 14)                        # the block's scale is 1
+    S = np.array([largest, 2.0 ** -16 * 0.999, 2.0 ** -40, 2.0 ** -149, 0.0, 2.0 ** -16, 2.0 ** -16 * 1.25], F)
+    seen = []
+    for step in range(1, 400):
+        _, codes, _, scale = oa.encode(np.zeros_like(S), S, 0, step, 3)
+        assert scale[0] == 1.0 and codes[1:6].tolist() == [1, 1, 1, 0, 1]
+        seen.append(oa.decode_s(codes[None], scale[None])[0])
+    assert set(seen[i][6] for i in range(len(seen))) == {F(2.0 ** -16), F(2.0 ** -15)}
+    # 399 roundings with a deviation of less than half a step each: five deviations
+    assert abs(np.mean([x[6] for x in seen]) - S[6]) < 2.0 ** -16 * 2.5 / np.sqrt(len(seen))
