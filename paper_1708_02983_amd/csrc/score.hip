@@ -556,8 +556,11 @@ __global__ __launch_bounds__(BLOCK, 8) void score_grad_kernel(ScoreArgs a)
 // all of a block waits for its sums.  2048 x 131072 bf16 with entropies 228 us = 4.7 TB/s (sums and gradients as two launches 287 us), 1024 x 65536 fp32,
 // the same bytes and half the exponentials, 93 us = 5.8 TB/s; 777 x 50001 fp16 34 us; 4096 x 2000 bf16 20 us.
 //
-// The sums of a wavefront's slots relative to the largest logit of its first slots, without a look at each; where they come out wrong
-// (a logit far above that one, masked places, NaN, large logits), once more relative to the largest of all.
+// The sums of a wavefront's slots relative to the largest logit of its first slots, without a look at each; where they come out wrong (a lane's sum above
+// 2^12, as by a logit 8.3 T above that one; large logits, NaN; with entropies masked places, 0 times infinity), once more relative to the largest of all,
+// which takes two further passes over the wavefront's slots.  With entropies an empty slot of a lane is a masked place, too: the first wavefront of every
+// row, whose lanes without a partial slot at the row's ends hold an empty one, and a wavefront whose last slots are not all there always take them, while the others
+// wait for their sums.
 template <int DT, int BLOCK, int NV, int NL, bool ENTROPY> struct HeldRow {
     using Type = LogitType<DT>;
     static constexpr int VEC = Type::VEC;
