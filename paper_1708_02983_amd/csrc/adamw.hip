@@ -429,7 +429,7 @@ __global__ __launch_bounds__(256) void adamw_own_kernel(AdamwArgs a)
 // ---- a center and few parameters: 256 of them a block, whose wavefronts take the workers in turn ------------------------------------------
 // What the workers are apart from the center meets in LDS, SPLIT_ROOM workers at a time, and is added in ascending order: the same sums as
 // worker by worker.  Four wavefronts a block (eight, or two, are slower), whose requests for two workers are under way at a time (one with moments in 8 bits):
-// 16 x 1.86 M, bf16 gradients, 144 us = 5.5 TB/s (a wavefront for all workers 174 us, room for 32 workers 163, which leaves a compute unit five blocks in the
+// 16 x 1.86 M, bf16 gradients, one worker sitting out, 142 us = 5.3 TB/s, all working 151 = 5.2 (a wavefront for all workers 174 us, room for 32 workers 163, which leaves a compute unit five blocks in the
 // place of eight).
 static constexpr int SPLIT_ROOM = 16;
 template <int GT, bool EIGHT, int ACCESS, int WAVES>
@@ -495,11 +495,12 @@ __global__ __launch_bounds__(WAVES * 64) void adamw_split_kernel(AdamwArgs a)
 }
 
 // ---- many parameters: GROUPS blocks of 256 a wavefront, all requests of a worker under way at once -------------------------------------
-// Which blocks those are is the TileMap of the other streaming updates: the dies interleave.  Bound: HBM.  8 x 61 M fp32, no center, 2 180 us =
-// 6.3 TB/s; moments in 8 bits with the center 1 365 us = 6.1 TB/s, the vector ALUs 72 % busy (some 59 instructions a parameter: decoding, the rule, two
-// maxima over 256 parameters, random bits, codes; 1 660 us for the first such kernel).
-// With moments in 32 bits two wavefronts a vector ALU and no more: fewer, longer bursts of requests stream faster (8 x 61 M 2 183 us, with
-// three 2 233, with four 2 274).
+// Which blocks those are is the TileMap of the other streaming updates: the dies interleave.  Bound: HBM.  8 x 61 M fp32, call after call on the same replicas:
+// moments in 32 bits 2 180 us = 6.3 TB/s, with the center 2 217 = 6.4; in 8 bits 1 322 us = 5.9 TB/s, with the center 1 360 = 6.1 (1 410 where other
+// calls come between), the vector ALUs 71 % busy (some 59 instructions a parameter: decoding, the rule, two maxima over 256 parameters, random bits, codes;
+// 1 660 us for the first such kernel).
+// With moments in 32 bits two wavefronts a vector ALU and no more: fewer, longer bursts of requests stream faster (without / with the center: 2 180 / 2 217 us,
+// with three 2 243 / 2 264, with four 2 245 / 2 489).
 template <int GT, bool EIGHT, bool CENTER, bool NT, int GROUPS, bool DIES>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(EIGHT ? 1 : 2, EIGHT ? 8 : 2))) void adamw_tile_kernel(AdamwArgs a)
 {
@@ -673,16 +674,16 @@ static int norm_parts(int P, size_t bytes)
 }
 
 // Tiles where every compute unit gets 64 blocks of 256 and more; with 16, 8 x 1 M takes 40 us against 35 for a wavefront a worker and block.
-// Tiles of 8 x 61 M, us (1 / 2 / 4 blocks of 256 a wavefront): moments in 32 bits 2306 / 2097 / 2024, in 8 bits 1436 / 1377 / 1489: these need more wavefronts
-// under way, whose arithmetic hides behind each other's loads.
+// Tiles of 8 x 61 M, us (1 / 2 / 4 blocks of 256 a wavefront): moments in 32 bits 2428 / 2237 / 2180, with the center 2671 / 2261 / 2217; in 8 bits 1420 / 1322 /
+// 1301, with the center 1415 / 1360 / 1471: these need more wavefronts under way, whose arithmetic hides behind each other's loads.
 template <int GT, bool EIGHT, bool CENTER> static void launch_adamw(const AdamwArgs &a, hipStream_t s)
 {
     constexpr int GROUPS = EIGHT ? 2 : 4;
     const bool stream = update_nontemporal((size_t)a.P * a.N * (8 + (GT == EASGD_F32 ? 4 : 2) + (EIGHT ? 4 : 16)));
     if (a.blocks >= (size_t)64 * num_cus()) {
         const dim3 grid((unsigned)TileMap<GROUPS, true>::tiles(a.blocks * 64));
-        // codes of rows at other alignments share lines between neighbouring pieces: through the caches and one die after the other (30 x 6 M packed 690 us,
-        // interleaved past the caches 781; with moments in 32 bits there is no difference: 8 x 30 M 1 390 to 1 438 us)
+        // codes of rows at other alignments share lines between neighbouring pieces: through the caches and one die after the other (30 x 6 M packed 680 us,
+        // interleaved past the caches 781; with moments in 32 bits there is no difference: 8 x 30 M 1 385 to 1 438 us)
         const bool apart = EIGHT && (a.ld % 4 != 0 || !aligned_to(a.M, 4) || !aligned_to(a.S, 4));
         if (apart) EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, false, GROUPS, !EIGHT>), dim3((unsigned)TileMap<GROUPS, !EIGHT>::tiles(a.blocks * 64)), dim3(256), 0, s, a);
         else if (stream) EASGD_LAUNCH((adamw_tile_kernel<GT, EIGHT, CENTER, true, GROUPS, true>), grid, dim3(256), 0, s, a);

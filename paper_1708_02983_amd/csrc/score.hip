@@ -262,7 +262,7 @@ template <int BLOCK, typename S> __device__ __forceinline__ float4 block_sums(co
     return join_waves<BLOCK>(w, lds, q);
 }
 
-// Bound: HBM, the vector ALUs 71 % busy with ranks.  2048 x 131072 bf16: 88 us = 6.1 TB/s, with ranks 105 (blocks of 512 or 1024 threads the same; loads
+// Bound: HBM, the vector ALUs 70 % busy with ranks.  2048 x 131072 bf16, call after call: 87 us = 6.2 TB/s, with ranks 104 (blocks of 512 or 1024 threads the same; loads
 // that stay in the caches 98).
 template <int DT, int BLOCK, bool ENTROPY, bool RANK, bool ONCE>
 __global__ __launch_bounds__(BLOCK) void score_rows_kernel(ScoreArgs a)
@@ -553,8 +553,9 @@ __global__ __launch_bounds__(BLOCK, 8) void score_grad_kernel(ScoreArgs a)
 // ---- loss and gradient in one pass over memory -----------------------------------------------------------------------------------
 // A block holds its row between the sums and the gradient, NV slots a thread in registers and NL in LDS; what is longer is read again, from the
 // caches.  Bound: the vector ALUs (an exponential takes four issue slots and either pass has one: 16 slots a logit with an entropy) and HBM in turn, since
-// all of a block waits for its sums.  2048 x 131072 bf16 with entropies 228 us = 4.7 TB/s (sums and gradients as two launches 287 us), 1024 x 65536 fp32,
-// the same bytes and half the exponentials, 93 us = 5.8 TB/s; 777 x 50001 fp16 34 us; 4096 x 2000 bf16 20 us.
+// all of a block waits for its sums.  2048 x 131072 bf16 with entropies 204 us = 5.3 TB/s call after call on the same logits, 228 on logits that were written just
+// before (sums and gradients as two launches 287), without entropies 181; 1024 x 65536 fp32, half the bytes and a quarter of the exponentials, 93 us = 5.8 TB/s;
+// 777 x 50001 fp16 34 us; 4096 x 2000 bf16 16 to 20 us.
 //
 // The sums of a wavefront's slots relative to the largest logit of its first slots, without a look at each; where they come out wrong (a lane's sum above
 // 2^12, as by a logit 8.3 T above that one; large logits, NaN; with entropies masked places, 0 times infinity), once more relative to the largest of all,
