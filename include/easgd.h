@@ -250,7 +250,8 @@ int adamw_round_8bit(float *W, uint8_t *M, uint8_t *S, float *M_scale, float *S_
 /*
  * The L2 norm of every worker's gradient, and the factor that brings it down to max_norm:
  *
- *     norm[i] = sqrt(G[i][0]^2 + ... + G[i][N-1]^2)        clip[i] = min(1, max_norm / norm[i]); 0 where norm[i] is infinite or NaN
+ *     norm[i] = sqrt(G[i][0]^2 + ... + G[i][N-1]^2)        clip[i] = min(1, max_norm / norm[i]); 0 where norm[i] is infinite or NaN,
+ *                                                          or the quotient rounds to it (below 2^-150)
  *
  *   G      DEVICE in [P][ld], dtype EASGD_F32, EASGD_BF16 or EASGD_F16
  *   norm   DEVICE out [P] fp32;  clip  DEVICE out [P] fp32, or NULL;  max_norm > 0 (infinity: no limit)
